@@ -52,7 +52,11 @@
 extern "C" {
 #endif
 
-typedef enum { PKMEM_F32 = 0, PKMEM_BF16 = 1 } pkmem_dtype;
+typedef enum {
+  PKMEM_F32 = 0,
+  PKMEM_BF16 = 1,
+  PKMEM_E4M3 = 2 /* 8 bits, 4 of exponent, largest 448 (OCP): only where a call names it */
+} pkmem_dtype;
 
 typedef enum {
   PKMEM_OK = 0,
@@ -355,6 +359,119 @@ int mem_bag_backward_sparse(const void* dy, const void* values, pkmem_dtype v_dt
                             void* ws, size_t ws_bytes, pkmem_stream_t stream);
 
 /* ------------------------------------------------------------------------ *
+ * Root-mean-square norm with the residual's addition: what stands in front of
+ * the query and gate projections of a memory block.
+ *   h[t,:] = x[t,:] + res[t,:]   added in fp32 and rounded once to dt: the
+ *                                stream as stored is what is normalised;
+ *   y[t,:] = h[t,:] * rstd[t] * weight,  rstd = 1 / sqrt(mean(h^2) + eps) in
+ *            fp32 (0 where mean + eps == 0), rounded once to y_dt.
+ *
+ *   x       [T, D] dtype dt (PKMEM_F32 or PKMEM_BF16).
+ *   res     [T, D] dtype dt; NULL: h = x.
+ *   weight  [D] dtype dt; NULL: ones.
+ *   D       D % 8 == 0, rows of at most 32 KiB (D <= 16384 bf16, 8192 fp32).
+ *   eps     >= 0 and finite.
+ *   sum_out [T, D] dtype dt: h; NULL to skip it.  May be x or res (in place).
+ *   y_out   [T, D] dtype y_dt, which is dt, or PKMEM_E4M3: y in 8 bits with one
+ *           scale a row, y ~ y_out * scale_out[t],
+ *           scale = max(max_j |y| / 448, 2^-126), codes to nearest even.
+ *   scale_out [T] fp32: required for PKMEM_E4M3, NULL otherwise.
+ * All buffers 16-byte aligned (scale_out 4).  T = 0 is a valid no-op.
+ * ------------------------------------------------------------------------ */
+int mem_rmsnorm(const void* x, const void* res, const void* weight, pkmem_dtype dt, int64_t T,
+                int D, float eps, void* sum_out, void* y_out, pkmem_dtype y_dt, float* scale_out,
+                pkmem_stream_t stream);
+
+/* ------------------------------------------------------------------------ *
+ * Backward of mem_rmsnorm (not of the 8-bit rounding).  With xh = h * rstd
+ * (recomputed from h as the forward did) and g = dy * weight:
+ *   dx_out      [T, D] dtype dt, written: rstd * (g - xh * mean(g * xh)) + dsum;
+ *               the gradient of x and of res alike.  May be dy, h or dsum.
+ *   grad_weight [D] fp32, ACCUMULATED: += sum_t dy * xh; NULL to skip it.
+ *               Bitwise deterministic (partial rows added in a fixed order).
+ *   dy, h       [T, D] dtype dt: the gradient of y; x (without res) or sum_out.
+ *   dsum        [T, D] dtype dt: what reaches h along the stream; NULL: none.
+ * Workspace: mem_rmsnorm_backward_workspace_size(T, D) bytes, 256-byte aligned
+ * (not needed, and may be NULL, without grad_weight).
+ * ------------------------------------------------------------------------ */
+size_t mem_rmsnorm_backward_workspace_size(int64_t T, int D);
+
+int mem_rmsnorm_backward(const void* dy, const void* h, const void* weight, pkmem_dtype dt,
+                         int64_t T, int D, float eps, const void* dsum, void* dx_out,
+                         float* grad_weight, void* ws, size_t ws_bytes, pkmem_stream_t stream);
+
+/* ------------------------------------------------------------------------ *
+ * Rows in 8 bits: q_out [R, C] PKMEM_E4M3 and scale_out [R] fp32 of
+ * x [R, C] dtype dt, as mem_rmsnorm writes them (for weights and activations
+ * of mem_linear's 8-bit products).  C % 8 == 0, rows of at most 32 KiB.
+ * ------------------------------------------------------------------------ */
+int mem_quantize_rows(const void* x, pkmem_dtype dt, int64_t R, int C, void* q_out,
+                      float* scale_out, pkmem_stream_t stream);
+
+/* ------------------------------------------------------------------------ *
+ * AdamW (decoupled weight decay) over many tensors in few launches.  With
+ * g = grad * *grad_scale (1 where grad_scale is NULL), t = step:
+ *   m = beta1 m + (1 - beta1) g;   v = beta2 v + (1 - beta2) g^2
+ *   p = p (1 - lr wd) - lr / (1 - beta1^t) * m / (sqrt(v) / sqrt(1 - beta2^t) + eps)
+ * in fp32; param, exp_avg and exp_avg_sq are updated in place.
+ *   param_dt  PKMEM_F32, or PKMEM_BF16 without a wider copy: the new value is
+ *             rounded up or down at random in proportion to what is cut off,
+ *             so that updates below half a step add up over the steps.
+ *   grad_dt   PKMEM_F32 or PKMEM_BF16.
+ *   state_dt  PKMEM_F32, or PKMEM_E4M3: exp_avg holds m, exp_avg_sq holds
+ *             sqrt(v), each as numel codes and ceil(numel / 128) fp32 scales,
+ *             one for each 128 consecutive elements (largest / 448), rounded at
+ *             random like bf16 parameters; a root above 0 stays above 0.  States
+ *             that are all zero start a run.  An element that is not finite
+ *             is stored as NaN and leaves its neighbours' scale alone.
+ * The random bits are a hash of (seed, step, position in the list, element):
+ * the same call gives the same result, bit for bit.
+ * lr_dev, step_dev and grad_scale are DEVICE scalars or NULL: with them the
+ * rate, the step number and the gradients' factor (a clipping factor, say) are
+ * read when the call runs, so a captured step can be replayed while they
+ * move on (lr and step are then not used).  Where *grad_scale is 0 or not
+ * finite the whole call changes nothing.
+ * Tensors of any length (0: skipped) and alignment; 16-byte aligned ones are
+ * fast.  No two may overlap.
+ * ------------------------------------------------------------------------ */
+typedef struct {
+  void* param;
+  const void* grad;
+  void* exp_avg;
+  void* exp_avg_sq;
+  float* exp_avg_scale;    /* PKMEM_E4M3 states only, else NULL */
+  float* exp_avg_sq_scale;
+  int64_t numel;
+  pkmem_dtype param_dt, grad_dt, state_dt;
+} pkmem_adamw_tensor;
+
+typedef struct {
+  double lr, beta1, beta2, eps, weight_decay; /* betas in [0, 1), others >= 0 */
+  int64_t step;                               /* 1 for the first */
+  uint64_t seed;
+  const float* lr_dev;
+  const int64_t* step_dev;
+  const float* grad_scale;
+} pkmem_adamw_opts;
+
+/* tensors, opts: host. */
+int mem_adamw(const pkmem_adamw_tensor* tensors, int count, const pkmem_adamw_opts* opts,
+              pkmem_stream_t stream);
+
+/* The same step on the touched rows of one table, as mem_bag_backward_sparse
+ * gives them: rows without a gradient keep value and states (no decay).
+ *   table      numel = N * D; param, exp_avg, exp_avg_sq [N, D]; grad [U, D]
+ *              PKMEM_F32 (grad_rows_out); PKMEM_E4M3 states need D % 128 == 0,
+ *              their scales are [N, D / 128], the same as mem_adamw's.
+ *   D          D % 8 == 0; all buffers 16-byte aligned.
+ *   rows       [U] int64, ascending, U <= 2^31 - 1.  Equal neighbours are one
+ *              row whose gradients are added in order; a row outside [0, N)
+ *              is passed over (with PKMEM_DEBUG both a row outside and a
+ *              descending list are errors). */
+int mem_adamw_rows(const pkmem_adamw_tensor* table, int64_t N, int D, const int64_t* rows,
+                   int64_t U, const pkmem_adamw_opts* opts, pkmem_stream_t stream);
+
+/* ------------------------------------------------------------------------ *
  * Benchmark instrumentation (host-side state; not thread-safe).
  * mem_timer_start(kernels) takes a comma-separated list of kernel names and
  * makes the library record a HIP event pair on the launch stream around every
@@ -367,6 +484,8 @@ int mem_bag_backward_sparse(const void* dy, const void* values, pkmem_dtype v_dt
  *   "gate_backward"                        (mem_gate_backward)
  *   "bag_backward_atomic", "sort_by_row",
  *   "bag_backward_rows", "softmax_backward" (mem_bag_backward[_sparse])
+ *   "rmsnorm", "rmsnorm_backward", "quantize_rows", "adamw", "adamw_rows"
+ *                                          (the calls of these names)
  * ("sort_by_row" spans the whole radix sort and segment pass.)
  * mem_timer_stop() stops recording.  mem_timer_read(ms_out, kernel_out, cap)
  * waits for the recorded events, writes up to cap entries in launch order to

@@ -29,9 +29,12 @@ __all__ = [
     "mem_bag_backward",
     "mem_bag_backward_sparse", "mem_search_workspace_size", "mem_bag_backward_workspace_size",
     "BWD_MODES", "F32", "BF16", "mem_timer_start", "mem_timer_stop", "mem_timer_read",
+    "E4M3", "mem_rmsnorm", "mem_rmsnorm_backward", "mem_quantize_rows",
+    "mem_adamw", "mem_adamw_rows", "mem_adamw_state", "ADAMW_STATE_BLOCK",
 ]
 
-F32, BF16 = 0, 1
+F32, BF16, E4M3 = 0, 1, 2
+ADAMW_STATE_BLOCK = 128  # elements that share the scales of 8-bit optimizer states
 NOALLOC_SCRATCH_BYTES = 128 << 20  # PKMEM_NOALLOC_SCRATCH_BYTES
 BWD_MODES = {"auto": 0, "atomic": 1, "sorted": 2}
 _HERE = os.path.dirname(os.path.abspath(__file__))
@@ -99,6 +102,18 @@ def load() -> ctypes.CDLL:
     L.mem_bag_backward_sparse.argtypes = [P, P, I32, I64, I32, P, P, I64, I32, I32, P, P, I64, P,
                                           P, P, P, SZ, P]
     L.mem_bag_backward_sparse.restype = I32
+    L.mem_rmsnorm.argtypes = [P, P, P, I32, I64, I32, F32, P, P, I32, P, P]
+    L.mem_rmsnorm.restype = I32
+    L.mem_rmsnorm_backward_workspace_size.argtypes = [I64, I32]
+    L.mem_rmsnorm_backward_workspace_size.restype = SZ
+    L.mem_rmsnorm_backward.argtypes = [P, P, P, I32, I64, I32, F32, P, P, P, P, SZ, P]
+    L.mem_rmsnorm_backward.restype = I32
+    L.mem_quantize_rows.argtypes = [P, I32, I64, I32, P, P, P]
+    L.mem_quantize_rows.restype = I32
+    L.mem_adamw.argtypes = [P, I32, P, P]
+    L.mem_adamw.restype = I32
+    L.mem_adamw_rows.argtypes = [P, I64, I32, P, I64, P, P]
+    L.mem_adamw_rows.restype = I32
     L.mem_last_error.argtypes = []
     L.mem_last_error.restype = ctypes.c_char_p
     L.mem_version.argtypes = []
@@ -550,3 +565,232 @@ def mem_bag_backward_sparse(dy: torch.Tensor, values: torch.Tensor, idx: torch.T
                                       _ptr(ws), ws.numel() * ws.element_size(), _stream(stream)))
     u = int(U.value)
     return rows[:u], grad_rows[:u], grad_w, grad_scores
+
+
+# ------------------------------------------------ norm, projections, optimizer
+def _here(*ts) -> None:
+    """The tensors lie, dense, on the device the call launches on."""
+    dev = None
+    for t in ts:
+        if t is None:
+            continue
+        if not t.is_cuda:
+            raise ValueError("tensors must be on the GPU")
+        if not t.is_contiguous():
+            raise ValueError("tensors must be contiguous")
+        if dev is None:
+            dev = t.device
+            if dev.index != torch._C._cuda_getDevice():
+                raise ValueError("tensors must be on the current device")
+        elif t.device != dev:
+            raise ValueError("tensors must be on one device")
+
+
+def _like(t, shape, dtype, what: str) -> None:
+    if t is not None and (tuple(t.shape) != tuple(shape) or t.dtype != dtype):
+        raise ValueError(f"{what} must be a {dtype} tensor of shape {tuple(shape)}")
+
+
+@_launches_on_stream
+def mem_rmsnorm(x: torch.Tensor, weight=None, residual=None, eps: float = 1e-5, *,
+                quantize: bool = False, sum_out=None, y_out=None, scale_out=None,
+                want_sum: bool = True, stream=None):
+    """Root-mean-square norm of h = x + residual ([T, D]; residual may be None).
+
+    Returns (y, h, scale): y in x's dtype and scale None, or with quantize y in
+    float8_e4m3fn with scale fp32 [T] (the norm is about y * scale[:, None]); h None
+    without a residual or with want_sum False (sum_out may be x or residual)."""
+    L = load()
+    _here(x, weight, residual, sum_out, y_out, scale_out)
+    T, D = x.shape
+    dt = _dt(x)
+    _like(weight, (D,), x.dtype, "weight")
+    _like(residual, (T, D), x.dtype, "residual")
+    if residual is None:
+        sum_out = None
+    elif sum_out is None and want_sum:
+        sum_out = torch.empty_like(x)
+    _like(sum_out, (T, D), x.dtype, "sum_out")
+    ydt = torch.float8_e4m3fn if quantize else x.dtype
+    if y_out is None:
+        y_out = torch.empty((T, D), dtype=ydt, device=x.device)
+    _like(y_out, (T, D), ydt, "y_out")
+    if not quantize:
+        scale_out = None
+    elif scale_out is None:
+        scale_out = torch.empty((T,), dtype=torch.float32, device=x.device)
+    _like(scale_out, (T,), torch.float32, "scale_out")
+    _check(L.mem_rmsnorm(_ptr(x), _ptr(residual), _ptr(weight), dt, T, D, float(eps), _ptr(sum_out),
+                         _ptr(y_out), E4M3 if quantize else dt, _ptr(scale_out), _stream(stream)))
+    return y_out, sum_out, scale_out
+
+
+@_launches_on_stream
+def mem_rmsnorm_backward(dy: torch.Tensor, h: torch.Tensor, weight=None, eps: float = 1e-5, *,
+                         dsum=None, dx=None, grad_weight=None, want_grad_weight: bool = True,
+                         workspace=None, stream=None):
+    """Backward of mem_rmsnorm: dy the gradient of y, h what was normalised (its sum,
+    or x without a residual), dsum what reaches h along the stream (or None).
+    Returns (dx [T, D] in dy's dtype, the gradient of x and residual alike; grad_weight
+    fp32 [D], ACCUMULATED: zeros are allocated if none is given)."""
+    L = load()
+    _here(dy, h, weight, dsum, dx, grad_weight, workspace)
+    T, D = dy.shape
+    _like(h, (T, D), dy.dtype, "h")
+    _like(weight, (D,), dy.dtype, "weight")
+    _like(dsum, (T, D), dy.dtype, "dsum")
+    if dx is None:
+        dx = torch.empty_like(dy)
+    _like(dx, (T, D), dy.dtype, "dx")
+    if grad_weight is None and want_grad_weight:
+        grad_weight = torch.zeros((D,), dtype=torch.float32, device=dy.device)
+    _like(grad_weight, (D,), torch.float32, "grad_weight")
+    ws = None
+    if grad_weight is not None:
+        ws = _workspace(int(L.mem_rmsnorm_backward_workspace_size(T, D)), dy.device, workspace)
+    _check(L.mem_rmsnorm_backward(_ptr(dy), _ptr(h), _ptr(weight), _dt(dy), T, D, float(eps),
+                                  _ptr(dsum), _ptr(dx), _ptr(grad_weight), _ptr(ws),
+                                  0 if ws is None else ws.numel() * ws.element_size(),
+                                  _stream(stream)))
+    return dx, grad_weight
+
+
+@_launches_on_stream
+def mem_quantize_rows(x: torch.Tensor, *, q_out=None, scale_out=None, stream=None):
+    """Rows of x [R, C] in 8 bits: (q float8_e4m3fn [R, C], scale fp32 [R]), x about
+    q * scale[:, None]."""
+    L = load()
+    _here(x, q_out, scale_out)
+    R, C = x.shape
+    dt = _dt(x)
+    if q_out is None:
+        q_out = torch.empty((R, C), dtype=torch.float8_e4m3fn, device=x.device)
+    _like(q_out, (R, C), torch.float8_e4m3fn, "q_out")
+    if scale_out is None:
+        scale_out = torch.empty((R,), dtype=torch.float32, device=x.device)
+    _like(scale_out, (R,), torch.float32, "scale_out")
+    _check(L.mem_quantize_rows(_ptr(x), dt, R, C, _ptr(q_out), _ptr(scale_out), _stream(stream)))
+    return q_out, scale_out
+
+
+class _AdamwTensor(ctypes.Structure):  # pkmem_adamw_tensor
+    _fields_ = [(n, ctypes.c_void_p) for n in ("param", "grad", "exp_avg", "exp_avg_sq",
+                                               "exp_avg_scale", "exp_avg_sq_scale")]
+    _fields_ += [("numel", ctypes.c_int64)]
+    _fields_ += [(n, ctypes.c_int) for n in ("param_dt", "grad_dt", "state_dt")]
+
+
+class _AdamwOpts(ctypes.Structure):  # pkmem_adamw_opts
+    _fields_ = [(n, ctypes.c_double) for n in ("lr", "beta1", "beta2", "eps", "weight_decay")]
+    _fields_ += [("step", ctypes.c_int64), ("seed", ctypes.c_uint64)]
+    _fields_ += [(n, ctypes.c_void_p) for n in ("lr_dev", "step_dev", "grad_scale")]
+
+
+def mem_adamw_state(param: torch.Tensor, bits: int = 32):
+    """Zero states of mem_adamw for one parameter: (exp_avg, exp_avg_sq, exp_avg_scale,
+    exp_avg_sq_scale), fp32 with scales None, or with bits = 8 float8_e4m3fn (the second
+    one the square root) with an fp32 scale per 128 elements."""
+    if bits == 32:
+        return (*(torch.zeros(param.shape, dtype=torch.float32, device=param.device)
+                  for _ in range(2)), None, None)
+    if bits != 8:
+        raise ValueError("states have 32 or 8 bits")
+    codes = [torch.zeros(param.shape, dtype=torch.uint8, device=param.device).view(torch.float8_e4m3fn)
+             for _ in range(2)]
+    blocks = -(-param.numel() // ADAMW_STATE_BLOCK)
+    return (*codes, *(torch.zeros((blocks,), dtype=torch.float32, device=param.device)
+                      for _ in range(2)))
+
+
+_ADAMW_DT = {torch.float32: F32, torch.bfloat16: BF16, torch.float8_e4m3fn: E4M3}
+
+
+def _adamw_tensor(p, g, m, v, sm, sv, gshape) -> tuple:
+    n = p.numel()
+    if m.shape != p.shape or v.shape != p.shape or g.shape != gshape:
+        raise ValueError("states must have the parameter's shape, gradients their own")
+    if m.dtype != v.dtype or m.dtype not in (torch.float32, torch.float8_e4m3fn):
+        raise TypeError("states must both be float32 or both float8_e4m3fn")
+    if p.dtype not in (torch.float32, torch.bfloat16) or g.dtype not in (torch.float32, torch.bfloat16):
+        raise TypeError("parameters and gradients must be float32 or bfloat16")
+    if m.dtype == torch.float32:
+        if sm is not None or sv is not None:
+            raise ValueError("scales belong to float8_e4m3fn states")
+    else:
+        blocks = -(-n // ADAMW_STATE_BLOCK)
+        for s in (sm, sv):
+            if s is None or s.dtype != torch.float32 or s.numel() != blocks:
+                raise ValueError(f"float8_e4m3fn states need fp32 scales, one per {ADAMW_STATE_BLOCK} elements")
+    return (p.data_ptr(), g.data_ptr(), m.data_ptr(), v.data_ptr(), _ptr(sm), _ptr(sv), n,
+            _ADAMW_DT[p.dtype], _ADAMW_DT[g.dtype], _ADAMW_DT[m.dtype])
+
+
+def _adamw_opts(lr, betas, eps, weight_decay, step, seed, grad_scale) -> _AdamwOpts:
+    o = _AdamwOpts(beta1=betas[0], beta2=betas[1], eps=eps, weight_decay=weight_decay,
+                   seed=int(seed) & 0xFFFFFFFFFFFFFFFF)
+    if isinstance(lr, torch.Tensor):
+        _like(lr.reshape(-1), (1,), torch.float32, "lr")
+        _here(lr)
+        o.lr_dev = lr.data_ptr()
+    else:
+        o.lr = lr
+    if isinstance(step, torch.Tensor):
+        _like(step.reshape(-1), (1,), torch.int64, "step")
+        _here(step)
+        o.step_dev = step.data_ptr()
+    else:
+        o.step = int(step)
+    if grad_scale is not None:
+        _like(grad_scale.reshape(-1), (1,), torch.float32, "grad_scale")
+        _here(grad_scale)
+        o.grad_scale = grad_scale.data_ptr()
+    return o
+
+
+@_launches_on_stream
+def mem_adamw(params, grads, exp_avgs, exp_avg_sqs, *, lr, step, betas=(0.9, 0.999),
+              eps: float = 1e-8, weight_decay: float = 0.01, exp_avg_scales=None,
+              exp_avg_sq_scales=None, grad_scale=None, seed: int = 0, stream=None) -> None:
+    """One AdamW step on lists of tensors, in place (states: mem_adamw_state).
+
+    lr: a number or an fp32 device scalar; step: 1, 2, ... or an int64 device scalar;
+    grad_scale: an fp32 device scalar that multiplies the gradients (0 or not finite: the
+    step changes nothing).  exp_avg_scales, exp_avg_sq_scales: lists of the 8-bit states'
+    scales (None entries for 32-bit ones).  seed: of the rounding of bf16 parameters and
+    8-bit states; the step number is mixed in."""
+    L = load()
+    n = len(params)
+    none = [None] * n
+    sms = none if exp_avg_scales is None else exp_avg_scales
+    svs = none if exp_avg_sq_scales is None else exp_avg_sq_scales
+    if not len(grads) == len(exp_avgs) == len(exp_avg_sqs) == len(sms) == len(svs) == n:
+        raise ValueError("lists of different lengths")
+    ts = (_AdamwTensor * max(n, 1))()
+    for i, (p, g, m, v, sm, sv) in enumerate(zip(params, grads, exp_avgs, exp_avg_sqs, sms, svs)):
+        _here(p, g, m, v, sm, sv)
+        ts[i] = _adamw_tensor(p, g, m, v, sm, sv, p.shape)
+    o = _adamw_opts(lr, betas, eps, weight_decay, step, seed, grad_scale)
+    _check(L.mem_adamw(ctypes.addressof(ts), n, ctypes.addressof(o), _stream(stream)))
+
+
+@_launches_on_stream
+def mem_adamw_rows(param: torch.Tensor, rows: torch.Tensor, grad_rows: torch.Tensor,
+                   exp_avg: torch.Tensor, exp_avg_sq: torch.Tensor, *, lr, step,
+                   betas=(0.9, 0.999), eps: float = 1e-8, weight_decay: float = 0.01,
+                   exp_avg_scale=None, exp_avg_sq_scale=None, grad_scale=None, seed: int = 0,
+                   stream=None) -> None:
+    """One AdamW step, in place, on the rows of param [N, D] that rows (int64 [U],
+    ascending) names, with their gradients grad_rows fp32 [U, D]: what
+    mem_bag_backward_sparse returns.  The other rows keep value and states.  Arguments
+    as mem_adamw's."""
+    L = load()
+    _here(param, rows, grad_rows, exp_avg, exp_avg_sq, exp_avg_scale, exp_avg_sq_scale)
+    N, D = param.shape
+    U = rows.shape[0]
+    _like(rows, (U,), torch.int64, "rows")
+    _like(grad_rows, (U, D), torch.float32, "grad_rows")
+    t = _AdamwTensor(*_adamw_tensor(param, grad_rows, exp_avg, exp_avg_sq, exp_avg_scale,
+                                    exp_avg_sq_scale, (U, D)))
+    o = _adamw_opts(lr, betas, eps, weight_decay, step, seed, grad_scale)
+    _check(L.mem_adamw_rows(ctypes.addressof(t), N, D, _ptr(rows), U, ctypes.addressof(o),
+                            _stream(stream)))

@@ -695,3 +695,169 @@ int mem_bag_backward_sparse(const void* dy, const void* values, pkmem_dtype v_dt
 }
 
 }  // extern "C"
+
+// ---- norm and optimizer ------------------------------------------------------
+
+namespace {
+
+constexpr size_t NORM_ROW_BYTES = 32 << 10;  // a row fits the registers of one workgroup
+
+int check_rows_shape(const char* fn, pkmem_dtype dt, int64_t T, int D) {
+  if (!dtype_ok(dt)) return fail(PKMEM_ERR_INVALID, "%s: unknown dtype %d", fn, (int)dt);
+  if (T < 0) return fail(PKMEM_ERR_INVALID, "%s: the number of rows must be >= 0", fn);
+  if (T > 0x7FFFFFFF) return fail(PKMEM_ERR_UNSUPPORTED, "%s: 2^31 rows or more", fn);
+  if (D < 8 || D % 8 != 0)
+    return fail(PKMEM_ERR_UNSUPPORTED, "%s: rows must be a positive multiple of 8 wide (got %d)", fn, D);
+  if ((size_t)D * esize(dt) > NORM_ROW_BYTES)
+    return fail(PKMEM_ERR_UNSUPPORTED, "%s: rows wider than 32 KiB are not supported (%d)", fn, D);
+  return PKMEM_OK;
+}
+
+int check_adamw_opts(const char* fn, const pkmem_adamw_opts* o) {
+  if (!o) return fail(PKMEM_ERR_INVALID, "%s: null pointer", fn);
+  if (!(o->beta1 >= 0 && o->beta1 < 1 && o->beta2 >= 0 && o->beta2 < 1))
+    return fail(PKMEM_ERR_INVALID, "%s: betas must lie in [0, 1)", fn);
+  if (!(o->lr >= 0 && o->lr <= 3e38 && o->eps >= 0 && o->eps <= 3e38 && o->weight_decay >= 0 &&
+        o->weight_decay <= 3e38))
+    return fail(PKMEM_ERR_INVALID, "%s: lr, eps and weight_decay must be finite and >= 0", fn);
+  if (o->step < 1 && !o->step_dev) return fail(PKMEM_ERR_INVALID, "%s: step must be >= 1", fn);
+  if (!aligned(o->lr_dev, 4) || !aligned(o->step_dev, 8) || !aligned(o->grad_scale, 4))
+    return fail(PKMEM_ERR_INVALID, "%s: lr_dev, step_dev and grad_scale must be aligned to their size", fn);
+  return PKMEM_OK;
+}
+
+// graded: gradients are there (a list of touched rows may be empty).
+int check_adamw_tensor(const char* fn, const pkmem_adamw_tensor& t, int i, bool graded) {
+  if (!dtype_ok(t.param_dt) || !dtype_ok(t.grad_dt) ||
+      (t.state_dt != PKMEM_F32 && t.state_dt != PKMEM_E4M3))
+    return fail(PKMEM_ERR_INVALID, "%s: tensor %d: unsupported dtype", fn, i);
+  if (t.numel < 0) return fail(PKMEM_ERR_INVALID, "%s: tensor %d: numel must be >= 0", fn, i);
+  if (t.numel > (int64_t(1) << 40)) return fail(PKMEM_ERR_UNSUPPORTED, "%s: tensor %d: more than 2^40 elements", fn, i);
+  const bool s8 = t.state_dt == PKMEM_E4M3;
+  if (t.numel > 0 && (!t.param || (graded && !t.grad) || !t.exp_avg || !t.exp_avg_sq ||
+                      (s8 && (!t.exp_avg_scale || !t.exp_avg_sq_scale))))
+    return fail(PKMEM_ERR_INVALID, "%s: tensor %d: null pointer", fn, i);
+  const size_t se = s8 ? 1 : 4;
+  if (!aligned(t.param, esize(t.param_dt)) || !aligned(t.grad, esize(t.grad_dt)) ||
+      !aligned(t.exp_avg, se) || !aligned(t.exp_avg_sq, se) ||
+      (s8 && (!aligned(t.exp_avg_scale, 4) || !aligned(t.exp_avg_sq_scale, 4))))
+    return fail(PKMEM_ERR_INVALID, "%s: tensor %d: not aligned to its element size", fn, i);
+  return PKMEM_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+int mem_rmsnorm(const void* x, const void* res, const void* weight, pkmem_dtype dt, int64_t T,
+                int D, float eps, void* sum_out, void* y_out, pkmem_dtype y_dt, float* scale_out,
+                pkmem_stream_t stream) {
+  const char* fn = "mem_rmsnorm";
+  int rc = check_rows_shape(fn, dt, T, D);
+  if (rc) return rc;
+  if (y_dt != dt && y_dt != PKMEM_E4M3)
+    return fail(PKMEM_ERR_INVALID, "%s: y_dt must be the row dtype or PKMEM_E4M3", fn);
+  if (!(eps >= 0.f && eps <= 3.0e38f)) return fail(PKMEM_ERR_INVALID, "%s: eps must be finite and >= 0", fn);
+  const bool q = y_dt == PKMEM_E4M3;
+  if (T > 0 && (!x || !y_out || (q && !scale_out))) return fail(PKMEM_ERR_INVALID, "%s: null pointer", fn);
+  if (!q && scale_out) return fail(PKMEM_ERR_INVALID, "%s: scale_out is for PKMEM_E4M3 only", fn);
+  if (!aligned(x, 16) || !aligned(res, 16) || !aligned(weight, 16) || !aligned(sum_out, 16) ||
+      !aligned(y_out, 16) || !aligned(scale_out, 4))
+    return fail(PKMEM_ERR_INVALID, "%s: buffers must be 16-byte aligned (scale_out 4)", fn);
+  if (T == 0) return PKMEM_OK;
+  return hip_status(pk::launch_rmsnorm(dt == PKMEM_BF16, x, res, weight, T, D, eps, sum_out, y_out,
+                                       scale_out, reinterpret_cast<hipStream_t>(stream)), fn);
+}
+
+size_t mem_rmsnorm_backward_workspace_size(int64_t T, int D) {
+  if (T < 0 || D < 1) return 0;
+  return align256(pk::rmsnorm_backward_ws_bytes(T, D));
+}
+
+int mem_rmsnorm_backward(const void* dy, const void* h, const void* weight, pkmem_dtype dt,
+                         int64_t T, int D, float eps, const void* dsum, void* dx_out,
+                         float* grad_weight, void* ws, size_t ws_bytes, pkmem_stream_t stream) {
+  const char* fn = "mem_rmsnorm_backward";
+  int rc = check_rows_shape(fn, dt, T, D);
+  if (rc) return rc;
+  if (!(eps >= 0.f && eps <= 3.0e38f)) return fail(PKMEM_ERR_INVALID, "%s: eps must be finite and >= 0", fn);
+  if (T > 0 && (!dy || !h || !dx_out)) return fail(PKMEM_ERR_INVALID, "%s: null pointer", fn);
+  if (!aligned(dy, 16) || !aligned(h, 16) || !aligned(weight, 16) || !aligned(dsum, 16) ||
+      !aligned(dx_out, 16) || !aligned(grad_weight, 4))
+    return fail(PKMEM_ERR_INVALID, "%s: buffers must be 16-byte aligned (grad_weight 4)", fn);
+  if (grad_weight) {
+    const size_t need = mem_rmsnorm_backward_workspace_size(T, D);
+    if (need > 0 && (!ws || ws_bytes < need))
+      return fail(PKMEM_ERR_WORKSPACE, "%s: workspace of %zu bytes needed, %zu given", fn, need, ws ? ws_bytes : (size_t)0);
+    if (!aligned(ws, 256)) return fail(PKMEM_ERR_INVALID, "%s: workspace must be 256-byte aligned", fn);
+  }
+  if (T == 0) return PKMEM_OK;
+  return hip_status(pk::launch_rmsnorm_backward(dt == PKMEM_BF16, dy, h, weight, dsum, T, D, eps,
+                                                dx_out, grad_weight, reinterpret_cast<float*>(ws),
+                                                reinterpret_cast<hipStream_t>(stream)), fn);
+}
+
+int mem_quantize_rows(const void* x, pkmem_dtype dt, int64_t R, int C, void* q_out,
+                      float* scale_out, pkmem_stream_t stream) {
+  const char* fn = "mem_quantize_rows";
+  int rc = check_rows_shape(fn, dt, R, C);
+  if (rc) return rc;
+  if (R > 0 && (!x || !q_out || !scale_out)) return fail(PKMEM_ERR_INVALID, "%s: null pointer", fn);
+  if (!aligned(x, 16) || !aligned(q_out, 16) || !aligned(scale_out, 4))
+    return fail(PKMEM_ERR_INVALID, "%s: x and q_out must be 16-byte aligned (scale_out 4)", fn);
+  if (R == 0) return PKMEM_OK;
+  return hip_status(pk::launch_quantize_rows(dt == PKMEM_BF16, x, R, C, q_out, scale_out,
+                                             reinterpret_cast<hipStream_t>(stream)), fn);
+}
+
+int mem_adamw(const pkmem_adamw_tensor* tensors, int count, const pkmem_adamw_opts* opts,
+              pkmem_stream_t stream) {
+  const char* fn = "mem_adamw";
+  int rc = check_adamw_opts(fn, opts);
+  if (rc) return rc;
+  if (count < 0) return fail(PKMEM_ERR_INVALID, "%s: count must be >= 0", fn);
+  if (count > 0 && !tensors) return fail(PKMEM_ERR_INVALID, "%s: null pointer", fn);
+  for (int i = 0; i < count; ++i) {
+    rc = check_adamw_tensor(fn, tensors[i], i, true);
+    if (rc) return rc;
+  }
+  return hip_status(pk::launch_adamw(tensors, count, *opts, reinterpret_cast<hipStream_t>(stream)), fn);
+}
+
+int mem_adamw_rows(const pkmem_adamw_tensor* table, int64_t N, int D, const int64_t* rows,
+                   int64_t U, const pkmem_adamw_opts* opts, pkmem_stream_t stream) {
+  const char* fn = "mem_adamw_rows";
+  int rc = check_adamw_opts(fn, opts);
+  if (rc) return rc;
+  if (!table) return fail(PKMEM_ERR_INVALID, "%s: null pointer", fn);
+  rc = check_adamw_tensor(fn, *table, 0, U > 0);
+  if (rc) return rc;
+  if (N < 1) return fail(PKMEM_ERR_INVALID, "%s: N must be >= 1", fn);
+  if (D < 8 || D % 8 != 0) return fail(PKMEM_ERR_UNSUPPORTED, "%s: D must be a positive multiple of 8 (got %d)", fn, D);
+  if (N > (int64_t(1) << 40) / D || table->numel != N * D)
+    return fail(PKMEM_ERR_INVALID, "%s: numel must be N * D and at most 2^40", fn);
+  if (table->grad_dt != PKMEM_F32) return fail(PKMEM_ERR_UNSUPPORTED, "%s: gradients of rows are fp32", fn);
+  const bool s8 = table->state_dt == PKMEM_E4M3;
+  if (s8 && D % pk::ADAMW_STATE_BLOCK != 0)
+    return fail(PKMEM_ERR_UNSUPPORTED, "%s: 8-bit states need D a multiple of %d (got %d)", fn, pk::ADAMW_STATE_BLOCK, D);
+  if (!aligned(table->param, 16) || !aligned(table->grad, 16) || !aligned(table->exp_avg, 16) ||
+      !aligned(table->exp_avg_sq, 16))
+    return fail(PKMEM_ERR_INVALID, "%s: buffers must be 16-byte aligned", fn);
+  if (U < 0) return fail(PKMEM_ERR_INVALID, "%s: U must be >= 0", fn);
+  if (U > 0x7FFFFFFF || U * (int64_t)((D + 127) / 128) > (int64_t(1) << 35))
+    return fail(PKMEM_ERR_UNSUPPORTED, "%s: too many rows", fn);
+  if (U > 0 && !rows) return fail(PKMEM_ERR_INVALID, "%s: null pointer", fn);
+  if (!aligned(rows, 8)) return fail(PKMEM_ERR_INVALID, "%s: rows must be 8-byte aligned", fn);
+  if (U == 0) return PKMEM_OK;
+  hipStream_t st = reinterpret_cast<hipStream_t>(stream);
+  if (debug_checks()) {
+    uint32_t* flag = nullptr;
+    rc = debug_flag(fn, &flag);
+    if (rc) return rc;
+    rc = debug_outcome(fn, pk::launch_check_rows(rows, U, N, flag, st), flag, N, st);
+    if (rc) return rc;
+  }
+  return hip_status(pk::launch_adamw_rows(*table, N, D, rows, U, *opts, st), fn);
+}
+
+}  // extern "C"

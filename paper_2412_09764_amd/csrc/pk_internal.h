@@ -5,6 +5,8 @@
 #include <stddef.h>
 #include <stdint.h>
 
+#include "pkmem.h"
+
 namespace pk {
 
 // Scope guard for benchmark instrumentation: while a timer runs for `name`
@@ -130,5 +132,33 @@ hipError_t launch_bag_backward_sorted(bool bf16, const void* dy, const void* val
                                       int bag, float* grad_values, int64_t* rows_out,
                                       float* grad_rows_out, float* grad_w, void* ws, float* part,
                                       uint32_t** num_rows_dev, hipStream_t st);
+
+// ---- norm (norm.hip) -------------------------------------------------------
+// res, w, sum_out nullable; scale_out non-null: y in e4m3.
+hipError_t launch_rmsnorm(bool bf16, const void* x, const void* res, const void* w, int64_t rows,
+                          int D, float eps, void* sum_out, void* y_out, float* scale_out,
+                          hipStream_t st);
+hipError_t launch_quantize_rows(bool bf16, const void* x, int64_t rows, int D, void* q_out,
+                                float* scale_out, hipStream_t st);
+size_t rmsnorm_backward_ws_bytes(int64_t rows, int D);
+hipError_t launch_rmsnorm_backward(bool bf16, const void* dy, const void* h, const void* w,
+                                   const void* dsum, int64_t rows, int D, float eps, void* dx,
+                                   float* grad_weight, float* part, hipStream_t st);
+
+// ---- optimizer (adamw.hip) -------------------------------------------------
+constexpr int ADAMW_STATE_BLOCK = 128;  // elements that share the scales of 8-bit states
+// A step's scalars in the precision that the kernels use them in.
+struct AdamwScalars {
+  float beta1, rest1, beta2, rest2, eps, decay, rate, root2;
+  double corr1;
+  uint32_t key;
+};
+hipError_t launch_adamw(const pkmem_adamw_tensor* tensors, int count, const pkmem_adamw_opts& o,
+                        hipStream_t st);
+hipError_t launch_adamw_rows(const pkmem_adamw_tensor& t, int64_t N, int D, const int64_t* rows,
+                             int64_t U, const pkmem_adamw_opts& o, hipStream_t st);
+// *bad = 1 unless rows ascend (equal neighbours allowed) within [0, N).
+hipError_t launch_check_rows(const int64_t* rows, int64_t U, int64_t N, uint32_t* bad,
+                             hipStream_t st);
 
 }  // namespace pk
