@@ -409,6 +409,64 @@ int mem_quantize_rows(const void* x, pkmem_dtype dt, int64_t R, int C, void* q_o
                       float* scale_out, pkmem_stream_t stream);
 
 /* ------------------------------------------------------------------------ *
+ * A projection of the block: matrix product with its epilogue in one call,
+ *   z[t,:] = x[t,:] W^T (times x_scale[t] * w_scale[n]) + bias,
+ *   y[t,:] = act(z[t,:]) + res[t,:],
+ * sums and epilogue in fp32, one rounding to y_dt.
+ *
+ *   x  [T, K], w [N, K]  dtype dt: PKMEM_F32, PKMEM_BF16, or PKMEM_E4M3 with
+ *           x_scale [T] and w_scale [N] fp32 (mem_rmsnorm's and
+ *           mem_quantize_rows' scales; NULL for the other dtypes).
+ *   bias [N], res [T, N] dtype y_dt; NULL: none.
+ *   y_dt    PKMEM_F32 or PKMEM_BF16; dt = PKMEM_F32 needs PKMEM_F32.
+ *   act     pkmem_act.
+ *   z_out   [T, N] dtype y_dt: z (what mem_act_backward needs); NULL to skip it.
+ *   y_out   [T, N] dtype y_dt; may be res (in place), no other input.
+ *   N % 8 == 0; K % 8 == 0 (PKMEM_E4M3: K % 16 == 0); N, K <= 2^20; any T
+ *   below 2^31.  All buffers 16-byte aligned.
+ * Workspace: mem_linear_workspace_size(T, N, K, dt) bytes, 256-byte aligned
+ * (may be 0: ws may then be NULL).  T = 0 is a valid no-op.
+ * ------------------------------------------------------------------------ */
+typedef enum {
+  PKMEM_ACT_NONE = 0,
+  PKMEM_ACT_RELU = 1,
+  PKMEM_ACT_SILU = 2, /* z sigmoid(z) */
+  PKMEM_ACT_GELU = 3  /* z (1 + erf(z / sqrt 2)) / 2 */
+} pkmem_act;
+
+size_t mem_linear_workspace_size(int64_t T, int N, int K, pkmem_dtype dt);
+
+int mem_linear(const void* x, const void* w, pkmem_dtype dt, const float* x_scale,
+               const float* w_scale, const void* bias, const void* res, int64_t T, int N, int K,
+               int act, void* z_out, void* y_out, pkmem_dtype y_dt, void* ws, size_t ws_bytes,
+               pkmem_stream_t stream);
+
+/* Gradient of the activation, element-wise: dz_out = dy * act'(z) over [T, N]
+ * dtype dt (PKMEM_F32 or PKMEM_BF16), rounded once; pass it to
+ * mem_linear_backward.  N % 8 == 0; 16-byte aligned; dz_out may be dy or z. */
+int mem_act_backward(const void* dy, const void* z, pkmem_dtype dt, int act, int64_t T, int N,
+                     void* dz_out, pkmem_stream_t stream);
+
+/* ------------------------------------------------------------------------ *
+ * Backward of the product, from dz = dL/dz [T, N] dtype dt (F32 or BF16) with
+ * the forward's x [T, K] and w [N, K]:
+ *   dx_out    [T, K] dtype dt, written: dz W + dx_add, rounded once; dx_add
+ *             [T, K] dtype dt (another path's gradient of x) or NULL; dx_out
+ *             may be dx_add.
+ *   grad_w    [N, K] fp32, ACCUMULATED: += dz^T x.
+ *   grad_bias [N] fp32, ACCUMULATED: += sum_t dz.
+ * Each output may be NULL.  (The gradient of the forward's res is dy itself.)
+ * Bitwise deterministic: the tokens are split by their number alone and the
+ * parts added in order.  Limits as mem_linear's.  Workspace:
+ * mem_linear_backward_workspace_size(T, N, K, dt) bytes, 256-byte aligned.
+ * ------------------------------------------------------------------------ */
+size_t mem_linear_backward_workspace_size(int64_t T, int N, int K, pkmem_dtype dt);
+
+int mem_linear_backward(const void* dz, const void* x, const void* w, pkmem_dtype dt, int64_t T,
+                        int N, int K, const void* dx_add, void* dx_out, float* grad_w,
+                        float* grad_bias, void* ws, size_t ws_bytes, pkmem_stream_t stream);
+
+/* ------------------------------------------------------------------------ *
  * AdamW (decoupled weight decay) over many tensors in few launches.  With
  * g = grad * *grad_scale (1 where grad_scale is NULL), t = step:
  *   m = beta1 m + (1 - beta1) g;   v = beta2 v + (1 - beta2) g^2
@@ -484,7 +542,8 @@ int mem_adamw_rows(const pkmem_adamw_tensor* table, int64_t N, int D, const int6
  *   "gate_backward"                        (mem_gate_backward)
  *   "bag_backward_atomic", "sort_by_row",
  *   "bag_backward_rows", "softmax_backward" (mem_bag_backward[_sparse])
- *   "rmsnorm", "rmsnorm_backward", "quantize_rows", "adamw", "adamw_rows"
+ *   "rmsnorm", "rmsnorm_backward", "quantize_rows", "linear", "act_backward",
+ *   "linear_backward", "adamw", "adamw_rows"
  *                                          (the calls of these names)
  * ("sort_by_row" spans the whole radix sort and segment pass.)
  * mem_timer_stop() stops recording.  mem_timer_read(ms_out, kernel_out, cap)

@@ -30,10 +30,12 @@ __all__ = [
     "mem_bag_backward_sparse", "mem_search_workspace_size", "mem_bag_backward_workspace_size",
     "BWD_MODES", "F32", "BF16", "mem_timer_start", "mem_timer_stop", "mem_timer_read",
     "E4M3", "mem_rmsnorm", "mem_rmsnorm_backward", "mem_quantize_rows",
+    "mem_linear", "mem_act_backward", "mem_linear_backward", "ACTIVATIONS",
     "mem_adamw", "mem_adamw_rows", "mem_adamw_state", "ADAMW_STATE_BLOCK",
 ]
 
 F32, BF16, E4M3 = 0, 1, 2
+ACTIVATIONS = {"none": 0, "relu": 1, "silu": 2, "gelu": 3}
 ADAMW_STATE_BLOCK = 128  # elements that share the scales of 8-bit optimizer states
 NOALLOC_SCRATCH_BYTES = 128 << 20  # PKMEM_NOALLOC_SCRATCH_BYTES
 BWD_MODES = {"auto": 0, "atomic": 1, "sorted": 2}
@@ -110,6 +112,16 @@ def load() -> ctypes.CDLL:
     L.mem_rmsnorm_backward.restype = I32
     L.mem_quantize_rows.argtypes = [P, I32, I64, I32, P, P, P]
     L.mem_quantize_rows.restype = I32
+    L.mem_linear_workspace_size.argtypes = [I64, I32, I32, I32]
+    L.mem_linear_workspace_size.restype = SZ
+    L.mem_linear.argtypes = [P, P, I32, P, P, P, P, I64, I32, I32, I32, P, P, I32, P, SZ, P]
+    L.mem_linear.restype = I32
+    L.mem_act_backward.argtypes = [P, P, I32, I32, I64, I32, P, P]
+    L.mem_act_backward.restype = I32
+    L.mem_linear_backward_workspace_size.argtypes = [I64, I32, I32, I32]
+    L.mem_linear_backward_workspace_size.restype = SZ
+    L.mem_linear_backward.argtypes = [P, P, P, I32, I64, I32, I32, P, P, P, P, P, SZ, P]
+    L.mem_linear_backward.restype = I32
     L.mem_adamw.argtypes = [P, I32, P, P]
     L.mem_adamw.restype = I32
     L.mem_adamw_rows.argtypes = [P, I64, I32, P, I64, P, P]
@@ -671,6 +683,106 @@ def mem_quantize_rows(x: torch.Tensor, *, q_out=None, scale_out=None, stream=Non
     _like(scale_out, (R,), torch.float32, "scale_out")
     _check(L.mem_quantize_rows(_ptr(x), dt, R, C, _ptr(q_out), _ptr(scale_out), _stream(stream)))
     return q_out, scale_out
+
+
+def _act(act) -> int:
+    return ACTIVATIONS[act] if isinstance(act, str) else int(act)
+
+
+@_launches_on_stream
+def mem_linear(x: torch.Tensor, w: torch.Tensor, bias=None, *, residual=None, act="none",
+               x_scale=None, w_scale=None, out_dtype=None, y_out=None, z_out=None,
+               want_z: bool = False, workspace=None, stream=None):
+    """act(x w^T + bias) + residual: x [T, K], w [N, K], bias [N], residual [T, N].
+
+    act: a name of ACTIVATIONS.  float8_e4m3fn operands come with x_scale [T] and
+    w_scale [N] (mem_rmsnorm(quantize=True), mem_quantize_rows).  out_dtype: float32 or
+    bfloat16 (default: x's, bfloat16 for 8 bits), the dtype of bias and residual too.
+    Returns (y, z) with z = x w^T + bias before the activation, None unless want_z.
+    y_out may be residual."""
+    L = load()
+    _here(x, w, bias, residual, x_scale, w_scale, y_out, z_out, workspace)
+    T, K = x.shape
+    N = w.shape[0]
+    _like(w, (N, K), x.dtype, "w")
+    if x.dtype == torch.float8_e4m3fn:
+        dt = E4M3
+        if x_scale is None or w_scale is None:
+            raise ValueError("float8_e4m3fn operands need x_scale and w_scale")
+        _like(x_scale, (T,), torch.float32, "x_scale")
+        _like(w_scale, (N,), torch.float32, "w_scale")
+    else:
+        dt = _dt(x)
+    if out_dtype is None:
+        out_dtype = torch.bfloat16 if dt == E4M3 else x.dtype
+    if y_out is None:
+        y_out = torch.empty((T, N), dtype=out_dtype, device=x.device)
+    if z_out is None and want_z:
+        z_out = torch.empty((T, N), dtype=out_dtype, device=x.device)
+    ydt = _dt(y_out)
+    _like(y_out, (T, N), out_dtype, "y_out")
+    _like(z_out, (T, N), out_dtype, "z_out")
+    _like(bias, (N,), out_dtype, "bias")
+    _like(residual, (T, N), out_dtype, "residual")
+    nbytes = int(L.mem_linear_workspace_size(T, N, K, dt))
+    ws = _workspace(nbytes, x.device, workspace) if nbytes else None
+    _check(L.mem_linear(_ptr(x), _ptr(w), dt, _ptr(x_scale), _ptr(w_scale), _ptr(bias),
+                        _ptr(residual), T, N, K, _act(act), _ptr(z_out), _ptr(y_out), ydt, _ptr(ws),
+                        0 if ws is None else ws.numel() * ws.element_size(), _stream(stream)))
+    return y_out, z_out
+
+
+@_launches_on_stream
+def mem_act_backward(dy: torch.Tensor, z: torch.Tensor, act, *, dz_out=None, stream=None):
+    """dz = dy * act'(z), [T, N]: what mem_linear_backward takes after mem_linear with an
+    activation.  dz_out may be dy or z."""
+    L = load()
+    _here(dy, z, dz_out)
+    T, N = dy.shape
+    _like(z, (T, N), dy.dtype, "z")
+    if dz_out is None:
+        dz_out = torch.empty_like(dy)
+    _like(dz_out, (T, N), dy.dtype, "dz_out")
+    _check(L.mem_act_backward(_ptr(dy), _ptr(z), _dt(dy), _act(act), T, N, _ptr(dz_out),
+                              _stream(stream)))
+    return dz_out
+
+
+@_launches_on_stream
+def mem_linear_backward(dz: torch.Tensor, x: torch.Tensor, w: torch.Tensor, *, dx_add=None,
+                        dx=None, grad_w=None, grad_bias=None, want_dx: bool = True,
+                        want_grad_w: bool = True, want_grad_bias: bool = True, workspace=None,
+                        stream=None):
+    """Gradients of x w^T + bias from dz [T, N]: (dx = dz w + dx_add [T, K] in dz's dtype,
+    grad_w fp32 [N, K] and grad_bias fp32 [N], both ACCUMULATED; zeros are allocated if
+    none are given).  dx may be dx_add."""
+    L = load()
+    _here(dz, x, w, dx_add, dx, grad_w, grad_bias, workspace)
+    T, N = dz.shape
+    K = x.shape[1]
+    _like(x, (T, K), dz.dtype, "x")
+    _like(w, (N, K), dz.dtype, "w")
+    _like(dx_add, (T, K), dz.dtype, "dx_add")
+    dev = dz.device
+    if dx is None and want_dx:
+        dx = torch.empty((T, K), dtype=dz.dtype, device=dev)
+    if grad_w is None and want_grad_w:
+        grad_w = torch.zeros((N, K), dtype=torch.float32, device=dev)
+    if grad_bias is None and want_grad_bias:
+        grad_bias = torch.zeros((N,), dtype=torch.float32, device=dev)
+    _like(dx, (T, K), dz.dtype, "dx")
+    _like(grad_w, (N, K), torch.float32, "grad_w")
+    _like(grad_bias, (N,), torch.float32, "grad_bias")
+    dt = _dt(dz)
+    nbytes = 0
+    if grad_w is not None or grad_bias is not None:
+        nbytes = int(L.mem_linear_backward_workspace_size(T, N, K, dt))
+    ws = _workspace(nbytes, dev, workspace) if nbytes else None
+    _check(L.mem_linear_backward(_ptr(dz), _ptr(x), _ptr(w), dt, T, N, K, _ptr(dx_add), _ptr(dx),
+                                 _ptr(grad_w), _ptr(grad_bias), _ptr(ws),
+                                 0 if ws is None else ws.numel() * ws.element_size(),
+                                 _stream(stream)))
+    return dx, grad_w, grad_bias
 
 
 class _AdamwTensor(ctypes.Structure):  # pkmem_adamw_tensor

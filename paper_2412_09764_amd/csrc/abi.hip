@@ -861,3 +861,100 @@ int mem_adamw_rows(const pkmem_adamw_tensor* table, int64_t N, int D, const int6
 }
 
 }  // extern "C"
+
+// ---- projections -------------------------------------------------------------
+
+namespace {
+
+int check_linear_shapes(const char* fn, pkmem_dtype dt, bool e4m3, int64_t T, int N, int K) {
+  if (!dtype_ok(dt) && !(e4m3 && dt == PKMEM_E4M3)) return fail(PKMEM_ERR_INVALID, "%s: unknown dtype %d", fn, (int)dt);
+  if (T < 0) return fail(PKMEM_ERR_INVALID, "%s: T must be >= 0", fn);
+  if (T > 0x7FFFFFFF) return fail(PKMEM_ERR_UNSUPPORTED, "%s: T must be < 2^31", fn);
+  const int ka = dt == PKMEM_E4M3 ? 16 : 8;
+  if (N < 8 || N % 8 != 0) return fail(PKMEM_ERR_UNSUPPORTED, "%s: N must be a positive multiple of 8 (got %d)", fn, N);
+  if (K < ka || K % ka != 0) return fail(PKMEM_ERR_UNSUPPORTED, "%s: K must be a positive multiple of %d (got %d)", fn, ka, K);
+  if (N > (1 << 20) || K > (1 << 20)) return fail(PKMEM_ERR_UNSUPPORTED, "%s: N and K must be <= 2^20", fn);
+  // 128 x 128 tiles of the largest grid, and what split products add to it
+  if (((T + 127) / 128) * ((int64_t)(N > K ? N : K) / 128 + 1) > (int64_t(1) << 30))
+    return fail(PKMEM_ERR_UNSUPPORTED, "%s: too many tiles", fn);
+  return PKMEM_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t mem_linear_workspace_size(int64_t T, int N, int K, pkmem_dtype dt) {
+  if (T < 1 || N < 1 || K < 1) return 0;
+  return align256(pk::linear_ws_bytes(T, N, K, dt));
+}
+
+int mem_linear(const void* x, const void* w, pkmem_dtype dt, const float* x_scale,
+               const float* w_scale, const void* bias, const void* res, int64_t T, int N, int K,
+               int act, void* z_out, void* y_out, pkmem_dtype y_dt, void* ws, size_t ws_bytes,
+               pkmem_stream_t stream) {
+  const char* fn = "mem_linear";
+  int rc = check_linear_shapes(fn, dt, true, T, N, K);
+  if (rc) return rc;
+  if (!dtype_ok(y_dt) || (dt == PKMEM_F32 && y_dt != PKMEM_F32))
+    return fail(PKMEM_ERR_INVALID, "%s: y_dt must be PKMEM_F32 or PKMEM_BF16 (PKMEM_F32 for fp32 operands)", fn);
+  if (act < PKMEM_ACT_NONE || act > PKMEM_ACT_GELU) return fail(PKMEM_ERR_INVALID, "%s: unknown activation %d", fn, act);
+  if (dt != PKMEM_E4M3 && (x_scale || w_scale))
+    return fail(PKMEM_ERR_INVALID, "%s: scales belong to PKMEM_E4M3 operands", fn);
+  if (T > 0 && (!x || !w || !y_out || (dt == PKMEM_E4M3 && (!x_scale || !w_scale))))
+    return fail(PKMEM_ERR_INVALID, "%s: null pointer", fn);
+  if (!aligned(x, 16) || !aligned(w, 16) || !aligned(x_scale, 4) || !aligned(w_scale, 16) ||
+      !aligned(bias, 16) || !aligned(res, 16) || !aligned(z_out, 16) || !aligned(y_out, 16))
+    return fail(PKMEM_ERR_INVALID, "%s: buffers must be 16-byte aligned", fn);
+  const size_t need = mem_linear_workspace_size(T, N, K, dt);
+  if (need > 0 && (!ws || ws_bytes < need))
+    return fail(PKMEM_ERR_WORKSPACE, "%s: workspace of %zu bytes needed, %zu given", fn, need, ws ? ws_bytes : (size_t)0);
+  if (!aligned(ws, 256)) return fail(PKMEM_ERR_INVALID, "%s: workspace must be 256-byte aligned", fn);
+  if (T == 0) return PKMEM_OK;
+  const pk::LinearCall c{x, w, dt, x_scale, w_scale, bias, res, T, N, K, act, z_out, y_out, y_dt == PKMEM_BF16, ws};
+  return hip_status(pk::launch_linear(c, reinterpret_cast<hipStream_t>(stream)), fn);
+}
+
+int mem_act_backward(const void* dy, const void* z, pkmem_dtype dt, int act, int64_t T, int N,
+                     void* dz_out, pkmem_stream_t stream) {
+  const char* fn = "mem_act_backward";
+  if (!dtype_ok(dt)) return fail(PKMEM_ERR_INVALID, "%s: unknown dtype %d", fn, (int)dt);
+  if (act < PKMEM_ACT_NONE || act > PKMEM_ACT_GELU) return fail(PKMEM_ERR_INVALID, "%s: unknown activation %d", fn, act);
+  if (T < 0) return fail(PKMEM_ERR_INVALID, "%s: T must be >= 0", fn);
+  if (T > 0x7FFFFFFF) return fail(PKMEM_ERR_UNSUPPORTED, "%s: T must be < 2^31", fn);
+  if (N < 8 || N % 8 != 0) return fail(PKMEM_ERR_UNSUPPORTED, "%s: N must be a positive multiple of 8 (got %d)", fn, N);
+  if (T > 0 && (!dy || !z || !dz_out)) return fail(PKMEM_ERR_INVALID, "%s: null pointer", fn);
+  if (!aligned(dy, 16) || !aligned(z, 16) || !aligned(dz_out, 16))
+    return fail(PKMEM_ERR_INVALID, "%s: buffers must be 16-byte aligned", fn);
+  if (T == 0) return PKMEM_OK;
+  return hip_status(pk::launch_act_backward(dt == PKMEM_BF16, dy, z, act, T * N, dz_out,
+                                            reinterpret_cast<hipStream_t>(stream)), fn);
+}
+
+size_t mem_linear_backward_workspace_size(int64_t T, int N, int K, pkmem_dtype dt) {
+  (void)dt;
+  if (T < 1 || N < 1 || K < 1) return 0;
+  return align256(pk::linear_backward_ws_bytes(T, N, K));
+}
+
+int mem_linear_backward(const void* dz, const void* x, const void* w, pkmem_dtype dt, int64_t T,
+                        int N, int K, const void* dx_add, void* dx_out, float* grad_w,
+                        float* grad_bias, void* ws, size_t ws_bytes, pkmem_stream_t stream) {
+  const char* fn = "mem_linear_backward";
+  int rc = check_linear_shapes(fn, dt, false, T, N, K);
+  if (rc) return rc;
+  if (T > 0 && (!dz || (dx_out && !w) || (grad_w && !x))) return fail(PKMEM_ERR_INVALID, "%s: null pointer", fn);
+  if (!aligned(dz, 16) || !aligned(x, 16) || !aligned(w, 16) || !aligned(dx_add, 16) ||
+      !aligned(dx_out, 16) || !aligned(grad_w, 16) || !aligned(grad_bias, 4))
+    return fail(PKMEM_ERR_INVALID, "%s: buffers must be 16-byte aligned (grad_bias 4)", fn);
+  const size_t need = mem_linear_backward_workspace_size(T, N, K, dt);
+  if ((grad_w || grad_bias) && need > 0 && (!ws || ws_bytes < need))
+    return fail(PKMEM_ERR_WORKSPACE, "%s: workspace of %zu bytes needed, %zu given", fn, need, ws ? ws_bytes : (size_t)0);
+  if (!aligned(ws, 256)) return fail(PKMEM_ERR_INVALID, "%s: workspace must be 256-byte aligned", fn);
+  if (T == 0 || (!dx_out && !grad_w && !grad_bias)) return PKMEM_OK;
+  return hip_status(pk::launch_linear_backward(dt == PKMEM_BF16, dz, x, w, T, N, K, dx_add, dx_out,
+                                               grad_w, grad_bias, ws,
+                                               reinterpret_cast<hipStream_t>(stream)), fn);
+}
+
+}  // extern "C"

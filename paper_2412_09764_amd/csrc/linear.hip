@@ -1,0 +1,617 @@
+// Matrix products of the projections around the memory, with their epilogue:
+//   forward   y = act(x W^T * scales + bias) + residual,
+//   backward  dx = dz W + add,  grad_W += dz^T x,  grad_bias += sum_t dz.
+//
+// One kernel computes C[i, j] = sum_k A(i, k) B(j, k) for the three layouts: an
+// operand lies either with k consecutive (x, W of the forward; dz of dx) or with
+// its rows consecutive and k strided (W of dx; both of grad_W).  The latter is
+// read from LDS by transposing reads (bf16) or element by element (fp32), so
+// nothing is transposed in memory.
+//
+// Tiles of 256 x 256 by eight waves (128 x 64 each, 32x32 MFMA: per 32 bytes of
+// k a wave reads 6 fragments for 8 products, three quarters of what LDS gives in
+// that time) or, where these are too few for the chip, 128 x 128 by four.  A
+// stage holds 64 bytes of k; four stages are in LDS, filled by direct loads that
+// run three stages ahead, and the fragments of the next half stage are read
+// while the matrix cores work on the current one.
+#include "pk_internal.h"
+#include "pk_mfma.h"
+#include "pk_row.h"
+
+namespace pk {
+
+namespace {
+
+constexpr int STAGE_K = 64;  // bytes of k per stage
+constexpr int NSTAGE = 4;
+constexpr uint32_t OUTSIDE = 0x80000000u;  // past the end of every buffer resource
+
+typedef __attribute__((ext_vector_type(4))) short s16x4_t;
+
+enum { D_F32 = 0, D_BF16 = 1, D_E4M3 = 2 };
+constexpr int elem_size(int d) { return d == D_F32 ? 4 : d == D_BF16 ? 2 : 1; }
+
+// Waits until at most VM of this wave's vector loads are outstanding and none of
+// its LDS reads.
+template <int VM>
+__device__ __forceinline__ void wait_loads() {
+  __builtin_amdgcn_s_waitcnt((VM & 15) | ((VM >> 4) << 14) | (7 << 4));
+}
+// The same, then the workgroup's barrier; nothing moves across.
+template <int VM>
+__device__ __forceinline__ void wait_and_meet() {
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_sched_barrier(0);
+  wait_loads<VM>();
+  __builtin_amdgcn_s_barrier();
+  __builtin_amdgcn_sched_barrier(0);
+  asm volatile("" ::: "memory");
+}
+
+struct GemmArgs {
+  const void* a;  // rows i
+  const void* b;  // rows j
+  int64_t M;
+  int N;
+  int64_t K;
+  int64_t k_split;  // k of one split (a multiple of a stage's)
+  int tiles_m, tiles_n;
+  // epilogue
+  const float* a_scale;
+  const float* b_scale;
+  const void* bias;
+  const void* res;
+  void* z;
+  void* out;
+  float* part;  // [splits, M, N] when the product is split
+  int act;
+  int out_bf16;
+};
+
+template <int DT>
+__device__ __forceinline__ void mma(uint4 b, uint4 a, f32x16_t& c) {
+  if constexpr (DT == D_BF16) {
+    c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, b),
+                                                __builtin_bit_cast(bf16x8_t, a), c, 0, 0, 0);
+  } else {
+    c = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(b.x), __uint_as_float(a.x), c, 0, 0, 0);
+    c = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(b.y), __uint_as_float(a.y), c, 0, 0, 0);
+    c = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(b.z), __uint_as_float(a.z), c, 0, 0, 0);
+    c = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(b.w), __uint_as_float(a.w), c, 0, 0, 0);
+  }
+}
+// 8 e4m3 codes as bf16 (exact).  The 8-bit matrix instructions align the products
+// of each 8 k to the largest of them and keep 13 bits below it; a sum in fp32 takes
+// the bf16 instruction.  (Measured: beside a product of 2^16 one of 2^2 is lost.)
+__device__ __forceinline__ uint4 widen8(uint32_t lo, uint32_t hi) {
+  return uint4{__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.f, false)),
+               __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.f, true)),
+               __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 1.f, false)),
+               __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 1.f, true))};
+}
+
+// An operand's tile: R rows by one stage of k.
+//   KS = false: LDS [R][64 bytes of k]; 16-byte chunk c of row r lies at slot
+//     c ^ ((r >> 1) & 3), so eight rows' reads of one chunk cover all banks.
+//   KS = true: LDS [k][R elements]; the 64-byte (bf16) or 128-byte (fp32) units
+//     of a k row are permuted by k so that the k rows of one read instruction
+//     lie in different banks.
+template <int DT, bool KS, int R, int NWAVE>
+struct Operand {
+  static constexpr int E = elem_size(DT);
+  static constexpr int BYTES = R * STAGE_K;
+  static constexpr int ROW = KS ? R * E : STAGE_K;     // bytes of an LDS row
+  static constexpr int LOADS = BYTES / 1024 / NWAVE;   // direct loads per wave and stage
+  static constexpr int STAGE_ROWS = STAGE_K / E;       // k of a stage
+  static_assert(BYTES % (1024 * NWAVE) == 0, "whole loads");
+  static constexpr int UNITS = ROW / 64;
+
+  uint32_t off[LOADS];  // this lane's source offsets in a stage
+  uint32_t kb;          // KS = false: byte of k in a stage, the same for all loads up to a swizzle
+  uint32_t kbs[LOADS];
+  uint32_t rd[R / 32 < 8 ? R / 32 : 8];
+  const char* base;
+  int64_t left, step;   // bytes from base to the end; bytes from stage to stage
+  int64_t kleft;        // KS = false: bytes of k left in this split
+
+  // rows: first row of the tile, of `rows`; k range [k0, k1) of ld = K (or rows) elements
+  __device__ __forceinline__ void init(const void* p, int64_t row0, int64_t rows, int64_t K,
+                                       int64_t k0, int64_t k1, int wave, int lane) {
+    if constexpr (!KS) {
+      const int64_t ld = K * E;
+      base = (const char*)p + row0 * ld + k0 * E;
+      left = rows * ld - row0 * ld - k0 * E;
+      step = STAGE_K;
+      kleft = (k1 - k0) * E;
+#pragma unroll
+      for (int i = 0; i < LOADS; ++i) {
+        const int slot = (i * NWAVE + wave) * 64 + lane;
+        const int r = slot >> 2, c = (slot & 3) ^ ((r >> 1) & 3);
+        off[i] = row0 + r < rows ? (uint32_t)(r * ld + c * 16) : OUTSIDE;
+        kbs[i] = c * 16;
+      }
+    } else {
+      const int64_t ld = rows * E;
+      base = (const char*)p + k0 * ld + row0 * E;
+      left = k1 * ld - k0 * ld - row0 * E;
+      step = (int64_t)STAGE_ROWS * ld;
+#pragma unroll
+      for (int i = 0; i < LOADS; ++i) {
+        const int slot = (i * NWAVE + wave) * 64 + lane;
+        const int k = slot / (ROW / 16);
+        int c = slot % (ROW / 16);
+        if constexpr (DT == D_F32) c ^= ((k >> 2) & 1) << 3;
+        else c ^= (((k & 3) | ((k >> 1) & 4)) & (UNITS - 1)) << 2;
+        off[i] = row0 + c * (16 / E) < rows ? (uint32_t)(k * ld + c * 16) : OUTSIDE;
+      }
+    }
+  }
+  // The next stage into lds (this wave's loads of it); advances.
+  __device__ __forceinline__ void load(unsigned char* lds, int wave) {
+    const int64_t n = left > 0x7FFFFFFF ? 0x7FFFFFFF : left > 0 ? left : 0;
+    const __amdgpu_buffer_rsrc_t r = raw_buffer(base, (uint32_t)n);
+#pragma unroll
+    for (int i = 0; i < LOADS; ++i) {
+      uint32_t o = off[i];
+      if constexpr (!KS) o = (int64_t)kbs[i] < kleft ? o : OUTSIDE;
+      lds_dma16_buf(r, o, 0u, lds + (i * NWAVE + wave) * 1024);
+    }
+    base += step;
+    left -= step;
+    if constexpr (!KS) kleft -= STAGE_K;
+  }
+  // Read addresses of this lane for blocks of 32 rows from row r0 on.
+  template <int NB>
+  __device__ __forceinline__ void init_read(int r0, int lane) {
+    if constexpr (!KS) {
+      const int r = r0 + (lane & 31);
+      rd[0] = r * STAGE_K + (((lane >> 5) ^ ((r >> 1) & 3)) << 4);
+    } else if constexpr (DT == D_F32) {
+      const int kh = lane >> 5;
+#pragma unroll
+      for (int b = 0; b < NB; ++b) rd[b] = 4 * kh * ROW + (((r0 / 32 + b) ^ kh) * 128) + (lane & 31) * 4;
+    } else {
+      const int g = lane >> 4, i = lane & 15;
+      const int f = ((i >> 2) | ((g >> 1) << 2)) & (UNITS - 1);
+#pragma unroll
+      for (int b = 0; b < NB; ++b)
+        rd[b] = (8 * (g >> 1) + (i >> 2)) * ROW + (((r0 / 32 + b) ^ f) * 64) + 32 * (g & 1) + 8 * (i & 3);
+    }
+  }
+  // Fragment of block b, half h of the stage (32 bytes of k).
+  __device__ __forceinline__ uint4 frag(const unsigned char* lds, int b, int h) const {
+    if constexpr (!KS) {
+      return *reinterpret_cast<const uint4*>(lds + ((rd[0] ^ (h << 5)) + b * 32 * STAGE_K));
+    } else if constexpr (DT == D_F32) {
+      const unsigned char* p = lds + rd[b] + h * 8 * ROW;
+      return uint4{*reinterpret_cast<const uint32_t*>(p), *reinterpret_cast<const uint32_t*>(p + ROW),
+                   *reinterpret_cast<const uint32_t*>(p + 2 * ROW),
+                   *reinterpret_cast<const uint32_t*>(p + 3 * ROW)};
+    } else {
+      const unsigned char* p = lds + rd[b] + h * 16 * ROW;
+      typedef __attribute__((address_space(3))) s16x4_t* lp;
+      const s16x4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lp)(unsigned char*)p);
+      const s16x4_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lp)(unsigned char*)(p + 4 * ROW));
+      const uint2 l = __builtin_bit_cast(uint2, lo), u = __builtin_bit_cast(uint2, hi);
+      return uint4{l.x, l.y, u.x, u.y};
+    }
+  }
+};
+
+// ---- activations -------------------------------------------------------------
+// FAST: for values that are rounded to bf16 afterwards.
+template <bool FAST>
+__device__ __forceinline__ float sigmoid_of(float z) {
+  if constexpr (FAST) return __builtin_amdgcn_rcpf(1.f + __expf(-z));
+  return 1.f / (1.f + expf(-z));
+}
+__device__ __forceinline__ float erf_of(float x) { return erff(x); }
+template <bool FAST>
+__device__ __forceinline__ float act_of(float z, int act) {
+  switch (act) {
+    case PKMEM_ACT_RELU: return z > 0.f ? z : (z != z ? z : 0.f);
+    case PKMEM_ACT_SILU: return FAST ? z * sigmoid_of<true>(z) : z / (1.f + expf(-z));
+    case PKMEM_ACT_GELU: return 0.5f * z * (1.f + erf_of(z * 0.70710678118654752f));
+    default: return z;
+  }
+}
+template <bool FAST>
+__device__ __forceinline__ float act_grad_of(float z, int act) {
+  switch (act) {
+    case PKMEM_ACT_RELU: return z > 0.f ? 1.f : (z != z ? z : 0.f);
+    case PKMEM_ACT_SILU: {
+      const float s = sigmoid_of<FAST>(z);
+      return s * (1.f + z * (1.f - s));
+    }
+    case PKMEM_ACT_GELU:
+      return 0.5f * (1.f + erf_of(z * 0.70710678118654752f)) + z * expf(-0.5f * z * z) * 0.39894228040143268f;
+    default: return 1.f;
+  }
+}
+
+__device__ __forceinline__ void load4(const void* p, size_t at, bool bf16, float (&v)[4]) {
+  if (bf16) {
+    const uint2 u = *reinterpret_cast<const uint2*>((const uint16_t*)p + at);
+    v[0] = bf16_lo(u.x); v[1] = bf16_hi(u.x); v[2] = bf16_lo(u.y); v[3] = bf16_hi(u.y);
+  } else {
+    const float4 f = *reinterpret_cast<const float4*>((const float*)p + at);
+    v[0] = f.x; v[1] = f.y; v[2] = f.z; v[3] = f.w;
+  }
+}
+__device__ __forceinline__ void store4(void* p, size_t at, bool bf16, const float (&v)[4]) {
+  if (bf16) *reinterpret_cast<uint2*>((uint16_t*)p + at) = uint2{to_bf16x2(v[0], v[1]), to_bf16x2(v[2], v[3])};
+  else *reinterpret_cast<float4*>((float*)p + at) = float4{v[0], v[1], v[2], v[3]};
+}
+
+// Four consecutive outputs (i, j .. j + 3) of the product: scales, bias,
+// activation and residual in fp32, one rounding.
+__device__ __forceinline__ void epilogue4(const GemmArgs& g, int64_t i, int j, float sa, float (&v)[4]) {
+  const bool h = g.out_bf16;
+  const size_t at = (size_t)i * g.N + j;
+  if (g.b_scale) {
+    const float4 s = *reinterpret_cast<const float4*>(g.b_scale + j);
+    v[0] *= sa * s.x; v[1] *= sa * s.y; v[2] *= sa * s.z; v[3] *= sa * s.w;
+  }
+  if (g.bias) {
+    float b[4];
+    load4(g.bias, j, h, b);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] += b[e];
+  }
+  if (g.z) store4(g.z, at, h, v);
+  if (g.act) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] = h ? act_of<true>(v[e], g.act) : act_of<false>(v[e], g.act);
+  }
+  if (g.res) {
+    float r[4];
+    load4(g.res, at, h, r);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] += r[e];
+  }
+  store4(g.out, at, h, v);
+}
+
+// GRAD: C is added to fp32 `out`, or written to `part` when split; else the
+// epilogue above.
+template <int DT, bool AKS, bool BKS, bool GRAD, int BM, int BN, int WM, int WN>
+__global__ __launch_bounds__(WM* WN * 64) void k_gemm(const GemmArgs g) {
+  constexpr int NW = WM * WN, MI = BM / WM / 32, NJ = BN / WN / 32;
+  using OA = Operand<DT, AKS, BM, NW>;
+  using OB = Operand<DT, BKS, BN, NW>;
+  constexpr int L = OA::LOADS + OB::LOADS;
+  constexpr int BYTES = OA::BYTES + OB::BYTES;
+  // a variable for each stage: the compiler then knows which loads a read of
+  // LDS depends on, and waits for no other
+  __shared__ __align__(1024) unsigned char st0[BYTES], st1[BYTES], st2[BYTES], st3[BYTES];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+
+  // XCD x (workgroup number mod 8) takes a contiguous run of tiles; within it
+  // four rows of tiles at a time, so that what one XCD's L2 holds is shared.
+  const int tiles = g.tiles_m * g.tiles_n, nwg = gridDim.x;
+  const int x = blockIdx.x & 7, q = nwg >> 3, rem = nwg & 7;
+  int pid = x * q + (x < rem ? x : rem) + (blockIdx.x >> 3);
+  const int split = pid / tiles;
+  pid -= split * tiles;
+  const int group = pid / (4 * g.tiles_n);
+  const int m_first = group * 4;
+  const int m_count = g.tiles_m - m_first < 4 ? g.tiles_m - m_first : 4;
+  pid -= group * 4 * g.tiles_n;
+  const int64_t i0 = (int64_t)(m_first + pid % m_count) * BM;
+  const int j0 = (pid / m_count) * BN;
+  const int64_t k0 = split * g.k_split;
+  const int64_t k1 = k0 + g.k_split < g.K ? k0 + g.k_split : g.K;
+
+  OA oa;
+  OB ob;
+  oa.init(g.a, i0, g.M, g.K, k0, k1, wave, lane);
+  ob.init(g.b, j0, g.N, g.K, k0, k1, wave, lane);
+  const int wi = (wave / WN) * (BM / WM), wj = (wave % WN) * (BN / WN);
+  oa.template init_read<MI>(wi, lane);
+  ob.template init_read<NJ>(wj, lane);
+
+  const int steps = (int)((k1 - k0 + OA::STAGE_ROWS - 1) / OA::STAGE_ROWS);
+  f32x16_t acc[MI][NJ];
+#pragma unroll
+  for (int mi = 0; mi < MI; ++mi)
+#pragma unroll
+    for (int nj = 0; nj < NJ; ++nj) acc[mi][nj] = f32x16_t{};
+
+  auto fill = [&](unsigned char* st) PK_INLINE {
+    oa.load(st, wave);
+    ob.load(st + OA::BYTES, wave);
+  };
+  fill(st0);
+  fill(st1);
+  fill(st2);
+  fill(st3);
+  wait_and_meet<3 * L>();
+  // Fragments of the halves 0 and 1 of a stage.
+  uint4 fa[2][MI], fb[2][NJ];
+  auto read = [&](const unsigned char* st, int h) PK_INLINE {
+#pragma unroll
+    for (int nj = 0; nj < NJ; ++nj) fb[h][nj] = ob.frag(st + OA::BYTES, nj, h);
+#pragma unroll
+    for (int mi = 0; mi < MI; ++mi) fa[h][mi] = oa.frag(st, mi, h);
+  };
+  auto products = [&](int h) PK_INLINE {
+    if constexpr (DT == D_E4M3) {
+#pragma unroll
+      for (int part = 0; part < 2; ++part) {
+        uint4 b[NJ];
+#pragma unroll
+        for (int nj = 0; nj < NJ; ++nj)
+          b[nj] = part ? widen8(fb[h][nj].z, fb[h][nj].w) : widen8(fb[h][nj].x, fb[h][nj].y);
+#pragma unroll
+        for (int mi = 0; mi < MI; ++mi) {
+          const uint4 a = part ? widen8(fa[h][mi].z, fa[h][mi].w) : widen8(fa[h][mi].x, fa[h][mi].y);
+#pragma unroll
+          for (int nj = 0; nj < NJ; ++nj) mma<D_BF16>(b[nj], a, acc[mi][nj]);
+        }
+      }
+    } else {
+#pragma unroll
+      for (int mi = 0; mi < MI; ++mi)
+#pragma unroll
+        for (int nj = 0; nj < NJ; ++nj) mma<DT>(fb[h][nj], fa[h][mi], acc[mi][nj]);
+    }
+  };
+  // One stage: st is visible to all, half 0 of it in registers.  After the
+  // barrier every wave has read st, and next has landed for all.
+  auto stage = [&](unsigned char* st, const unsigned char* next) PK_INLINE {
+    read(st, 1);
+    products(0);
+    wait_and_meet<2 * L>();
+    fill(st);
+    read(next, 0);
+    products(1);
+  };
+  read(st0, 0);
+  int s = 0;
+  for (; s + 4 <= steps; s += 4) {
+    stage(st0, st1);
+    stage(st1, st2);
+    stage(st2, st3);
+    stage(st3, st0);
+  }
+  if (s < steps) stage(st0, st1);
+  if (s + 1 < steps) stage(st1, st2);
+  if (s + 2 < steps) stage(st2, st3);
+  wait_loads<0>();  // no load may reach LDS after the workgroup has left it
+
+  const int il = lane & 31, kh = lane >> 5;
+#pragma unroll
+  for (int mi = 0; mi < MI; ++mi) {
+    const int64_t i = i0 + wi + mi * 32 + il;
+    if (i >= g.M) continue;
+    const float sa = !GRAD && g.a_scale ? g.a_scale[i] : 1.f;
+#pragma unroll
+    for (int nj = 0; nj < NJ; ++nj) {
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const int j = j0 + wj + nj * 32 + 8 * r + 4 * kh;
+        if (j >= g.N) continue;
+        float v[4] = {acc[mi][nj][4 * r], acc[mi][nj][4 * r + 1], acc[mi][nj][4 * r + 2], acc[mi][nj][4 * r + 3]};
+        if constexpr (GRAD) {
+          const size_t at = (size_t)i * g.N + j;
+          if (g.part) {
+            store4(g.part, (size_t)split * g.M * g.N + at, false, v);
+          } else {
+            float o[4];
+            load4(g.out, at, false, o);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[e] += o[e];
+            store4(g.out, at, false, v);
+          }
+        } else {
+          epilogue4(g, i, j, sa, v);
+        }
+      }
+    }
+  }
+}
+
+// out += part[0] + part[1] + ... in this order, 4 elements a thread.
+__global__ __launch_bounds__(256) void k_add_parts(const float* __restrict__ part, int splits,
+                                                   size_t n, float* __restrict__ out) {
+  const size_t at = ((size_t)blockIdx.x * 256 + threadIdx.x) * 4;
+  if (at >= n) return;
+  float s[4] = {0.f, 0.f, 0.f, 0.f};
+  for (int p = 0; p < splits; ++p) {
+    float v[4];
+    load4(part, p * n + at, false, v);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) s[e] += v[e];
+  }
+  float o[4];
+  load4(out, at, false, o);
+#pragma unroll
+  for (int e = 0; e < 4; ++e) o[e] += s[e];
+  store4(out, at, false, o);
+}
+
+// Sums over rows: part[b, c] for the rows of workgroup b (a fixed stride
+// apart), 8 columns a thread; the parts are added by launch_add_rows.
+template <typename T>
+__global__ __launch_bounds__(256) void k_column_sums(const T* __restrict__ x, int64_t rows, int N,
+                                                     float* __restrict__ part) {
+  constexpr int C = Chunk<T>::N;
+  const int chunks = N / C;
+  for (int c = blockIdx.y * 256 + threadIdx.x; c < chunks; c += gridDim.y * 256) {
+    float s[C];
+#pragma unroll
+    for (int e = 0; e < C; ++e) s[e] = 0.f;
+#pragma unroll 4
+    for (int64_t r = blockIdx.x; r < rows; r += gridDim.x) {
+      float v[C];
+      Chunk<T>::unpack(ld16(x + (size_t)r * N + (size_t)c * C), v);
+#pragma unroll
+      for (int e = 0; e < C; ++e) s[e] += v[e];
+    }
+#pragma unroll
+    for (int e = 0; e < C; ++e) part[(size_t)blockIdx.x * N + (size_t)c * C + e] = s[e];
+  }
+}
+
+// dz = dy act'(z), 16 bytes a thread.
+template <typename T, bool FAST>
+__global__ __launch_bounds__(256) void k_act_bwd(const T* dy, const T* z, int act, int64_t chunks, T* dz) {
+  using Ch = Chunk<T>;
+  for (int64_t c = (int64_t)blockIdx.x * 256 + threadIdx.x; c < chunks; c += (int64_t)gridDim.x * 256) {
+    float d[Ch::N], v[Ch::N];
+    Ch::unpack(ld16_nt(dy + c * Ch::N), d);
+    Ch::unpack(ld16_nt(z + c * Ch::N), v);
+#pragma unroll
+    for (int e = 0; e < Ch::N; ++e) d[e] *= act_grad_of<FAST>(v[e], act);
+    *reinterpret_cast<uint4*>(dz + c * Ch::N) = Ch::pack(d);
+  }
+}
+
+inline int ceil_div(int64_t a, int64_t b) { return (int)((a + b - 1) / b); }
+
+constexpr int64_t BIG_TILES = 200;  // 256 x 256 tiles from which on they fill the chip
+
+template <int DT, bool AKS, bool BKS, bool GRAD>
+void gemm_launch(GemmArgs g, bool big, int splits, hipStream_t st) {
+  const int t = big ? 256 : 128;
+  g.tiles_m = ceil_div(g.M, t);
+  g.tiles_n = ceil_div(g.N, t);
+  const dim3 grid((unsigned)(g.tiles_m * g.tiles_n * splits));
+  if (big)
+    hipLaunchKernelGGL((k_gemm<DT, AKS, BKS, GRAD, 256, 256, 2, 4>), grid, dim3(512), 0, st, g);
+  else
+    hipLaunchKernelGGL((k_gemm<DT, AKS, BKS, GRAD, 128, 128, 2, 2>), grid, dim3(256), 0, st, g);
+}
+
+bool big_tiles(int64_t M, int64_t N) { return (int64_t)ceil_div(M, 256) * ceil_div(N, 256) >= BIG_TILES; }
+
+// grad_W [N, K] from T tokens: tiles of its own shape, the tokens split so that
+// the workgroups fill the chip; at least 512 tokens a split.
+struct GradPlan {
+  bool big;
+  int splits;
+  int64_t k_split;
+};
+GradPlan grad_plan(int64_t T, int N, int K) {
+  GradPlan p;
+  const int64_t b = (int64_t)ceil_div(N, 256) * ceil_div(K, 256);
+  p.big = b >= 16 && T >= 4096;
+  const int64_t tiles = p.big ? b : (int64_t)ceil_div(N, 128) * ceil_div(K, 128);
+  int64_t s = (p.big ? 256 : 512) / tiles;
+  const int64_t most = T / 512;
+  if (s > most) s = most;
+  if (s < 1) s = 1;
+  if (s > 64) s = 64;
+  p.k_split = ((T + s - 1) / s + 63) / 64 * 64;
+  p.splits = T > 0 ? ceil_div(T, p.k_split) : 1;
+  return p;
+}
+// Workgroups along the tokens of the bias gradient.
+int bias_parts(int64_t T) { return (int)(T < 512 ? T : 512); }
+
+inline size_t up256(size_t x) { return (x + 255) & ~size_t(255); }
+
+}  // namespace
+
+hipError_t launch_linear(const LinearCall& c, hipStream_t st) {
+  if (c.T <= 0) return hipSuccess;
+  LaunchTimer lt("linear", st);
+  GemmArgs g{};
+  g.a = c.x;
+  g.b = c.w;
+  g.M = c.T;
+  g.N = c.N;
+  g.K = g.k_split = c.K;
+  g.a_scale = c.x_scale;
+  g.b_scale = c.w_scale;
+  g.bias = c.bias;
+  g.res = c.res;
+  g.z = c.z;
+  g.out = c.y;
+  g.act = c.act;
+  g.out_bf16 = c.out_bf16;
+  const bool big = big_tiles(c.T, c.N);
+  if (c.dt == PKMEM_BF16) gemm_launch<D_BF16, false, false, false>(g, big, 1, st);
+  else if (c.dt == PKMEM_E4M3) gemm_launch<D_E4M3, false, false, false>(g, big, 1, st);
+  else gemm_launch<D_F32, false, false, false>(g, big, 1, st);
+  return hipGetLastError();
+}
+
+size_t linear_ws_bytes(int64_t T, int N, int K, pkmem_dtype dt) {
+  (void)T; (void)N; (void)K; (void)dt;
+  return 0;
+}
+
+hipError_t launch_act_backward(bool bf16, const void* dy, const void* z, int act, int64_t n, void* dz,
+                               hipStream_t st) {
+  if (n <= 0) return hipSuccess;
+  LaunchTimer lt("act_backward", st);
+  const int64_t chunks = n / (bf16 ? 8 : 4);
+  int64_t blocks = (chunks + 255) / 256;
+  if (blocks > 16384) blocks = 16384;
+  if (bf16)
+    hipLaunchKernelGGL((k_act_bwd<uint16_t, true>), dim3((unsigned)blocks), dim3(256), 0, st,
+                       (const uint16_t*)dy, (const uint16_t*)z, act, chunks, (uint16_t*)dz);
+  else
+    hipLaunchKernelGGL((k_act_bwd<float, false>), dim3((unsigned)blocks), dim3(256), 0, st,
+                       (const float*)dy, (const float*)z, act, chunks, (float*)dz);
+  return hipGetLastError();
+}
+
+size_t linear_backward_ws_bytes(int64_t T, int N, int K) {
+  const GradPlan p = grad_plan(T, N, K);
+  return (p.splits > 1 ? up256((size_t)p.splits * N * K * sizeof(float)) : 0) +
+         up256((size_t)bias_parts(T) * N * sizeof(float));
+}
+
+hipError_t launch_linear_backward(bool bf16, const void* dz, const void* x, const void* w, int64_t T,
+                                  int N, int K, const void* add, void* dx, float* grad_w,
+                                  float* grad_bias, void* ws, hipStream_t st) {
+  if (T <= 0) return hipSuccess;
+  LaunchTimer lt("linear_backward", st);
+  if (dx) {
+    GemmArgs g{};
+    g.a = dz;
+    g.b = w;
+    g.M = T;
+    g.N = K;
+    g.K = g.k_split = N;
+    g.res = add;
+    g.out = dx;
+    g.out_bf16 = bf16;
+    const bool big = big_tiles(T, K);
+    if (bf16) gemm_launch<D_BF16, false, true, false>(g, big, 1, st);
+    else gemm_launch<D_F32, false, true, false>(g, big, 1, st);
+  }
+  char* p = (char*)ws;
+  const GradPlan plan = grad_plan(T, N, K);
+  if (grad_w) {
+    GemmArgs g{};
+    g.a = dz;
+    g.b = x;
+    g.M = N;
+    g.N = K;
+    g.K = T;
+    g.k_split = plan.k_split;
+    g.out = grad_w;
+    g.part = plan.splits > 1 ? (float*)p : nullptr;
+    if (bf16) gemm_launch<D_BF16, true, true, true>(g, plan.big, plan.splits, st);
+    else gemm_launch<D_F32, true, true, true>(g, plan.big, plan.splits, st);
+    if (plan.splits > 1) {
+      const size_t n = (size_t)N * K;
+      hipLaunchKernelGGL(k_add_parts, dim3((unsigned)((n / 4 + 255) / 256)), dim3(256), 0, st, g.part,
+                         plan.splits, n, grad_w);
+    }
+  }
+  if (grad_bias) {
+    if (plan.splits > 1) p += up256((size_t)plan.splits * N * K * sizeof(float));
+    const int parts = bias_parts(T), cols = ceil_div(N / (bf16 ? 8 : 4), 256);
+    const dim3 grid((unsigned)parts, (unsigned)(cols < 64 ? cols : 64));
+    if (bf16) hipLaunchKernelGGL(k_column_sums<uint16_t>, grid, dim3(256), 0, st, (const uint16_t*)dz, T, N, (float*)p);
+    else hipLaunchKernelGGL(k_column_sums<float>, grid, dim3(256), 0, st, (const float*)dz, T, N, (float*)p);
+    launch_add_rows((const float*)p, parts, N, grad_bias, st);
+  }
+  return hipGetLastError();
+}
+
+}  // namespace pk

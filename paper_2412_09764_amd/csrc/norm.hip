@@ -133,7 +133,7 @@ __global__ __launch_bounds__(BLOCK) void k_rmsnorm(const T* x, const T* res,
 //   dx = rstd (g - xh mean(g xh)) + dsum,   grad_weight += sum over rows of dy xh.
 // A row group (wave or workgroup) walks rows a fixed stride apart and keeps
 // its part of grad_weight in registers; the waves of a workgroup add theirs
-// in wave order, and k_norm_reduce adds the workgroups' parts in a fixed
+// in wave order, and k_add_rows adds the workgroups' parts in a fixed
 // order: the same bits on every run.
 template <typename T, int NCH, int WPR>
 __global__ __launch_bounds__(BLOCK) void k_rmsnorm_bwd(const T* dy, const T* h_in,
@@ -237,7 +237,7 @@ __global__ __launch_bounds__(BLOCK) void k_rmsnorm_bwd(const T* dy, const T* h_i
 
 // grad[c] += sum over the parts of part[p, c]: 32 columns per workgroup, eight
 // groups of parts added in group order.
-__global__ __launch_bounds__(BLOCK) void k_norm_reduce(const float* __restrict__ part, int parts,
+__global__ __launch_bounds__(BLOCK) void k_add_rows(const float* __restrict__ part, int parts,
                                                        int D, float* __restrict__ grad) {
   __shared__ float red[8][32];
   const int c = threadIdx.x & 31, g = threadIdx.x >> 5;
@@ -300,6 +300,11 @@ void norm_bwd_launch(const void* dy, const void* h, const void* w, const void* d
 
 }  // namespace
 
+void launch_add_rows(const float* part, int parts, int cols, float* out, hipStream_t st) {
+  hipLaunchKernelGGL(k_add_rows, dim3((unsigned)((cols + 31) / 32)), dim3(BLOCK), 0, st, part, parts,
+                     cols, out);
+}
+
 hipError_t launch_rmsnorm(bool bf16, const void* x, const void* res, const void* w, int64_t rows,
                           int D, float eps, void* sum_out, void* y_out, float* scale_out,
                           hipStream_t st) {
@@ -335,9 +340,7 @@ hipError_t launch_rmsnorm_backward(bool bf16, const void* dy, const void* h, con
   LaunchTimer lt("rmsnorm_backward", st);
   if (bf16) norm_bwd_launch<uint16_t>(dy, h, w, dsum, rows, D, eps, dx, grad_weight ? part : nullptr, st);
   else norm_bwd_launch<float>(dy, h, w, dsum, rows, D, eps, dx, grad_weight ? part : nullptr, st);
-  if (grad_weight)
-    hipLaunchKernelGGL(k_norm_reduce, dim3((unsigned)((D + 31) / 32)), dim3(BLOCK), 0, st, part,
-                       norm_parts(rows), D, grad_weight);
+  if (grad_weight) launch_add_rows(part, norm_parts(rows), D, grad_weight, st);
   return hipGetLastError();
 }
 

@@ -145,6 +145,35 @@ hipError_t launch_rmsnorm_backward(bool bf16, const void* dy, const void* h, con
                                    const void* dsum, int64_t rows, int D, float eps, void* dx,
                                    float* grad_weight, float* part, hipStream_t st);
 
+// out[c] += the sum over p of part[p, c], in a fixed order.
+void launch_add_rows(const float* part, int parts, int cols, float* out, hipStream_t st);
+
+// ---- projections (linear.hip) ----------------------------------------------
+struct LinearCall {
+  const void* x;
+  const void* w;
+  pkmem_dtype dt;
+  const float* x_scale;
+  const float* w_scale;
+  const void* bias;
+  const void* res;
+  int64_t T;
+  int N, K, act;
+  void* z;
+  void* y;
+  bool out_bf16;
+  void* ws;
+};
+size_t linear_ws_bytes(int64_t T, int N, int K, pkmem_dtype dt);
+hipError_t launch_linear(const LinearCall& c, hipStream_t st);
+hipError_t launch_act_backward(bool bf16, const void* dy, const void* z, int act, int64_t n, void* dz,
+                               hipStream_t st);
+size_t linear_backward_ws_bytes(int64_t T, int N, int K);
+// add, dx, grad_w and grad_bias nullable.
+hipError_t launch_linear_backward(bool bf16, const void* dz, const void* x, const void* w, int64_t T,
+                                  int N, int K, const void* add, void* dx, float* grad_w,
+                                  float* grad_bias, void* ws, hipStream_t st);
+
 // ---- optimizer (adamw.hip) -------------------------------------------------
 constexpr int ADAMW_STATE_BLOCK = 128;  // elements that share the scales of 8-bit states
 // A step's scalars in the precision that the kernels use them in.
