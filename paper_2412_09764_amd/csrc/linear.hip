@@ -229,48 +229,89 @@ __device__ __forceinline__ float act_grad_of(float z, int act) {
   }
 }
 
-__device__ __forceinline__ void load4(const void* p, size_t at, bool bf16, float (&v)[4]) {
-  if (bf16) {
-    const uint2 u = *reinterpret_cast<const uint2*>((const uint16_t*)p + at);
-    v[0] = bf16_lo(u.x); v[1] = bf16_hi(u.x); v[2] = bf16_lo(u.y); v[3] = bf16_hi(u.y);
-  } else {
-    const float4 f = *reinterpret_cast<const float4*>((const float*)p + at);
-    v[0] = f.x; v[1] = f.y; v[2] = f.z; v[3] = f.w;
-  }
+__device__ __forceinline__ void load4(const float* p, size_t at, float (&v)[4]) {
+  const float4 f = *reinterpret_cast<const float4*>(p + at);
+  v[0] = f.x; v[1] = f.y; v[2] = f.z; v[3] = f.w;
 }
-__device__ __forceinline__ void store4(void* p, size_t at, bool bf16, const float (&v)[4]) {
-  if (bf16) *reinterpret_cast<uint2*>((uint16_t*)p + at) = uint2{to_bf16x2(v[0], v[1]), to_bf16x2(v[2], v[3])};
-  else *reinterpret_cast<float4*>((float*)p + at) = float4{v[0], v[1], v[2], v[3]};
+__device__ __forceinline__ void store4(float* p, size_t at, const float (&v)[4]) {
+  *reinterpret_cast<float4*>(p + at) = float4{v[0], v[1], v[2], v[3]};
+}
+// Eight consecutive elements of a bf16 or fp32 array, as stored.
+struct Raw8 {
+  uint4 lo, hi;  // bf16: lo
+  __device__ __forceinline__ void load(const void* p, size_t at, bool bf16) {
+    if (bf16) {
+      lo = ld16((const uint16_t*)p + at);
+    } else {
+      lo = ld16((const float*)p + at);
+      hi = ld16((const float*)p + at + 4);
+    }
+  }
+  __device__ __forceinline__ void unpack(bool bf16, float (&v)[8]) const {
+    if (bf16) {
+      Chunk<uint16_t>::unpack(lo, v);
+    } else {
+      Chunk<float>::unpack(lo, v);
+      Chunk<float>::unpack(hi, v + 4);
+    }
+  }
+};
+__device__ __forceinline__ void store8(void* p, size_t at, bool bf16, const float (&v)[8]) {
+  if (bf16) {
+    *reinterpret_cast<uint4*>((uint16_t*)p + at) = Chunk<uint16_t>::pack(v);
+  } else {
+    *reinterpret_cast<uint4*>((float*)p + at) = Chunk<float>::pack(v);
+    *reinterpret_cast<uint4*>((float*)p + at + 4) = Chunk<float>::pack(v + 4);
+  }
 }
 
-// Four consecutive outputs (i, j .. j + 3) of the product: scales, bias,
-// activation and residual in fp32, one rounding.
-__device__ __forceinline__ void epilogue4(const GemmArgs& g, int64_t i, int j, float sa, float (&v)[4]) {
-  const bool h = g.out_bf16;
-  const size_t at = (size_t)i * g.N + j;
-  if (g.b_scale) {
-    const float4 s = *reinterpret_cast<const float4*>(g.b_scale + j);
-    v[0] *= sa * s.x; v[1] *= sa * s.y; v[2] *= sa * s.z; v[3] *= sa * s.w;
+// The epilogue of 8 columns (from j on, the same for every row a lane handles):
+// scales, bias, activation and residual in fp32, one rounding.
+struct Epilogue {
+  float scale[8], bias[8];
+  __device__ __forceinline__ void init(const GemmArgs& g, int j) {
+    if (j >= g.N) return;
+    if (g.b_scale) {
+      Raw8 r;
+      r.load(g.b_scale, j, false);
+      r.unpack(false, scale);
+    }
+    if (g.bias) {
+      Raw8 r;
+      r.load(g.bias, j, g.out_bf16);
+      r.unpack(g.out_bf16, bias);
+    }
   }
-  if (g.bias) {
-    float b[4];
-    load4(g.bias, j, h, b);
+  __device__ __forceinline__ void store(const GemmArgs& g, size_t at, float sa, const Raw8& res,
+                                        float (&v)[8]) const {
+    const bool h = g.out_bf16;
+    if (g.b_scale) {
 #pragma unroll
-    for (int e = 0; e < 4; ++e) v[e] += b[e];
-  }
-  if (g.z) store4(g.z, at, h, v);
-  if (g.act) {
+      for (int e = 0; e < 8; ++e) v[e] *= sa * scale[e];
+    }
+    if (g.bias) {
 #pragma unroll
-    for (int e = 0; e < 4; ++e) v[e] = h ? act_of<true>(v[e], g.act) : act_of<false>(v[e], g.act);
-  }
-  if (g.res) {
-    float r[4];
-    load4(g.res, at, h, r);
+      for (int e = 0; e < 8; ++e) v[e] += bias[e];
+    }
+    if (g.z) store8(g.z, at, h, v);
+    if (g.act) {
+      if (h) {
 #pragma unroll
-    for (int e = 0; e < 4; ++e) v[e] += r[e];
+        for (int e = 0; e < 8; ++e) v[e] = act_of<true>(v[e], g.act);
+      } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = act_of<false>(v[e], g.act);
+      }
+    }
+    if (g.res) {
+      float r[8];
+      res.unpack(h, r);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[e] += r[e];
+    }
+    store8(g.out, at, h, v);
   }
-  store4(g.out, at, h, v);
-}
+};
 
 // GRAD: C is added to fp32 `out`, or written to `part` when split; else the
 // epilogue above.
@@ -379,33 +420,66 @@ __global__ __launch_bounds__(WM* WN * 64) void k_gemm(const GemmArgs g) {
   if (s + 2 < steps) stage(st2, st3);
   wait_loads<0>();  // no load may reach LDS after the workgroup has left it
 
-  const int il = lane & 31, kh = lane >> 5;
+  // The sums leave through LDS, 64 rows of a wave's 64 columns at a time (16 KiB a
+  // wave), so that eight lanes hold a row's 64 columns: every load and store of
+  // the epilogue covers whole cache lines.  16-byte chunk c of row r lies at slot
+  // c ^ (r & 15).
+  __syncthreads();
+  constexpr int WAVES_PER_STAGE = BYTES / 16384;
+  static_assert(NJ == 2 && MI % 2 == 0 && WAVES_PER_STAGE >= 1, "64 x 64 pieces");
+  const int si = wave / WAVES_PER_STAGE;
+  unsigned char* buf = (si == 0 ? st0 : si == 1 ? st1 : si == 2 ? st2 : st3) + (wave % WAVES_PER_STAGE) * 16384;
+  const int il = lane & 31, kh = lane >> 5, rr = lane >> 3, cc = lane & 7;
+  const int j = j0 + wj + 8 * cc;
+  Epilogue epi;
+  if constexpr (!GRAD) epi.init(g, j);
 #pragma unroll
-  for (int mi = 0; mi < MI; ++mi) {
-    const int64_t i = i0 + wi + mi * 32 + il;
-    if (i >= g.M) continue;
-    const float sa = !GRAD && g.a_scale ? g.a_scale[i] : 1.f;
+  for (int mp = 0; mp < MI; mp += 2) {
+    const int64_t ip = i0 + wi + mp * 32 + rr;
+    Raw8 res[8];
+    if constexpr (!GRAD) {
+      if (g.res) {
 #pragma unroll
-    for (int nj = 0; nj < NJ; ++nj) {
+        for (int t = 0; t < 8; ++t)
+          if (ip + 8 * t < g.M && j < g.N) res[t].load(g.res, (size_t)(ip + 8 * t) * g.N + j, g.out_bf16);
+      }
+    }
 #pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        const int j = j0 + wj + nj * 32 + 8 * r + 4 * kh;
-        if (j >= g.N) continue;
-        float v[4] = {acc[mi][nj][4 * r], acc[mi][nj][4 * r + 1], acc[mi][nj][4 * r + 2], acc[mi][nj][4 * r + 3]};
-        if constexpr (GRAD) {
-          const size_t at = (size_t)i * g.N + j;
-          if (g.part) {
-            store4(g.part, (size_t)split * g.M * g.N + at, false, v);
-          } else {
-            float o[4];
-            load4(g.out, at, false, o);
+    for (int m = 0; m < 2; ++m)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) v[e] += o[e];
-            store4(g.out, at, false, v);
-          }
-        } else {
-          epilogue4(g, i, j, sa, v);
+      for (int nj = 0; nj < 2; ++nj)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const f32x16_t& c = acc[mp + m][nj];
+          const int row = m * 32 + il, ch = nj * 8 + 2 * r + kh;
+          *reinterpret_cast<float4*>(buf + row * 256 + ((ch ^ (row & 15)) << 4)) =
+              float4{c[4 * r], c[4 * r + 1], c[4 * r + 2], c[4 * r + 3]};
         }
+#pragma unroll
+    for (int t = 0; t < 8; ++t) {
+      const int row = 8 * t + rr;
+      const int64_t i = ip + 8 * t;
+      float v[8];
+      Raw8 a;
+      a.lo = ld16(buf + row * 256 + (((2 * cc) ^ (row & 15)) << 4));
+      a.hi = ld16(buf + row * 256 + (((2 * cc + 1) ^ (row & 15)) << 4));
+      if (i >= g.M || j >= g.N) continue;
+      a.unpack(false, v);
+      const size_t at = (size_t)i * g.N + j;
+      if constexpr (GRAD) {
+        if (g.part) {
+          store8(g.part + (size_t)split * g.M * g.N, at, false, v);
+        } else {
+          float o[8];
+          Raw8 old;
+          old.load(g.out, at, false);
+          old.unpack(false, o);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) v[e] += o[e];
+          store8(g.out, at, false, v);
+        }
+      } else {
+        epi.store(g, at, g.a_scale ? g.a_scale[i] : 1.f, res[t], v);
       }
     }
   }
@@ -419,15 +493,15 @@ __global__ __launch_bounds__(256) void k_add_parts(const float* __restrict__ par
   float s[4] = {0.f, 0.f, 0.f, 0.f};
   for (int p = 0; p < splits; ++p) {
     float v[4];
-    load4(part, p * n + at, false, v);
+    load4(part, p * n + at, v);
 #pragma unroll
     for (int e = 0; e < 4; ++e) s[e] += v[e];
   }
   float o[4];
-  load4(out, at, false, o);
+  load4(out, at, o);
 #pragma unroll
   for (int e = 0; e < 4; ++e) o[e] += s[e];
-  store4(out, at, false, o);
+  store4(out, at, o);
 }
 
 // Sums over rows: part[b, c] for the rows of workgroup b (a fixed stride
