@@ -10,8 +10,8 @@
 //
 // Tiles of 256 x 256 by eight waves (128 x 64 each, 32x32 MFMA: per 32 bytes of
 // k a wave reads 6 fragments for 8 products, three quarters of what LDS gives in
-// that time) or, where these are too few for the chip, 128 x 128 by four.  A
-// stage holds 64 bytes of k; four stages are in LDS, filled by direct loads that
+// that time); where these are too few for the chip, smaller ones whose waves
+// also share k (64 x 64 each).  A stage holds 64 bytes of k; four stages are in LDS, filled by direct loads that
 // run three stages ahead, and the fragments of the next half stage are read
 // while the matrix cores work on the current one.
 #include "pk_internal.h"
@@ -23,7 +23,6 @@ namespace pk {
 namespace {
 
 constexpr int STAGE_K = 64;  // bytes of k per stage
-constexpr int NSTAGE = 4;
 constexpr uint32_t OUTSIDE = 0x80000000u;  // past the end of every buffer resource
 
 typedef __attribute__((ext_vector_type(4))) short s16x4_t;
@@ -101,64 +100,57 @@ struct Operand {
   static constexpr int E = elem_size(DT);
   static constexpr int BYTES = R * STAGE_K;
   static constexpr int ROW = KS ? R * E : STAGE_K;     // bytes of an LDS row
-  static constexpr int LOADS = BYTES / 1024 / NWAVE;   // direct loads per wave and stage
+  static constexpr int LOADS = BYTES / 1024 / NWAVE;  // direct loads per wave and stage
   static constexpr int STAGE_ROWS = STAGE_K / E;       // k of a stage
   static_assert(BYTES % (1024 * NWAVE) == 0, "whole loads");
   static constexpr int UNITS = ROW / 64;
 
-  uint32_t off[LOADS];  // this lane's source offsets in a stage
-  uint32_t kb;          // KS = false: byte of k in a stage, the same for all loads up to a swizzle
-  uint32_t kbs[LOADS];
+  uint32_t off[LOADS];  // this lane's source offsets in a stage; OUTSIDE: no such row
   uint32_t rd[R / 32 < 8 ? R / 32 : 8];
-  const char* base;
-  int64_t left, step;   // bytes from base to the end; bytes from stage to stage
-  int64_t kleft;        // KS = false: bytes of k left in this split
+  const char* base;     // of the next stage
+  int64_t step;         // bytes from stage to stage
+  int whole;            // stages left that lie within k
 
   // rows: first row of the tile, of `rows`; k range [k0, k1) of ld = K (or rows) elements
   __device__ __forceinline__ void init(const void* p, int64_t row0, int64_t rows, int64_t K,
                                        int64_t k0, int64_t k1, int wave, int lane) {
-    if constexpr (!KS) {
-      const int64_t ld = K * E;
-      base = (const char*)p + row0 * ld + k0 * E;
-      left = rows * ld - row0 * ld - k0 * E;
-      step = STAGE_K;
-      kleft = (k1 - k0) * E;
+    whole = k1 > k0 ? (int)((k1 - k0) / STAGE_ROWS) : 0;
+    const int64_t ld = (KS ? rows : K) * E;
+    base = (const char*)p + (KS ? k0 * ld + row0 * E : row0 * ld + k0 * E);
+    step = KS ? (int64_t)STAGE_ROWS * ld : STAGE_K;
 #pragma unroll
-      for (int i = 0; i < LOADS; ++i) {
-        const int slot = (i * NWAVE + wave) * 64 + lane;
-        const int r = slot >> 2, c = (slot & 3) ^ ((r >> 1) & 3);
-        off[i] = row0 + r < rows ? (uint32_t)(r * ld + c * 16) : OUTSIDE;
-        kbs[i] = c * 16;
-      }
-    } else {
-      const int64_t ld = rows * E;
-      base = (const char*)p + k0 * ld + row0 * E;
-      left = k1 * ld - k0 * ld - row0 * E;
-      step = (int64_t)STAGE_ROWS * ld;
-#pragma unroll
-      for (int i = 0; i < LOADS; ++i) {
-        const int slot = (i * NWAVE + wave) * 64 + lane;
-        const int k = slot / (ROW / 16);
-        int c = slot % (ROW / 16);
-        if constexpr (DT == D_F32) c ^= ((k >> 2) & 1) << 3;
-        else c ^= (((k & 3) | ((k >> 1) & 4)) & (UNITS - 1)) << 2;
+    for (int i = 0; i < LOADS; ++i) {
+      const int slot = (i * NWAVE + wave) * 64 + lane;
+      if constexpr (!KS) {
+        const int r = slot >> 2;
+        off[i] = row0 + r < rows ? (uint32_t)(r * ld + source_chunk(slot) * 16) : OUTSIDE;
+      } else {
+        const int k = slot / (ROW / 16), c = source_chunk(slot);
         off[i] = row0 + c * (16 / E) < rows ? (uint32_t)(k * ld + c * 16) : OUTSIDE;
       }
     }
   }
-  // The next stage into lds (this wave's loads of it); advances.
-  __device__ __forceinline__ void load(unsigned char* lds, int wave) {
-    const int64_t n = left > 0x7FFFFFFF ? 0x7FFFFFFF : left > 0 ? left : 0;
-    const __amdgpu_buffer_rsrc_t r = raw_buffer(base, (uint32_t)n);
-#pragma unroll
-    for (int i = 0; i < LOADS; ++i) {
-      uint32_t o = off[i];
-      if constexpr (!KS) o = (int64_t)kbs[i] < kleft ? o : OUTSIDE;
-      lds_dma16_buf(r, o, 0u, lds + (i * NWAVE + wave) * 1024);
+  // The 16-byte chunk of its row that a slot of the stage holds.
+  __device__ static __forceinline__ int source_chunk(int slot) {
+    if constexpr (!KS) return (slot & 3) ^ ((slot >> 3) & 3);
+    const int k = slot / (ROW / 16), c = slot % (ROW / 16);
+    if constexpr (DT == D_F32) return c ^ (((k >> 2) & 1) << 3);
+    return c ^ ((((k & 3) | ((k >> 1) & 4)) & (UNITS - 1)) << 2);
+  }
+  // Load i of this wave of the next stage into lds; `left`: k of the range from
+  // that stage on (0 or less: nothing is read, the slots become 0).
+  __device__ __forceinline__ void load(int i, unsigned char* lds, int wave, int lane, int left) const {
+    uint32_t o = off[i];
+    if (whole <= 0) {  // the end of k lies in this stage, or before it
+      const int slot = (i * NWAVE + wave) * 64 + lane;
+      const int k = KS ? slot / (ROW / 16) : source_chunk(slot) * (16 / E);
+      o = k < left ? o : OUTSIDE;
     }
+    lds_dma16_buf(raw_buffer(base, 0x7FFFFFFFu), o, 0u, lds + (i * NWAVE + wave) * 1024);
+  }
+  __device__ __forceinline__ void advance() {
     base += step;
-    left -= step;
-    if constexpr (!KS) kleft -= STAGE_K;
+    --whole;
   }
   // Read addresses of this lane for blocks of 32 rows from row r0 on.
   template <int NB>
@@ -205,28 +197,47 @@ __device__ __forceinline__ float sigmoid_of(float z) {
   if constexpr (FAST) return __builtin_amdgcn_rcpf(1.f + __expf(-z));
   return 1.f / (1.f + expf(-z));
 }
-__device__ __forceinline__ float erf_of(float x) { return erff(x); }
+// FAST: Abramowitz and Stegun 7.1.26, off by at most 1.5e-7.
 template <bool FAST>
-__device__ __forceinline__ float act_of(float z, int act) {
-  switch (act) {
-    case PKMEM_ACT_RELU: return z > 0.f ? z : (z != z ? z : 0.f);
-    case PKMEM_ACT_SILU: return FAST ? z * sigmoid_of<true>(z) : z / (1.f + expf(-z));
-    case PKMEM_ACT_GELU: return 0.5f * z * (1.f + erf_of(z * 0.70710678118654752f));
-    default: return z;
-  }
+__device__ __forceinline__ float erf_of(float x) {
+  if constexpr (!FAST) return erff(x);
+  const float a = fabsf(x), t = __builtin_amdgcn_rcpf(fmaf(0.3275911f, a, 1.f));
+  const float p = t * fmaf(t, fmaf(t, fmaf(t, fmaf(t, 1.061405429f, -1.453152027f), 1.421413741f), -0.284496736f), 0.254829592f);
+  return copysignf(1.f - p * __expf(-a * a), x);
 }
-template <bool FAST>
-__device__ __forceinline__ float act_grad_of(float z, int act) {
-  switch (act) {
-    case PKMEM_ACT_RELU: return z > 0.f ? 1.f : (z != z ? z : 0.f);
-    case PKMEM_ACT_SILU: {
-      const float s = sigmoid_of<FAST>(z);
-      return s * (1.f + z * (1.f - s));
-    }
-    case PKMEM_ACT_GELU:
-      return 0.5f * (1.f + erf_of(z * 0.70710678118654752f)) + z * expf(-0.5f * z * z) * 0.39894228040143268f;
-    default: return 1.f;
+template <bool FAST, int ACT>
+__device__ __forceinline__ float act_of(float z) {
+  if constexpr (ACT == PKMEM_ACT_RELU) return z > 0.f ? z : (z != z ? z : 0.f);
+  if constexpr (ACT == PKMEM_ACT_SILU) return FAST ? z * sigmoid_of<true>(z) : z / (1.f + expf(-z));
+  if constexpr (ACT == PKMEM_ACT_GELU) return 0.5f * z * (1.f + erf_of<FAST>(z * 0.70710678118654752f));
+  return z;
+}
+template <bool FAST, int ACT>
+__device__ __forceinline__ float act_grad_of(float z) {
+  if constexpr (ACT == PKMEM_ACT_RELU) return z > 0.f ? 1.f : (z != z ? z : 0.f);
+  if constexpr (ACT == PKMEM_ACT_SILU) {
+    const float s = sigmoid_of<FAST>(z);
+    return s * (1.f + z * (1.f - s));
   }
+  if constexpr (ACT == PKMEM_ACT_GELU)
+    return 0.5f * (1.f + erf_of<FAST>(z * 0.70710678118654752f)) +
+           z * (FAST ? __expf(-0.5f * z * z) : expf(-0.5f * z * z)) * 0.39894228040143268f;
+  return 1.f;
+}
+template <bool FAST, int N>
+__device__ __forceinline__ void apply_act(float (&v)[N], int act) {
+#define PK_ACT(A)                                             \
+  case A: {                                                   \
+    _Pragma("unroll") for (int e = 0; e < N; ++e) v[e] = act_of<FAST, A>(v[e]); \
+    break;                                                    \
+  }
+  switch (act) {
+    PK_ACT(PKMEM_ACT_RELU)
+    PK_ACT(PKMEM_ACT_SILU)
+    PK_ACT(PKMEM_ACT_GELU)
+    default: break;
+  }
+#undef PK_ACT
 }
 
 __device__ __forceinline__ void load4(const float* p, size_t at, float (&v)[4]) {
@@ -294,15 +305,8 @@ struct Epilogue {
       for (int e = 0; e < 8; ++e) v[e] += bias[e];
     }
     if (g.z) store8(g.z, at, h, v);
-    if (g.act) {
-      if (h) {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = act_of<true>(v[e], g.act);
-      } else {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = act_of<false>(v[e], g.act);
-      }
-    }
+    if (h) apply_act<true>(v, g.act);
+    else apply_act<false>(v, g.act);
     if (g.res) {
       float r[8];
       res.unpack(h, r);
@@ -313,19 +317,20 @@ struct Epilogue {
   }
 };
 
-// GRAD: C is added to fp32 `out`, or written to `part` when split; else the
+// KG groups of waves share the tile's k.  GRAD: C is added to fp32 `out`, or written to `part` when split; else the
 // epilogue above.
-template <int DT, bool AKS, bool BKS, bool GRAD, int BM, int BN, int WM, int WN>
-__global__ __launch_bounds__(WM* WN * 64) void k_gemm(const GemmArgs g) {
+template <int DT, bool AKS, bool BKS, bool GRAD, int BM, int BN, int WM, int WN, int KG>
+__global__ __launch_bounds__(WM* WN* KG * 64) void k_gemm(const GemmArgs g) {
   constexpr int NW = WM * WN, MI = BM / WM / 32, NJ = BN / WN / 32;
   using OA = Operand<DT, AKS, BM, NW>;
   using OB = Operand<DT, BKS, BN, NW>;
   constexpr int L = OA::LOADS + OB::LOADS;
-  constexpr int BYTES = OA::BYTES + OB::BYTES;
+  constexpr int GROUP_BYTES = OA::BYTES + OB::BYTES, BYTES = KG * GROUP_BYTES;
   // a variable for each stage: the compiler then knows which loads a read of
   // LDS depends on, and waits for no other
   __shared__ __align__(1024) unsigned char st0[BYTES], st1[BYTES], st2[BYTES], st3[BYTES];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int wave = w % NW, kg = w / NW;
 
   // XCD x (workgroup number mod 8) takes a contiguous run of tiles; within it
   // four rows of tiles at a time, so that what one XCD's L2 holds is shared.
@@ -340,8 +345,15 @@ __global__ __launch_bounds__(WM* WN * 64) void k_gemm(const GemmArgs g) {
   pid -= group * 4 * g.tiles_n;
   const int64_t i0 = (int64_t)(m_first + pid % m_count) * BM;
   const int j0 = (pid / m_count) * BN;
-  const int64_t k0 = split * g.k_split;
-  const int64_t k1 = k0 + g.k_split < g.K ? k0 + g.k_split : g.K;
+  int64_t k0 = split * g.k_split;
+  int64_t k1 = k0 + g.k_split < g.K ? k0 + g.k_split : g.K;
+  // this group's share of k; all groups take the same number of steps
+  const int steps = (int)((k1 - k0 + KG * OA::STAGE_ROWS - 1) / (KG * OA::STAGE_ROWS));
+  if constexpr (KG > 1) {
+    k0 += (int64_t)kg * steps * OA::STAGE_ROWS;
+    const int64_t end = k0 + (int64_t)steps * OA::STAGE_ROWS;
+    k1 = end < k1 ? end : k1;
+  }
 
   OA oa;
   OB ob;
@@ -351,16 +363,28 @@ __global__ __launch_bounds__(WM* WN * 64) void k_gemm(const GemmArgs g) {
   oa.template init_read<MI>(wi, lane);
   ob.template init_read<NJ>(wj, lane);
 
-  const int steps = (int)((k1 - k0 + OA::STAGE_ROWS - 1) / OA::STAGE_ROWS);
   f32x16_t acc[MI][NJ];
 #pragma unroll
   for (int mi = 0; mi < MI; ++mi)
 #pragma unroll
     for (int nj = 0; nj < NJ; ++nj) acc[mi][nj] = f32x16_t{};
 
+  const int group_at = KG > 1 ? kg * GROUP_BYTES : 0;
+  int left = k1 > k0 ? (int)(k1 - k0 < 0x7FFFFFFF ? k1 - k0 : 0x7FFFFFFF) : 0;
+  // Load i of a stage (A's first), and the step to the next one.
+  auto load = [&](unsigned char* st, int i) PK_INLINE {
+    if (i < OA::LOADS) oa.load(i, st + group_at, wave, lane, left);
+    else ob.load(i - OA::LOADS, st + group_at + OA::BYTES, wave, lane, left);
+  };
+  auto advance = [&]() PK_INLINE {
+    oa.advance();
+    ob.advance();
+    left -= OA::STAGE_ROWS;
+  };
   auto fill = [&](unsigned char* st) PK_INLINE {
-    oa.load(st, wave);
-    ob.load(st + OA::BYTES, wave);
+#pragma unroll
+    for (int i = 0; i < L; ++i) load(st, i);
+    advance();
   };
   fill(st0);
   fill(st1);
@@ -371,41 +395,52 @@ __global__ __launch_bounds__(WM* WN * 64) void k_gemm(const GemmArgs g) {
   uint4 fa[2][MI], fb[2][NJ];
   auto read = [&](const unsigned char* st, int h) PK_INLINE {
 #pragma unroll
-    for (int nj = 0; nj < NJ; ++nj) fb[h][nj] = ob.frag(st + OA::BYTES, nj, h);
+    for (int nj = 0; nj < NJ; ++nj) fb[h][nj] = ob.frag(st + group_at + OA::BYTES, nj, h);
 #pragma unroll
-    for (int mi = 0; mi < MI; ++mi) fa[h][mi] = oa.frag(st, mi, h);
+    for (int mi = 0; mi < MI; ++mi) fa[h][mi] = oa.frag(st + group_at, mi, h);
   };
-  auto products = [&](int h) PK_INLINE {
-    if constexpr (DT == D_E4M3) {
+  // The products of half h, by blocks of A's rows; between them, where asked for,
+  // the loads of a stage into st.
+  auto products = [&](int h, bool refill, unsigned char* st) PK_INLINE {
+    constexpr int GROUPS = DT == D_E4M3 ? 2 * MI : MI;
+    uint4 b[NJ];
 #pragma unroll
-      for (int part = 0; part < 2; ++part) {
-        uint4 b[NJ];
+    for (int q = 0; q < GROUPS; ++q) {
+      const int mi = q % MI;
+      if constexpr (DT == D_E4M3) {
+        if (mi == 0) {
 #pragma unroll
-        for (int nj = 0; nj < NJ; ++nj)
-          b[nj] = part ? widen8(fb[h][nj].z, fb[h][nj].w) : widen8(fb[h][nj].x, fb[h][nj].y);
-#pragma unroll
-        for (int mi = 0; mi < MI; ++mi) {
-          const uint4 a = part ? widen8(fa[h][mi].z, fa[h][mi].w) : widen8(fa[h][mi].x, fa[h][mi].y);
-#pragma unroll
-          for (int nj = 0; nj < NJ; ++nj) mma<D_BF16>(b[nj], a, acc[mi][nj]);
+          for (int nj = 0; nj < NJ; ++nj)
+            b[nj] = q ? widen8(fb[h][nj].z, fb[h][nj].w) : widen8(fb[h][nj].x, fb[h][nj].y);
         }
-      }
-    } else {
+        const uint4 a = q >= MI ? widen8(fa[h][mi].z, fa[h][mi].w) : widen8(fa[h][mi].x, fa[h][mi].y);
 #pragma unroll
-      for (int mi = 0; mi < MI; ++mi)
+        for (int nj = 0; nj < NJ; ++nj) mma<D_BF16>(b[nj], a, acc[mi][nj]);
+      } else {
 #pragma unroll
         for (int nj = 0; nj < NJ; ++nj) mma<DT>(fb[h][nj], fa[h][mi], acc[mi][nj]);
+      }
+      if (refill) {
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int i = q * L / GROUPS; i < (q + 1) * L / GROUPS; ++i) load(st, i);
+        __builtin_amdgcn_sched_barrier(0);
+      }
     }
   };
   // One stage: st is visible to all, half 0 of it in registers.  After the
-  // barrier every wave has read st, and next has landed for all.
+  // barrier every wave has read st, and next has landed for all.  The reads of
+  // a half are issued before the products of the half before it and return
+  // while these run.
   auto stage = [&](unsigned char* st, const unsigned char* next) PK_INLINE {
     read(st, 1);
-    products(0);
+    __builtin_amdgcn_sched_barrier(0);
+    products(0, false, st);
     wait_and_meet<2 * L>();
-    fill(st);
     read(next, 0);
-    products(1);
+    __builtin_amdgcn_sched_barrier(0);
+    products(1, true, st);
+    advance();
   };
   read(st0, 0);
   int s = 0;
@@ -423,24 +458,30 @@ __global__ __launch_bounds__(WM* WN * 64) void k_gemm(const GemmArgs g) {
   // The sums leave through LDS, 64 rows of a wave's 64 columns at a time (16 KiB a
   // wave), so that eight lanes hold a row's 64 columns: every load and store of
   // the epilogue covers whole cache lines.  16-byte chunk c of row r lies at slot
-  // c ^ (r & 15).
+  // c ^ (r & 15).  The waves of the groups of k that share a piece add its parts
+  // in group order, each for its share of the rows.
   __syncthreads();
-  constexpr int WAVES_PER_STAGE = BYTES / 16384;
+  constexpr int WAVES_PER_STAGE = BYTES / 16384, ROWS = 8 / KG;
   static_assert(NJ == 2 && MI % 2 == 0 && WAVES_PER_STAGE >= 1, "64 x 64 pieces");
-  const int si = wave / WAVES_PER_STAGE;
-  unsigned char* buf = (si == 0 ? st0 : si == 1 ? st1 : si == 2 ? st2 : st3) + (wave % WAVES_PER_STAGE) * 16384;
+  static_assert(KG == 1 || MI == 2, "one piece a wave where k is shared");
+  auto piece = [&](int w) PK_INLINE {
+    const int si = w / WAVES_PER_STAGE;
+    return (si == 0 ? st0 : si == 1 ? st1 : si == 2 ? st2 : st3) + (w % WAVES_PER_STAGE) * 16384;
+  };
+  unsigned char* buf = piece(kg * NW + wave);
   const int il = lane & 31, kh = lane >> 5, rr = lane >> 3, cc = lane & 7;
   const int j = j0 + wj + 8 * cc;
   Epilogue epi;
   if constexpr (!GRAD) epi.init(g, j);
 #pragma unroll
   for (int mp = 0; mp < MI; mp += 2) {
-    const int64_t ip = i0 + wi + mp * 32 + rr;
-    Raw8 res[8];
+    const int row0 = kg * ROWS * 8 + rr;
+    const int64_t ip = i0 + wi + mp * 32 + row0;
+    Raw8 res[ROWS];
     if constexpr (!GRAD) {
       if (g.res) {
 #pragma unroll
-        for (int t = 0; t < 8; ++t)
+        for (int t = 0; t < ROWS; ++t)
           if (ip + 8 * t < g.M && j < g.N) res[t].load(g.res, (size_t)(ip + 8 * t) * g.N + j, g.out_bf16);
       }
     }
@@ -455,16 +496,24 @@ __global__ __launch_bounds__(WM* WN * 64) void k_gemm(const GemmArgs g) {
           *reinterpret_cast<float4*>(buf + row * 256 + ((ch ^ (row & 15)) << 4)) =
               float4{c[4 * r], c[4 * r + 1], c[4 * r + 2], c[4 * r + 3]};
         }
+    if constexpr (KG > 1) __syncthreads();
 #pragma unroll
-    for (int t = 0; t < 8; ++t) {
-      const int row = 8 * t + rr;
+    for (int t = 0; t < ROWS; ++t) {
+      const int row = row0 + 8 * t;
       const int64_t i = ip + 8 * t;
       float v[8];
-      Raw8 a;
-      a.lo = ld16(buf + row * 256 + (((2 * cc) ^ (row & 15)) << 4));
-      a.hi = ld16(buf + row * 256 + (((2 * cc + 1) ^ (row & 15)) << 4));
+#pragma unroll
+      for (int q = 0; q < KG; ++q) {
+        const unsigned char* from = KG > 1 ? piece(q * NW + wave) : buf;
+        Raw8 a;
+        a.lo = ld16(from + row * 256 + (((2 * cc) ^ (row & 15)) << 4));
+        a.hi = ld16(from + row * 256 + (((2 * cc + 1) ^ (row & 15)) << 4));
+        float u[8];
+        a.unpack(false, u);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = q ? v[e] + u[e] : u[e];
+      }
       if (i >= g.M || j >= g.N) continue;
-      a.unpack(false, v);
       const size_t at = (size_t)i * g.N + j;
       if constexpr (GRAD) {
         if (g.part) {
@@ -483,6 +532,92 @@ __global__ __launch_bounds__(WM* WN * 64) void k_gemm(const GemmArgs g) {
       }
     }
   }
+}
+
+// Few rows of x: a workgroup takes 16 rows of W and up to 16 TT rows of x; its
+// waves share k in chunks of 64 bytes, straight from memory into the 16x16
+// fragments (rows past the end are read as the last one and dropped), and add
+// their sums through LDS in wave order.  Bound by reading W once.
+template <int DT>
+struct Few {
+  typedef __attribute__((ext_vector_type(4))) float f32x4_t;
+  __device__ static __forceinline__ void mma16(uint4 w, uint4 x, f32x4_t& c) {
+    if constexpr (DT == D_F32) {
+      c = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(w.x), __uint_as_float(x.x), c, 0, 0, 0);
+      c = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(w.y), __uint_as_float(x.y), c, 0, 0, 0);
+      c = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(w.z), __uint_as_float(x.z), c, 0, 0, 0);
+      c = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(w.w), __uint_as_float(x.w), c, 0, 0, 0);
+    } else if constexpr (DT == D_BF16) {
+      c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, w),
+                                                  __builtin_bit_cast(bf16x8_t, x), c, 0, 0, 0);
+    } else {
+      c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, widen8(w.x, w.y)),
+                                                  __builtin_bit_cast(bf16x8_t, widen8(x.x, x.y)), c, 0, 0, 0);
+      c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, widen8(w.z, w.w)),
+                                                  __builtin_bit_cast(bf16x8_t, widen8(x.z, x.w)), c, 0, 0, 0);
+    }
+  }
+};
+constexpr int FEW_WAVES = 8;
+constexpr int FEW_T = 64;  // rows of x up to which this form is taken
+
+template <int DT, int TT>
+__global__ __launch_bounds__(FEW_WAVES * 64) void k_gemm_few(const GemmArgs g) {
+  using F = Few<DT>;
+  constexpr int AHEAD = 4;  // chunks in flight
+  __shared__ __align__(16) float sums[FEW_WAVES][TT * 16][16];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int n0 = blockIdx.x * 16, kq = (lane >> 4) * 16;
+  const int64_t t0 = (int64_t)blockIdx.y * (16 * TT);
+  const int64_t row_bytes = g.K * elem_size(DT);
+  const int n = n0 + (lane & 15);
+  const char* wp = (const char*)g.b + (int64_t)(n < g.N ? n : g.N - 1) * row_bytes + kq;
+  const char* xp[TT];
+#pragma unroll
+  for (int t = 0; t < TT; ++t) {
+    const int64_t r = t0 + 16 * t + (lane & 15);
+    xp[t] = (const char*)g.a + (r < g.M ? r : g.M - 1) * row_bytes + kq;
+  }
+  typename F::f32x4_t acc[TT];
+#pragma unroll
+  for (int t = 0; t < TT; ++t) acc[t] = typename F::f32x4_t{0.f, 0.f, 0.f, 0.f};
+  const uint4 zero{0, 0, 0, 0};
+  for (int64_t kb = wave * 64; kb < row_bytes; kb += FEW_WAVES * 64 * AHEAD) {
+    uint4 w[AHEAD], x[AHEAD][TT];
+#pragma unroll
+    for (int a = 0; a < AHEAD; ++a) {
+      const int64_t at = kb + a * (FEW_WAVES * 64);
+      const bool in = at + kq < row_bytes;
+      w[a] = in ? ld16_nt(wp + at) : zero;
+#pragma unroll
+      for (int t = 0; t < TT; ++t) x[a][t] = in ? ld16(xp[t] + at) : zero;
+    }
+#pragma unroll
+    for (int a = 0; a < AHEAD; ++a)
+#pragma unroll
+      for (int t = 0; t < TT; ++t) F::mma16(w[a], x[a][t], acc[t]);
+  }
+#pragma unroll
+  for (int t = 0; t < TT; ++t)
+    *reinterpret_cast<float4*>(&sums[wave][16 * t + (lane & 15)][4 * (lane >> 4)]) =
+        float4{acc[t][0], acc[t][1], acc[t][2], acc[t][3]};
+  __syncthreads();
+  const int r = threadIdx.x >> 1, c = (threadIdx.x & 1) * 8;
+  const int64_t i = t0 + r;
+  const int j = n0 + c;
+  if (r >= 16 * TT || i >= g.M || j >= g.N) return;
+  Epilogue epi;
+  epi.init(g, j);
+  Raw8 res;
+  const size_t at = (size_t)i * g.N + j;
+  if (g.res) res.load(g.res, at, g.out_bf16);
+  float v[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) v[e] = sums[0][r][c + e];
+  for (int q = 1; q < FEW_WAVES; ++q)
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] += sums[q][r][c + e];
+  epi.store(g, at, g.a_scale ? g.a_scale[i] : 1.f, res, v);
 }
 
 // out += part[0] + part[1] + ... in this order, 4 elements a thread.
@@ -528,51 +663,71 @@ __global__ __launch_bounds__(256) void k_column_sums(const T* __restrict__ x, in
 }
 
 // dz = dy act'(z), 16 bytes a thread.
-template <typename T, bool FAST>
-__global__ __launch_bounds__(256) void k_act_bwd(const T* dy, const T* z, int act, int64_t chunks, T* dz) {
+template <typename T, bool FAST, int ACT>
+__global__ __launch_bounds__(256) void k_act_bwd(const T* dy, const T* z, int64_t chunks, T* dz) {
   using Ch = Chunk<T>;
   for (int64_t c = (int64_t)blockIdx.x * 256 + threadIdx.x; c < chunks; c += (int64_t)gridDim.x * 256) {
     float d[Ch::N], v[Ch::N];
     Ch::unpack(ld16_nt(dy + c * Ch::N), d);
     Ch::unpack(ld16_nt(z + c * Ch::N), v);
 #pragma unroll
-    for (int e = 0; e < Ch::N; ++e) d[e] *= act_grad_of<FAST>(v[e], act);
+    for (int e = 0; e < Ch::N; ++e) d[e] *= act_grad_of<FAST, ACT>(v[e]);
     *reinterpret_cast<uint4*>(dz + c * Ch::N) = Ch::pack(d);
   }
 }
 
 inline int ceil_div(int64_t a, int64_t b) { return (int)((a + b - 1) / b); }
 
-constexpr int64_t BIG_TILES = 200;  // 256 x 256 tiles from which on they fill the chip
-
-template <int DT, bool AKS, bool BKS, bool GRAD>
-void gemm_launch(GemmArgs g, bool big, int splits, hipStream_t st) {
-  const int t = big ? 256 : 128;
-  g.tiles_m = ceil_div(g.M, t);
-  g.tiles_n = ceil_div(g.N, t);
-  const dim3 grid((unsigned)(g.tiles_m * g.tiles_n * splits));
-  if (big)
-    hipLaunchKernelGGL((k_gemm<DT, AKS, BKS, GRAD, 256, 256, 2, 4>), grid, dim3(512), 0, st, g);
-  else
-    hipLaunchKernelGGL((k_gemm<DT, AKS, BKS, GRAD, 128, 128, 2, 2>), grid, dim3(256), 0, st, g);
+// Tiles: 256 x 256 by eight waves; 128 x 128 by four, and four more for the other
+// half of k; 64 x 64 by four waves that share k.
+enum { TILE_256, TILE_128, TILE_64 };
+constexpr int tile_size(int t) { return t == TILE_256 ? 256 : t == TILE_128 ? 128 : 64; }
+int64_t tile_count(int t, int64_t M, int64_t N) { return (int64_t)ceil_div(M, tile_size(t)) * ceil_div(N, tile_size(t)); }
+// The largest tiles that are enough to fill the chip.
+int pick_tile(int64_t M, int64_t N) {
+  if (tile_count(TILE_256, M, N) >= 200) return TILE_256;
+  if (tile_count(TILE_128, M, N) >= 128) return TILE_128;
+  return TILE_64;
 }
 
-bool big_tiles(int64_t M, int64_t N) { return (int64_t)ceil_div(M, 256) * ceil_div(N, 256) >= BIG_TILES; }
+template <int DT, bool AKS, bool BKS, bool GRAD>
+void gemm_launch(GemmArgs g, int tile, int splits, hipStream_t st) {
+  g.tiles_m = ceil_div(g.M, tile_size(tile));
+  g.tiles_n = ceil_div(g.N, tile_size(tile));
+  const dim3 grid((unsigned)(g.tiles_m * g.tiles_n * splits));
+  if (tile == TILE_256)
+    hipLaunchKernelGGL((k_gemm<DT, AKS, BKS, GRAD, 256, 256, 2, 4, 1>), grid, dim3(512), 0, st, g);
+  else if (tile == TILE_128)
+    hipLaunchKernelGGL((k_gemm<DT, AKS, BKS, GRAD, 128, 128, 2, 2, 2>), grid, dim3(512), 0, st, g);
+  else
+    hipLaunchKernelGGL((k_gemm<DT, AKS, BKS, GRAD, 64, 64, 1, 1, 4>), grid, dim3(256), 0, st, g);
+}
+template <int DT>
+void few_launch(const GemmArgs& g, hipStream_t st) {
+  const int tt = g.M <= 16 ? 1 : g.M <= 32 ? 2 : 4;
+  const dim3 grid((unsigned)ceil_div(g.N, 16), (unsigned)ceil_div(g.M, 16 * tt)), block(FEW_WAVES * 64);
+  if (tt == 1) hipLaunchKernelGGL((k_gemm_few<DT, 1>), grid, block, 0, st, g);
+  else if (tt == 2) hipLaunchKernelGGL((k_gemm_few<DT, 2>), grid, block, 0, st, g);
+  else hipLaunchKernelGGL((k_gemm_few<DT, 4>), grid, block, 0, st, g);
+}
+template <int DT>
+void forward_launch(const GemmArgs& g, hipStream_t st) {
+  if (g.M <= FEW_T) few_launch<DT>(g, st);
+  else gemm_launch<DT, false, false, false>(g, pick_tile(g.M, g.N), 1, st);
+}
 
 // grad_W [N, K] from T tokens: tiles of its own shape, the tokens split so that
 // the workgroups fill the chip; at least 512 tokens a split.
 struct GradPlan {
-  bool big;
-  int splits;
+  int tile, splits;
   int64_t k_split;
 };
 GradPlan grad_plan(int64_t T, int N, int K) {
   GradPlan p;
-  const int64_t b = (int64_t)ceil_div(N, 256) * ceil_div(K, 256);
-  p.big = b >= 16 && T >= 4096;
-  const int64_t tiles = p.big ? b : (int64_t)ceil_div(N, 128) * ceil_div(K, 128);
-  int64_t s = (p.big ? 256 : 512) / tiles;
-  const int64_t most = T / 512;
+  p.tile = tile_count(TILE_256, N, K) >= 16 && T >= 4096 ? TILE_256
+           : tile_count(TILE_128, N, K) >= 32 ? TILE_128 : TILE_64;
+  int64_t s = 256 / tile_count(p.tile, N, K);
+  const int64_t most = T / 256;
   if (s > most) s = most;
   if (s < 1) s = 1;
   if (s > 64) s = 64;
@@ -604,10 +759,9 @@ hipError_t launch_linear(const LinearCall& c, hipStream_t st) {
   g.out = c.y;
   g.act = c.act;
   g.out_bf16 = c.out_bf16;
-  const bool big = big_tiles(c.T, c.N);
-  if (c.dt == PKMEM_BF16) gemm_launch<D_BF16, false, false, false>(g, big, 1, st);
-  else if (c.dt == PKMEM_E4M3) gemm_launch<D_E4M3, false, false, false>(g, big, 1, st);
-  else gemm_launch<D_F32, false, false, false>(g, big, 1, st);
+  if (c.dt == PKMEM_BF16) forward_launch<D_BF16>(g, st);
+  else if (c.dt == PKMEM_E4M3) forward_launch<D_E4M3>(g, st);
+  else forward_launch<D_F32>(g, st);
   return hipGetLastError();
 }
 
@@ -623,12 +777,22 @@ hipError_t launch_act_backward(bool bf16, const void* dy, const void* z, int act
   const int64_t chunks = n / (bf16 ? 8 : 4);
   int64_t blocks = (chunks + 255) / 256;
   if (blocks > 16384) blocks = 16384;
-  if (bf16)
-    hipLaunchKernelGGL((k_act_bwd<uint16_t, true>), dim3((unsigned)blocks), dim3(256), 0, st,
-                       (const uint16_t*)dy, (const uint16_t*)z, act, chunks, (uint16_t*)dz);
-  else
-    hipLaunchKernelGGL((k_act_bwd<float, false>), dim3((unsigned)blocks), dim3(256), 0, st,
-                       (const float*)dy, (const float*)z, act, chunks, (float*)dz);
+#define PK_ACT(A)                                                                                  \
+  case A:                                                                                          \
+    if (bf16)                                                                                      \
+      hipLaunchKernelGGL((k_act_bwd<uint16_t, true, A>), dim3((unsigned)blocks), dim3(256), 0, st, \
+                         (const uint16_t*)dy, (const uint16_t*)z, chunks, (uint16_t*)dz);          \
+    else                                                                                           \
+      hipLaunchKernelGGL((k_act_bwd<float, false, A>), dim3((unsigned)blocks), dim3(256), 0, st,   \
+                         (const float*)dy, (const float*)z, chunks, (float*)dz);                   \
+    break;
+  switch (act) {
+    PK_ACT(PKMEM_ACT_RELU)
+    PK_ACT(PKMEM_ACT_SILU)
+    PK_ACT(PKMEM_ACT_GELU)
+    PK_ACT(PKMEM_ACT_NONE)
+  }
+#undef PK_ACT
   return hipGetLastError();
 }
 
@@ -653,9 +817,9 @@ hipError_t launch_linear_backward(bool bf16, const void* dz, const void* x, cons
     g.res = add;
     g.out = dx;
     g.out_bf16 = bf16;
-    const bool big = big_tiles(T, K);
-    if (bf16) gemm_launch<D_BF16, false, true, false>(g, big, 1, st);
-    else gemm_launch<D_F32, false, true, false>(g, big, 1, st);
+    const int tile = pick_tile(T, K);
+    if (bf16) gemm_launch<D_BF16, false, true, false>(g, tile, 1, st);
+    else gemm_launch<D_F32, false, true, false>(g, tile, 1, st);
   }
   char* p = (char*)ws;
   const GradPlan plan = grad_plan(T, N, K);
@@ -669,8 +833,8 @@ hipError_t launch_linear_backward(bool bf16, const void* dz, const void* x, cons
     g.k_split = plan.k_split;
     g.out = grad_w;
     g.part = plan.splits > 1 ? (float*)p : nullptr;
-    if (bf16) gemm_launch<D_BF16, true, true, true>(g, plan.big, plan.splits, st);
-    else gemm_launch<D_F32, true, true, true>(g, plan.big, plan.splits, st);
+    if (bf16) gemm_launch<D_BF16, true, true, true>(g, plan.tile, plan.splits, st);
+    else gemm_launch<D_F32, true, true, true>(g, plan.tile, plan.splits, st);
     if (plan.splits > 1) {
       const size_t n = (size_t)N * K;
       hipLaunchKernelGGL(k_add_parts, dim3((unsigned)((n / 4 + 255) / 256)), dim3(256), 0, st, g.part,
