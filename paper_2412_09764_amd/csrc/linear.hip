@@ -91,7 +91,8 @@ __device__ __forceinline__ uint4 widen8(uint32_t lo, uint32_t hi) {
 
 // An operand's tile: R rows by one stage of k.
 //   KS = false: LDS [R][64 bytes of k]; 16-byte chunk c of row r lies at slot
-//     c ^ ((r >> 1) & 3), so eight rows' reads of one chunk cover all banks.
+//     c ^ ((r >> 2) & 3): the 16 lanes that LDS serves at once (lanes 0-3, 12-15,
+//     20-27 and so on) then read 16 different 16-byte columns of its 64 banks.
 //   KS = true: LDS [k][R elements]; the 64-byte (bf16) or 128-byte (fp32) units
 //     of a k row are permuted by k so that the k rows of one read instruction
 //     lie in different banks.
@@ -132,7 +133,7 @@ struct Operand {
   }
   // The 16-byte chunk of its row that a slot of the stage holds.
   __device__ static __forceinline__ int source_chunk(int slot) {
-    if constexpr (!KS) return (slot & 3) ^ ((slot >> 3) & 3);
+    if constexpr (!KS) return (slot & 3) ^ ((slot >> 4) & 3);
     const int k = slot / (ROW / 16), c = slot % (ROW / 16);
     if constexpr (DT == D_F32) return c ^ (((k >> 2) & 1) << 3);
     return c ^ ((((k & 3) | ((k >> 1) & 4)) & (UNITS - 1)) << 2);
@@ -157,7 +158,7 @@ struct Operand {
   __device__ __forceinline__ void init_read(int r0, int lane) {
     if constexpr (!KS) {
       const int r = r0 + (lane & 31);
-      rd[0] = r * STAGE_K + (((lane >> 5) ^ ((r >> 1) & 3)) << 4);
+      rd[0] = r * STAGE_K + (((lane >> 5) ^ ((r >> 2) & 3)) << 4);
     } else if constexpr (DT == D_F32) {
       const int kh = lane >> 5;
 #pragma unroll
@@ -639,26 +640,49 @@ __global__ __launch_bounds__(256) void k_add_parts(const float* __restrict__ par
   store4(out, at, o);
 }
 
-// Sums over rows: part[b, c] for the rows of workgroup b (a fixed stride
-// apart), 8 columns a thread; the parts are added by launch_add_rows.
+// Sums over rows: part[b, c] for the rows of workgroup b (four at a time, one a
+// wave, 4 gridDim.x apart), 64 chunks of columns a workgroup; the parts are
+// added by launch_add_rows.
 template <typename T>
 __global__ __launch_bounds__(256) void k_column_sums(const T* __restrict__ x, int64_t rows, int N,
                                                      float* __restrict__ part) {
-  constexpr int C = Chunk<T>::N;
-  const int chunks = N / C;
-  for (int c = blockIdx.y * 256 + threadIdx.x; c < chunks; c += gridDim.y * 256) {
-    float s[C];
+  constexpr int C = Chunk<T>::N, AHEAD = 8;
+  __shared__ float sums[3][64][C + 1];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int c = blockIdx.y * 64 + lane;
+  const bool in = c < N / C;
+  const int64_t step = 4 * (int64_t)gridDim.x;
+  float s[C];
 #pragma unroll
-    for (int e = 0; e < C; ++e) s[e] = 0.f;
-#pragma unroll 4
-    for (int64_t r = blockIdx.x; r < rows; r += gridDim.x) {
-      float v[C];
-      Chunk<T>::unpack(ld16(x + (size_t)r * N + (size_t)c * C), v);
+  for (int e = 0; e < C; ++e) s[e] = 0.f;
+  if (in) {
+    for (int64_t r = 4 * (int64_t)blockIdx.x + wave; r < rows; r += AHEAD * step) {
+      uint4 v[AHEAD];
 #pragma unroll
-      for (int e = 0; e < C; ++e) s[e] += v[e];
+      for (int a = 0; a < AHEAD; ++a)
+        v[a] = r + a * step < rows ? ld16(x + (size_t)(r + a * step) * N + (size_t)c * C) : uint4{0, 0, 0, 0};
+#pragma unroll
+      for (int a = 0; a < AHEAD; ++a) {
+        float f[C];
+        Chunk<T>::unpack(v[a], f);
+#pragma unroll
+        for (int e = 0; e < C; ++e) s[e] += f[e];
+      }
     }
+  }
+  if (wave > 0) {
 #pragma unroll
-    for (int e = 0; e < C; ++e) part[(size_t)blockIdx.x * N + (size_t)c * C + e] = s[e];
+    for (int e = 0; e < C; ++e) sums[wave - 1][lane][e] = s[e];
+  }
+  __syncthreads();
+  if (wave == 0 && in) {
+#pragma unroll
+    for (int e = 0; e < C; ++e) {
+      s[e] += sums[0][lane][e];
+      s[e] += sums[1][lane][e];
+      s[e] += sums[2][lane][e];
+      part[(size_t)blockIdx.x * N + (size_t)c * C + e] = s[e];
+    }
   }
 }
 
@@ -736,7 +760,10 @@ GradPlan grad_plan(int64_t T, int N, int K) {
   return p;
 }
 // Workgroups along the tokens of the bias gradient.
-int bias_parts(int64_t T) { return (int)(T < 512 ? T : 512); }
+int bias_parts(int64_t T) {
+  const int64_t p = (T + 63) / 64;
+  return (int)(p < 256 ? p : 256);
+}
 
 inline size_t up256(size_t x) { return (x + 255) & ~size_t(255); }
 
@@ -843,8 +870,8 @@ hipError_t launch_linear_backward(bool bf16, const void* dz, const void* x, cons
   }
   if (grad_bias) {
     if (plan.splits > 1) p += up256((size_t)plan.splits * N * K * sizeof(float));
-    const int parts = bias_parts(T), cols = ceil_div(N / (bf16 ? 8 : 4), 256);
-    const dim3 grid((unsigned)parts, (unsigned)(cols < 64 ? cols : 64));
+    const int parts = bias_parts(T);
+    const dim3 grid((unsigned)parts, (unsigned)ceil_div(N / (bf16 ? 8 : 4), 64));
     if (bf16) hipLaunchKernelGGL(k_column_sums<uint16_t>, grid, dim3(256), 0, st, (const uint16_t*)dz, T, N, (float*)p);
     else hipLaunchKernelGGL(k_column_sums<float>, grid, dim3(256), 0, st, (const float*)dz, T, N, (float*)p);
     launch_add_rows((const float*)p, parts, N, grad_bias, st);

@@ -235,21 +235,23 @@ __global__ __launch_bounds__(BLOCK) void k_rmsnorm_bwd(const T* dy, const T* h_i
   }
 }
 
-// grad[c] += sum over the parts of part[p, c]: 32 columns per workgroup, eight
-// groups of parts added in group order.
-__global__ __launch_bounds__(BLOCK) void k_add_rows(const float* __restrict__ part, int parts,
-                                                       int D, float* __restrict__ grad) {
-  __shared__ float red[8][32];
+// grad[c] += sum over the parts of part[p, c]: 32 columns per workgroup, 32
+// groups of parts (every 32nd) added in group order.
+__global__ __launch_bounds__(1024) void k_add_rows(const float* __restrict__ part, int parts,
+                                                   int D, float* __restrict__ grad) {
+  __shared__ float red[32][33];
   const int c = threadIdx.x & 31, g = threadIdx.x >> 5;
   const int col = blockIdx.x * 32 + c;
   float s = 0.f;
-  if (col < D)
-    for (int p = g; p < parts; p += 8) s += part[(size_t)p * D + col];
+  if (col < D) {
+#pragma unroll 8
+    for (int p = g; p < parts; p += 32) s += part[(size_t)p * D + col];
+  }
   red[g][c] = s;
   __syncthreads();
   if (g == 0 && col < D) {
 #pragma unroll
-    for (int i = 1; i < 8; ++i) s += red[i][c];
+    for (int i = 1; i < 32; ++i) s += red[i][c];
     grad[col] += s;
   }
 }
@@ -301,7 +303,7 @@ void norm_bwd_launch(const void* dy, const void* h, const void* w, const void* d
 }  // namespace
 
 void launch_add_rows(const float* part, int parts, int cols, float* out, hipStream_t st) {
-  hipLaunchKernelGGL(k_add_rows, dim3((unsigned)((cols + 31) / 32)), dim3(BLOCK), 0, st, part, parts,
+  hipLaunchKernelGGL(k_add_rows, dim3((unsigned)((cols + 31) / 32)), dim3(1024), 0, st, part, parts,
                      cols, out);
 }
 
