@@ -423,9 +423,7 @@ int mem_quantize_rows(const void* x, pkmem_dtype dt, int64_t R, int C, void* q_o
  *   z_out   [T, N] dtype y_dt: z (what mem_act_backward needs); NULL to skip it.
  *   y_out   [T, N] dtype y_dt; may be res (in place), no other input.
  *   N % 8 == 0; K % 8 == 0 (PKMEM_E4M3: K % 16 == 0); N, K <= 2^20; any T
- *   below 2^31.  All buffers 16-byte aligned.
- * Workspace: mem_linear_workspace_size(T, N, K, dt) bytes, 256-byte aligned
- * (may be 0: ws may then be NULL).  T = 0 is a valid no-op.
+ *   below 2^31.  All buffers 16-byte aligned.  T = 0 is a valid no-op.
  * ------------------------------------------------------------------------ */
 typedef enum {
   PKMEM_ACT_NONE = 0,
@@ -434,12 +432,9 @@ typedef enum {
   PKMEM_ACT_GELU = 3  /* z (1 + erf(z / sqrt 2)) / 2 */
 } pkmem_act;
 
-size_t mem_linear_workspace_size(int64_t T, int N, int K, pkmem_dtype dt);
-
 int mem_linear(const void* x, const void* w, pkmem_dtype dt, const float* x_scale,
                const float* w_scale, const void* bias, const void* res, int64_t T, int N, int K,
-               int act, void* z_out, void* y_out, pkmem_dtype y_dt, void* ws, size_t ws_bytes,
-               pkmem_stream_t stream);
+               int act, void* z_out, void* y_out, pkmem_dtype y_dt, pkmem_stream_t stream);
 
 /* Gradient of the activation, element-wise: dz_out = dy * act'(z) over [T, N]
  * dtype dt (PKMEM_F32 or PKMEM_BF16), rounded once; pass it to

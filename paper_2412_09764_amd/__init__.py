@@ -17,6 +17,7 @@ from __future__ import annotations
 import ctypes
 import functools
 import os
+import struct
 
 import torch  # noqa: F401  (first: the library binds to the HIP runtime torch loads)
 
@@ -112,9 +113,7 @@ def load() -> ctypes.CDLL:
     L.mem_rmsnorm_backward.restype = I32
     L.mem_quantize_rows.argtypes = [P, I32, I64, I32, P, P, P]
     L.mem_quantize_rows.restype = I32
-    L.mem_linear_workspace_size.argtypes = [I64, I32, I32, I32]
-    L.mem_linear_workspace_size.restype = SZ
-    L.mem_linear.argtypes = [P, P, I32, P, P, P, P, I64, I32, I32, I32, P, P, I32, P, SZ, P]
+    L.mem_linear.argtypes = [P, P, I32, P, P, P, P, I64, I32, I32, I32, P, P, I32, P]
     L.mem_linear.restype = I32
     L.mem_act_backward.argtypes = [P, P, I32, I32, I64, I32, P, P]
     L.mem_act_backward.restype = I32
@@ -580,26 +579,29 @@ def mem_bag_backward_sparse(dy: torch.Tensor, values: torch.Tensor, idx: torch.T
 
 
 # ------------------------------------------------ norm, projections, optimizer
+_current_device = torch._C._cuda_getDevice if hasattr(torch._C, "_cuda_getDevice") else None
+
+
 def _here(*ts) -> None:
     """The tensors lie, dense, on the device the call launches on."""
-    dev = None
+    dev = -2  # of no tensor
     for t in ts:
-        if t is None:
-            continue
-        if not t.is_cuda:
-            raise ValueError("tensors must be on the GPU")
-        if not t.is_contiguous():
-            raise ValueError("tensors must be contiguous")
-        if dev is None:
-            dev = t.device
-            if dev.index != torch._C._cuda_getDevice():
-                raise ValueError("tensors must be on the current device")
-        elif t.device != dev:
-            raise ValueError("tensors must be on one device")
+        if t is not None:
+            d = t.get_device()
+            if d != dev:
+                if d < 0:
+                    raise ValueError("tensors must be on the GPU")
+                if dev >= 0:
+                    raise ValueError("tensors must be on one device")
+                if d != _current_device():
+                    raise ValueError("tensors must be on the current device")
+                dev = d
+            if not t.is_contiguous():
+                raise ValueError("tensors must be contiguous")
 
 
 def _like(t, shape, dtype, what: str) -> None:
-    if t is not None and (tuple(t.shape) != tuple(shape) or t.dtype != dtype):
+    if t is not None and (t.shape != shape or t.dtype is not dtype):
         raise ValueError(f"{what} must be a {dtype} tensor of shape {tuple(shape)}")
 
 
@@ -614,24 +616,28 @@ def mem_rmsnorm(x: torch.Tensor, weight=None, residual=None, eps: float = 1e-5, 
     without a residual or with want_sum False (sum_out may be x or residual)."""
     L = load()
     _here(x, weight, residual, sum_out, y_out, scale_out)
-    T, D = x.shape
+    shape, xdt = x.shape, x.dtype
+    T, D = shape
     dt = _dt(x)
-    _like(weight, (D,), x.dtype, "weight")
-    _like(residual, (T, D), x.dtype, "residual")
+    _like(weight, (D,), xdt, "weight")
+    _like(residual, shape, xdt, "residual")
     if residual is None:
         sum_out = None
-    elif sum_out is None and want_sum:
+    elif sum_out is not None:
+        _like(sum_out, shape, xdt, "sum_out")
+    elif want_sum:
         sum_out = torch.empty_like(x)
-    _like(sum_out, (T, D), x.dtype, "sum_out")
-    ydt = torch.float8_e4m3fn if quantize else x.dtype
+    ydt = torch.float8_e4m3fn if quantize else xdt
     if y_out is None:
-        y_out = torch.empty((T, D), dtype=ydt, device=x.device)
-    _like(y_out, (T, D), ydt, "y_out")
+        y_out = torch.empty_like(x, dtype=ydt)
+    else:
+        _like(y_out, shape, ydt, "y_out")
     if not quantize:
         scale_out = None
     elif scale_out is None:
         scale_out = torch.empty((T,), dtype=torch.float32, device=x.device)
-    _like(scale_out, (T,), torch.float32, "scale_out")
+    else:
+        _like(scale_out, (T,), torch.float32, "scale_out")
     _check(L.mem_rmsnorm(_ptr(x), _ptr(residual), _ptr(weight), dt, T, D, float(eps), _ptr(sum_out),
                          _ptr(y_out), E4M3 if quantize else dt, _ptr(scale_out), _stream(stream)))
     return y_out, sum_out, scale_out
@@ -692,7 +698,7 @@ def _act(act) -> int:
 @_launches_on_stream
 def mem_linear(x: torch.Tensor, w: torch.Tensor, bias=None, *, residual=None, act="none",
                x_scale=None, w_scale=None, out_dtype=None, y_out=None, z_out=None,
-               want_z: bool = False, workspace=None, stream=None):
+               want_z: bool = False, stream=None):
     """act(x w^T + bias) + residual: x [T, K], w [N, K], bias [N], residual [T, N].
 
     act: a name of ACTIVATIONS.  float8_e4m3fn operands come with x_scale [T] and
@@ -701,11 +707,11 @@ def mem_linear(x: torch.Tensor, w: torch.Tensor, bias=None, *, residual=None, ac
     Returns (y, z) with z = x w^T + bias before the activation, None unless want_z.
     y_out may be residual."""
     L = load()
-    _here(x, w, bias, residual, x_scale, w_scale, y_out, z_out, workspace)
+    _here(x, w, bias, residual, x_scale, w_scale, y_out, z_out)
     T, K = x.shape
-    N = w.shape[0]
-    _like(w, (N, K), x.dtype, "w")
-    if x.dtype == torch.float8_e4m3fn:
+    N, xdt = w.shape[0], x.dtype
+    _like(w, (N, K), xdt, "w")
+    if xdt is torch.float8_e4m3fn:
         dt = E4M3
         if x_scale is None or w_scale is None:
             raise ValueError("float8_e4m3fn operands need x_scale and w_scale")
@@ -714,21 +720,21 @@ def mem_linear(x: torch.Tensor, w: torch.Tensor, bias=None, *, residual=None, ac
     else:
         dt = _dt(x)
     if out_dtype is None:
-        out_dtype = torch.bfloat16 if dt == E4M3 else x.dtype
+        out_dtype = torch.bfloat16 if dt == E4M3 else xdt
+    shape = (T, N)
     if y_out is None:
-        y_out = torch.empty((T, N), dtype=out_dtype, device=x.device)
-    if z_out is None and want_z:
-        z_out = torch.empty((T, N), dtype=out_dtype, device=x.device)
-    ydt = _dt(y_out)
-    _like(y_out, (T, N), out_dtype, "y_out")
-    _like(z_out, (T, N), out_dtype, "z_out")
+        y_out = x.new_empty(shape, dtype=out_dtype)
+    else:
+        _like(y_out, shape, out_dtype, "y_out")
+    if z_out is not None:
+        _like(z_out, shape, out_dtype, "z_out")
+    elif want_z:
+        z_out = x.new_empty(shape, dtype=out_dtype)
     _like(bias, (N,), out_dtype, "bias")
-    _like(residual, (T, N), out_dtype, "residual")
-    nbytes = int(L.mem_linear_workspace_size(T, N, K, dt))
-    ws = _workspace(nbytes, x.device, workspace) if nbytes else None
+    _like(residual, shape, out_dtype, "residual")
     _check(L.mem_linear(_ptr(x), _ptr(w), dt, _ptr(x_scale), _ptr(w_scale), _ptr(bias),
-                        _ptr(residual), T, N, K, _act(act), _ptr(z_out), _ptr(y_out), ydt, _ptr(ws),
-                        0 if ws is None else ws.numel() * ws.element_size(), _stream(stream)))
+                        _ptr(residual), T, N, K, _act(act), _ptr(z_out), _ptr(y_out), _dt(y_out),
+                        _stream(stream)))
     return y_out, z_out
 
 
@@ -792,6 +798,9 @@ class _AdamwTensor(ctypes.Structure):  # pkmem_adamw_tensor
     _fields_ += [(n, ctypes.c_int) for n in ("param_dt", "grad_dt", "state_dt")]
 
 
+_ADAMW_PACK = struct.Struct("6Pq3i4x")  # the same, several times faster to fill
+
+
 class _AdamwOpts(ctypes.Structure):  # pkmem_adamw_opts
     _fields_ = [(n, ctypes.c_double) for n in ("lr", "beta1", "beta2", "eps", "weight_decay")]
     _fields_ += [("step", ctypes.c_int64), ("seed", ctypes.c_uint64)]
@@ -814,27 +823,33 @@ def mem_adamw_state(param: torch.Tensor, bits: int = 32):
                       for _ in range(2)))
 
 
-_ADAMW_DT = {torch.float32: F32, torch.bfloat16: BF16, torch.float8_e4m3fn: E4M3}
+_DT = {torch.float32: F32, torch.bfloat16: BF16}
+_ADAMW_STATES = {torch.float32: F32, torch.float8_e4m3fn: E4M3}
 
 
 def _adamw_tensor(p, g, m, v, sm, sv, gshape) -> tuple:
-    n = p.numel()
-    if m.shape != p.shape or v.shape != p.shape or g.shape != gshape:
+    """The checked fields of one _AdamwTensor."""
+    _here(p, g, m, v, sm, sv)
+    shape, sdt = p.shape, m.dtype
+    if m.shape != shape or v.shape != shape or g.shape != gshape:
         raise ValueError("states must have the parameter's shape, gradients their own")
-    if m.dtype != v.dtype or m.dtype not in (torch.float32, torch.float8_e4m3fn):
+    if v.dtype is not sdt or sdt not in _ADAMW_STATES:
         raise TypeError("states must both be float32 or both float8_e4m3fn")
-    if p.dtype not in (torch.float32, torch.bfloat16) or g.dtype not in (torch.float32, torch.bfloat16):
+    if p.dtype not in _DT or g.dtype not in _DT:
         raise TypeError("parameters and gradients must be float32 or bfloat16")
-    if m.dtype == torch.float32:
+    n = p.numel()
+    if sdt is torch.float32:
         if sm is not None or sv is not None:
             raise ValueError("scales belong to float8_e4m3fn states")
+        sm = sv = 0
     else:
         blocks = -(-n // ADAMW_STATE_BLOCK)
         for s in (sm, sv):
-            if s is None or s.dtype != torch.float32 or s.numel() != blocks:
+            if s is None or s.dtype is not torch.float32 or s.numel() != blocks:
                 raise ValueError(f"float8_e4m3fn states need fp32 scales, one per {ADAMW_STATE_BLOCK} elements")
-    return (p.data_ptr(), g.data_ptr(), m.data_ptr(), v.data_ptr(), _ptr(sm), _ptr(sv), n,
-            _ADAMW_DT[p.dtype], _ADAMW_DT[g.dtype], _ADAMW_DT[m.dtype])
+        sm, sv = sm.data_ptr(), sv.data_ptr()
+    return (p.data_ptr(), g.data_ptr(), m.data_ptr(), v.data_ptr(), sm, sv, n, _DT[p.dtype],
+            _DT[g.dtype], _ADAMW_STATES[sdt])
 
 
 def _adamw_opts(lr, betas, eps, weight_decay, step, seed, grad_scale) -> _AdamwOpts:
@@ -877,10 +892,10 @@ def mem_adamw(params, grads, exp_avgs, exp_avg_sqs, *, lr, step, betas=(0.9, 0.9
     svs = none if exp_avg_sq_scales is None else exp_avg_sq_scales
     if not len(grads) == len(exp_avgs) == len(exp_avg_sqs) == len(sms) == len(svs) == n:
         raise ValueError("lists of different lengths")
-    ts = (_AdamwTensor * max(n, 1))()
+    size = _ADAMW_PACK.size
+    ts = ctypes.create_string_buffer(max(n, 1) * size)
     for i, (p, g, m, v, sm, sv) in enumerate(zip(params, grads, exp_avgs, exp_avg_sqs, sms, svs)):
-        _here(p, g, m, v, sm, sv)
-        ts[i] = _adamw_tensor(p, g, m, v, sm, sv, p.shape)
+        _ADAMW_PACK.pack_into(ts, i * size, *_adamw_tensor(p, g, m, v, sm, sv, p.shape))
     o = _adamw_opts(lr, betas, eps, weight_decay, step, seed, grad_scale)
     _check(L.mem_adamw(ctypes.addressof(ts), n, ctypes.addressof(o), _stream(stream)))
 
@@ -896,11 +911,12 @@ def mem_adamw_rows(param: torch.Tensor, rows: torch.Tensor, grad_rows: torch.Ten
     mem_bag_backward_sparse returns.  The other rows keep value and states.  Arguments
     as mem_adamw's."""
     L = load()
-    _here(param, rows, grad_rows, exp_avg, exp_avg_sq, exp_avg_scale, exp_avg_sq_scale)
     N, D = param.shape
-    U = rows.shape[0]
+    U = rows.numel()
+    _here(param, rows)
     _like(rows, (U,), torch.int64, "rows")
-    _like(grad_rows, (U, D), torch.float32, "grad_rows")
+    if grad_rows.dtype is not torch.float32:
+        raise TypeError("gradients of rows must be float32")
     t = _AdamwTensor(*_adamw_tensor(param, grad_rows, exp_avg, exp_avg_sq, exp_avg_scale,
                                     exp_avg_sq_scale, (U, D)))
     o = _adamw_opts(lr, betas, eps, weight_decay, step, seed, grad_scale)

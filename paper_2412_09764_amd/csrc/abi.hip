@@ -884,15 +884,9 @@ int check_linear_shapes(const char* fn, pkmem_dtype dt, bool e4m3, int64_t T, in
 
 extern "C" {
 
-size_t mem_linear_workspace_size(int64_t T, int N, int K, pkmem_dtype dt) {
-  if (T < 1 || N < 1 || K < 1) return 0;
-  return align256(pk::linear_ws_bytes(T, N, K, dt));
-}
-
 int mem_linear(const void* x, const void* w, pkmem_dtype dt, const float* x_scale,
                const float* w_scale, const void* bias, const void* res, int64_t T, int N, int K,
-               int act, void* z_out, void* y_out, pkmem_dtype y_dt, void* ws, size_t ws_bytes,
-               pkmem_stream_t stream) {
+               int act, void* z_out, void* y_out, pkmem_dtype y_dt, pkmem_stream_t stream) {
   const char* fn = "mem_linear";
   int rc = check_linear_shapes(fn, dt, true, T, N, K);
   if (rc) return rc;
@@ -906,12 +900,8 @@ int mem_linear(const void* x, const void* w, pkmem_dtype dt, const float* x_scal
   if (!aligned(x, 16) || !aligned(w, 16) || !aligned(x_scale, 4) || !aligned(w_scale, 16) ||
       !aligned(bias, 16) || !aligned(res, 16) || !aligned(z_out, 16) || !aligned(y_out, 16))
     return fail(PKMEM_ERR_INVALID, "%s: buffers must be 16-byte aligned", fn);
-  const size_t need = mem_linear_workspace_size(T, N, K, dt);
-  if (need > 0 && (!ws || ws_bytes < need))
-    return fail(PKMEM_ERR_WORKSPACE, "%s: workspace of %zu bytes needed, %zu given", fn, need, ws ? ws_bytes : (size_t)0);
-  if (!aligned(ws, 256)) return fail(PKMEM_ERR_INVALID, "%s: workspace must be 256-byte aligned", fn);
   if (T == 0) return PKMEM_OK;
-  const pk::LinearCall c{x, w, dt, x_scale, w_scale, bias, res, T, N, K, act, z_out, y_out, y_dt == PKMEM_BF16, ws};
+  const pk::LinearCall c{x, w, dt, x_scale, w_scale, bias, res, T, N, K, act, z_out, y_out, y_dt == PKMEM_BF16};
   return hip_status(pk::launch_linear(c, reinterpret_cast<hipStream_t>(stream)), fn);
 }
 

@@ -463,8 +463,7 @@ __global__ __launch_bounds__(WM* WN* KG * 64) void k_gemm(const GemmArgs g) {
   // in group order, each for its share of the rows.
   __syncthreads();
   constexpr int WAVES_PER_STAGE = BYTES / 16384, ROWS = 8 / KG;
-  static_assert(NJ == 2 && MI % 2 == 0 && WAVES_PER_STAGE >= 1, "64 x 64 pieces");
-  static_assert(KG == 1 || MI == 2, "one piece a wave where k is shared");
+  static_assert(NJ == 2 && MI % 2 == 0 && WAVES_PER_STAGE >= 1 && WAVES_PER_STAGE * 4 >= NW * KG, "64 x 64 pieces");
   auto piece = [&](int w) PK_INLINE {
     const int si = w / WAVES_PER_STAGE;
     return (si == 0 ? st0 : si == 1 ? st1 : si == 2 ? st2 : st3) + (w % WAVES_PER_STAGE) * 16384;
@@ -532,6 +531,7 @@ __global__ __launch_bounds__(WM* WN* KG * 64) void k_gemm(const GemmArgs g) {
         epi.store(g, at, g.a_scale ? g.a_scale[i] : 1.f, res[t], v);
       }
     }
+    if constexpr (KG > 1 && MI > 2) __syncthreads();  // the pieces are read before they are written again
   }
 }
 
@@ -702,16 +702,17 @@ __global__ __launch_bounds__(256) void k_act_bwd(const T* dy, const T* z, int64_
 
 inline int ceil_div(int64_t a, int64_t b) { return (int)((a + b - 1) / b); }
 
-// Tiles: 256 x 256 by eight waves; 128 x 128 by four, and four more for the other
-// half of k; 64 x 64 by four waves that share k.
-enum { TILE_256, TILE_128, TILE_64 };
-constexpr int tile_size(int t) { return t == TILE_256 ? 256 : t == TILE_128 ? 128 : 64; }
+// Tiles: 256 x 256 by eight waves; 128 x 128 by four, two workgroups a CU; the same
+// with four waves more for the other half of k, one workgroup a CU; 64 x 64 by
+// four waves that share k.
+enum { TILE_256, TILE_128, TILE_128_K2, TILE_64 };
+constexpr int tile_size(int t) { return t == TILE_256 ? 256 : t == TILE_64 ? 64 : 128; }
 int64_t tile_count(int t, int64_t M, int64_t N) { return (int64_t)ceil_div(M, tile_size(t)) * ceil_div(N, tile_size(t)); }
 // The largest tiles that are enough to fill the chip.
 int pick_tile(int64_t M, int64_t N) {
   if (tile_count(TILE_256, M, N) >= 200) return TILE_256;
-  if (tile_count(TILE_128, M, N) >= 128) return TILE_128;
-  return TILE_64;
+  const int64_t mid = tile_count(TILE_128, M, N);
+  return mid > 256 ? TILE_128 : mid >= 128 ? TILE_128_K2 : TILE_64;
 }
 
 template <int DT, bool AKS, bool BKS, bool GRAD>
@@ -722,6 +723,8 @@ void gemm_launch(GemmArgs g, int tile, int splits, hipStream_t st) {
   if (tile == TILE_256)
     hipLaunchKernelGGL((k_gemm<DT, AKS, BKS, GRAD, 256, 256, 2, 4, 1>), grid, dim3(512), 0, st, g);
   else if (tile == TILE_128)
+    hipLaunchKernelGGL((k_gemm<DT, AKS, BKS, GRAD, 128, 128, 2, 2, 1>), grid, dim3(256), 0, st, g);
+  else if (tile == TILE_128_K2)
     hipLaunchKernelGGL((k_gemm<DT, AKS, BKS, GRAD, 128, 128, 2, 2, 2>), grid, dim3(512), 0, st, g);
   else
     hipLaunchKernelGGL((k_gemm<DT, AKS, BKS, GRAD, 64, 64, 1, 1, 4>), grid, dim3(256), 0, st, g);
@@ -749,9 +752,10 @@ struct GradPlan {
 GradPlan grad_plan(int64_t T, int N, int K) {
   GradPlan p;
   p.tile = tile_count(TILE_256, N, K) >= 16 && T >= 4096 ? TILE_256
-           : tile_count(TILE_128, N, K) >= 32 ? TILE_128 : TILE_64;
+           : tile_count(TILE_128, N, K) >= 32 ? TILE_128_K2 : TILE_64;
   int64_t s = 256 / tile_count(p.tile, N, K);
-  const int64_t most = T / 256;
+  // a split costs a launch to add the parts up: about what 1024 tokens cost here
+  const int64_t most = T / 1024;
   if (s > most) s = most;
   if (s < 1) s = 1;
   if (s > 64) s = 64;
@@ -790,11 +794,6 @@ hipError_t launch_linear(const LinearCall& c, hipStream_t st) {
   else if (c.dt == PKMEM_E4M3) forward_launch<D_E4M3>(g, st);
   else forward_launch<D_F32>(g, st);
   return hipGetLastError();
-}
-
-size_t linear_ws_bytes(int64_t T, int N, int K, pkmem_dtype dt) {
-  (void)T; (void)N; (void)K; (void)dt;
-  return 0;
 }
 
 hipError_t launch_act_backward(bool bf16, const void* dy, const void* z, int act, int64_t n, void* dz,

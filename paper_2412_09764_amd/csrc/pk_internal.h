@@ -162,9 +162,7 @@ struct LinearCall {
   void* z;
   void* y;
   bool out_bf16;
-  void* ws;
 };
-size_t linear_ws_bytes(int64_t T, int N, int K, pkmem_dtype dt);
 hipError_t launch_linear(const LinearCall& c, hipStream_t st);
 hipError_t launch_act_backward(bool bf16, const void* dy, const void* z, int act, int64_t n, void* dz,
                                hipStream_t st);

@@ -20,8 +20,8 @@ def msg(lib):
 
 
 def linear(lib, x=FAKE, w=FAKE, dt=BF16, sx=None, sw=None, b=None, r=None, T=4, N=64, K=64, act=0, z=None, y=FAKE,
-           ydt=BF16, ws=FAKE, n=BIG):
-    return lib.mem_linear(x, w, dt, sx, sw, b, r, T, N, K, act, z, y, ydt, ws, n, None)
+           ydt=BF16):
+    return lib.mem_linear(x, w, dt, sx, sw, b, r, T, N, K, act, z, y, ydt, None)
 
 
 @pytest.mark.parametrize("kw,code,text", [
@@ -55,7 +55,6 @@ def linear(lib, x=FAKE, w=FAKE, dt=BF16, sx=None, sw=None, b=None, r=None, T=4, 
     (dict(y=FAKE + 2), INVALID, "aligned"),
     (dict(dt=E4M3, sx=FAKE + 2, sw=FAKE), INVALID, "aligned"),
     (dict(dt=E4M3, sx=FAKE, sw=FAKE + 4), INVALID, "aligned"),
-    (dict(ws=FAKE + 8), INVALID, "256-byte"),
 ])
 def test_linear_rejects(lib, kw, code, text):
     assert linear(lib, **kw) == code and text in msg(lib)
@@ -106,7 +105,6 @@ def test_noops_and_sizes(lib):
     assert linear(lib, T=0, x=None, y=None) == OK
     assert bwd(lib, T=0, dz=None) == OK
     assert bwd(lib, dx=None, gw=None, gb=None, ws=None, n=0, x=None, w=None) == OK
-    assert lib.mem_linear_workspace_size(0, 64, 64, BF16) == 0
     assert lib.mem_linear_backward_workspace_size(-1, 64, 64, BF16) == 0
     small, large = (lib.mem_linear_backward_workspace_size(t, 1024, 1024, BF16) for t in (8, 16384))
     assert 1024 * 4 <= small < large
