@@ -922,9 +922,8 @@ int mem_act_backward(const void* dy, const void* z, pkmem_dtype dt, int act, int
 }
 
 size_t mem_linear_backward_workspace_size(int64_t T, int N, int K, pkmem_dtype dt) {
-  (void)dt;
   if (T < 1 || N < 1 || K < 1) return 0;
-  return align256(pk::linear_backward_ws_bytes(T, N, K));
+  return align256(pk::linear_backward_ws_bytes(dt == PKMEM_BF16, T, N, K));
 }
 
 int mem_linear_backward(const void* dz, const void* x, const void* w, pkmem_dtype dt, int64_t T,

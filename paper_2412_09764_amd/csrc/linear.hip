@@ -63,6 +63,9 @@ struct GemmArgs {
   void* z;
   void* out;
   float* part;  // [splits, M, N] when the product is split
+  // sums of A over k (the bias gradient, where A is dz): added to bias_sum, or, when
+  // split, the parts [splits * tiles_n, M] written to it; null: none
+  float* bias_sum;
   int act;
   int out_bf16;
 };
@@ -152,6 +155,22 @@ struct Operand {
   __device__ __forceinline__ void advance() {
     base += step;
     --whole;
+  }
+  // KS: adds the stage's k to sums of 16 bytes of rows each, for this thread of
+  // THREADS that share the stage: rows chunk t % CHUNKS, k from t / CHUNKS on.
+  static constexpr int CHUNKS = ROW / 16, THREADS = NWAVE * 64, K_GROUPS = THREADS / CHUNKS;
+  __device__ __forceinline__ void add_rows(const unsigned char* lds, int t, float (&sum)[16 / E]) const {
+    const int c = t % CHUNKS;
+#pragma unroll
+    for (int k = t / CHUNKS, u = 0; u < STAGE_ROWS / K_GROUPS; ++u, k += K_GROUPS) {
+      // source_chunk is its own inverse within a row
+      const uint4 v = ld16(lds + k * ROW + source_chunk(k * CHUNKS + c) % CHUNKS * 16);
+      float f[16 / E];
+      if constexpr (DT == D_F32) Chunk<float>::unpack(v, f);
+      else Chunk<uint16_t>::unpack(v, f);
+#pragma unroll
+      for (int e = 0; e < 16 / E; ++e) sum[e] += f[e];
+    }
   }
   // Read addresses of this lane for blocks of 32 rows from row r0 on.
   template <int NB>
@@ -345,7 +364,7 @@ __global__ __launch_bounds__(WM* WN* KG * 64) void k_gemm(const GemmArgs g) {
   const int m_count = g.tiles_m - m_first < 4 ? g.tiles_m - m_first : 4;
   pid -= group * 4 * g.tiles_n;
   const int64_t i0 = (int64_t)(m_first + pid % m_count) * BM;
-  const int j0 = (pid / m_count) * BN;
+  const int tile_n = pid / m_count, j0 = tile_n * BN;
   int64_t k0 = split * g.k_split;
   int64_t k1 = k0 + g.k_split < g.K ? k0 + g.k_split : g.K;
   // this group's share of k; all groups take the same number of steps
@@ -429,6 +448,14 @@ __global__ __launch_bounds__(WM* WN* KG * 64) void k_gemm(const GemmArgs g) {
       }
     }
   };
+  // The sums over A's k: when split, the tiles along j take the stages in turn, else
+  // the first of them takes all.
+  constexpr int BIAS = AKS ? 16 / OA::E : 1;
+  float bias[BIAS];
+#pragma unroll
+  for (int e = 0; e < BIAS; ++e) bias[e] = 0.f;
+  int bias_turn = !AKS || !g.bias_sum || (!g.part && tile_n > 0) ? -1 : g.part ? tile_n : 0;
+  const int bias_every = g.part ? g.tiles_n : 1;
   // One stage: st is visible to all, half 0 of it in registers.  After the
   // barrier every wave has read st, and next has landed for all.  The reads of
   // a half are issued before the products of the half before it and return
@@ -437,6 +464,13 @@ __global__ __launch_bounds__(WM* WN* KG * 64) void k_gemm(const GemmArgs g) {
     read(st, 1);
     __builtin_amdgcn_sched_barrier(0);
     products(0, false, st);
+    if constexpr (AKS) {
+      if (bias_turn == 0) {
+        oa.add_rows(st + group_at, wave * 64 + lane, bias);
+        bias_turn = bias_every;
+      }
+      if (bias_turn > 0) --bias_turn;
+    }
     wait_and_meet<2 * L>();
     read(next, 0);
     __builtin_amdgcn_sched_barrier(0);
@@ -468,6 +502,25 @@ __global__ __launch_bounds__(WM* WN* KG * 64) void k_gemm(const GemmArgs g) {
     const int si = w / WAVES_PER_STAGE;
     return (si == 0 ? st0 : si == 1 ? st1 : si == 2 ? st2 : st3) + (w % WAVES_PER_STAGE) * 16384;
   };
+  if constexpr (AKS) {
+    if (g.bias_sum && (g.part || tile_n == 0)) {  // the threads' sums in the order of their k
+      float* all = reinterpret_cast<float*>(st0);
+      constexpr int GROUPS = KG * OA::K_GROUPS;
+      static_assert(GROUPS * BM * 4 <= BYTES, "the sums of a workgroup fit a stage");
+      const int t = wave * 64 + lane, at = (kg * OA::K_GROUPS + t / OA::CHUNKS) * BM + t % OA::CHUNKS * BIAS;
+#pragma unroll
+      for (int e = 0; e < BIAS; ++e) all[at + e] = bias[e];
+      __syncthreads();
+      const int r = threadIdx.x;
+      if (r < BM && i0 + r < g.M) {
+        float v = 0.f;
+        for (int q = 0; q < GROUPS; ++q) v += all[q * BM + r];
+        if (g.part) g.bias_sum[(size_t)(split * g.tiles_n + tile_n) * g.M + i0 + r] = v;
+        else g.bias_sum[i0 + r] += v;
+      }
+      __syncthreads();
+    }
+  }
   unsigned char* buf = piece(kg * NW + wave);
   const int il = lane & 31, kh = lane >> 5, rr = lane >> 3, cc = lane & 7;
   const int j = j0 + wj + 8 * cc;
@@ -621,12 +674,25 @@ __global__ __launch_bounds__(FEW_WAVES * 64) void k_gemm_few(const GemmArgs g) {
   epi.store(g, at, g.a_scale ? g.a_scale[i] : 1.f, res, v);
 }
 
-// out += part[0] + part[1] + ... in this order, 4 elements a thread.
+// out += part[0] + part[1] + ... in this order, 4 elements a thread; the last
+// workgroups do the same for the bias (one column a thread, `rows` parts).
 __global__ __launch_bounds__(256) void k_add_parts(const float* __restrict__ part, int splits,
-                                                   size_t n, float* __restrict__ out) {
+                                                   size_t n, float* __restrict__ out,
+                                                   unsigned blocks, const float* __restrict__ bias_part,
+                                                   int rows, int cols, float* __restrict__ bias) {
+  if (blockIdx.x >= blocks) {
+    const int c = (blockIdx.x - blocks) * 256 + threadIdx.x;
+    if (c >= cols) return;
+    float s = 0.f;
+#pragma unroll 8
+    for (int p = 0; p < rows; ++p) s += bias_part[(size_t)p * cols + c];
+    bias[c] += s;
+    return;
+  }
   const size_t at = ((size_t)blockIdx.x * 256 + threadIdx.x) * 4;
   if (at >= n) return;
   float s[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
   for (int p = 0; p < splits; ++p) {
     float v[4];
     load4(part, p * n + at, v);
@@ -743,25 +809,38 @@ void forward_launch(const GemmArgs& g, hipStream_t st) {
   else gemm_launch<DT, false, false, false>(g, pick_tile(g.M, g.N), 1, st);
 }
 
-// grad_W [N, K] from T tokens: tiles of its own shape, the tokens split so that
-// the workgroups fill the chip; at least 512 tokens a split.
+// grad_W [N, K] from T tokens: the tile and the number of splits of the tokens
+// with the least time by these measured parts: a stage of 64 bytes of k takes a
+// workgroup 0.85 us (256 wide), 0.35 (128, two groups) or 0.11 (64, four groups) in
+// bf16 and 3.9, 0.95, 0.24 in fp32, whose matrix rate is a sixteenth for twice the
+// bytes; a workgroup's start and end 5 us; splitting a launch of 5 us, and
+// writing and reading the parts at 5 TB/s.
 struct GradPlan {
   int tile, splits;
   int64_t k_split;
 };
-GradPlan grad_plan(int64_t T, int N, int K) {
-  GradPlan p;
-  p.tile = tile_count(TILE_256, N, K) >= 16 && T >= 4096 ? TILE_256
-           : tile_count(TILE_128, N, K) >= 32 ? TILE_128_K2 : TILE_64;
-  int64_t s = 256 / tile_count(p.tile, N, K);
-  // a split costs a launch to add the parts up: about what 1024 tokens cost here
-  const int64_t most = T / 1024;
-  if (s > most) s = most;
-  if (s < 1) s = 1;
-  if (s > 64) s = 64;
-  p.k_split = ((T + s - 1) / s + 63) / 64 * 64;
-  p.splits = T > 0 ? ceil_div(T, p.k_split) : 1;
-  return p;
+GradPlan grad_plan(bool bf16, int64_t T, int N, int K) {
+  constexpr int tiles[3] = {TILE_256, TILE_128_K2, TILE_64};
+  constexpr double stage_us[2][3] = {{3.9, 0.95, 0.24}, {0.85, 0.35, 0.11}};
+  const int64_t per_stage = bf16 ? 32 : 16;
+  GradPlan best{TILE_64, 1, T};
+  double least = 1e30;
+  for (int c = 0; c < 3; ++c) {
+    const int64_t count = tile_count(tiles[c], N, K);
+    for (int s = 1; s <= 64; s *= 2) {
+      const int64_t k_split = ((T + s - 1) / s + 63) / 64 * 64;
+      const int splits = T > 0 ? ceil_div(T, k_split) : 1;
+      if (splits < s && s > 1) break;
+      const double rounds = (double)ceil_div(count * splits, 256);
+      const double us = rounds * (5.0 + stage_us[bf16][c] * ceil_div(k_split, per_stage)) +
+                        (splits > 1 ? 5.0 + 8e-6 * splits * N * K / 5.0 : 0.0);
+      if (us < least) {
+        least = us;
+        best = GradPlan{tiles[c], splits, k_split};
+      }
+    }
+  }
+  return best;
 }
 // Workgroups along the tokens of the bias gradient.
 int bias_parts(int64_t T) {
@@ -822,10 +901,12 @@ hipError_t launch_act_backward(bool bf16, const void* dy, const void* z, int act
   return hipGetLastError();
 }
 
-size_t linear_backward_ws_bytes(int64_t T, int N, int K) {
-  const GradPlan p = grad_plan(T, N, K);
+size_t linear_backward_ws_bytes(bool bf16, int64_t T, int N, int K) {
+  const GradPlan p = grad_plan(bf16, T, N, K);
+  const int64_t rows = (int64_t)p.splits * ceil_div(K, tile_size(p.tile));  // of the bias, beside the weights
+  const int64_t alone = bias_parts(T);
   return (p.splits > 1 ? up256((size_t)p.splits * N * K * sizeof(float)) : 0) +
-         up256((size_t)bias_parts(T) * N * sizeof(float));
+         up256((size_t)(rows > alone ? rows : alone) * N * sizeof(float));
 }
 
 hipError_t launch_linear_backward(bool bf16, const void* dz, const void* x, const void* w, int64_t T,
@@ -847,9 +928,9 @@ hipError_t launch_linear_backward(bool bf16, const void* dz, const void* x, cons
     if (bf16) gemm_launch<D_BF16, false, true, false>(g, tile, 1, st);
     else gemm_launch<D_F32, false, true, false>(g, tile, 1, st);
   }
-  char* p = (char*)ws;
-  const GradPlan plan = grad_plan(T, N, K);
   if (grad_w) {
+    const GradPlan plan = grad_plan(bf16, T, N, K);
+    const size_t n = (size_t)N * K;
     GemmArgs g{};
     g.a = dz;
     g.b = x;
@@ -858,22 +939,26 @@ hipError_t launch_linear_backward(bool bf16, const void* dz, const void* x, cons
     g.K = T;
     g.k_split = plan.k_split;
     g.out = grad_w;
-    g.part = plan.splits > 1 ? (float*)p : nullptr;
+    g.bias_sum = grad_bias;
+    if (plan.splits > 1) {
+      g.part = (float*)ws;
+      if (grad_bias) g.bias_sum = (float*)((char*)ws + up256((size_t)plan.splits * n * sizeof(float)));
+    }
     if (bf16) gemm_launch<D_BF16, true, true, true>(g, plan.tile, plan.splits, st);
     else gemm_launch<D_F32, true, true, true>(g, plan.tile, plan.splits, st);
     if (plan.splits > 1) {
-      const size_t n = (size_t)N * K;
-      hipLaunchKernelGGL(k_add_parts, dim3((unsigned)((n / 4 + 255) / 256)), dim3(256), 0, st, g.part,
-                         plan.splits, n, grad_w);
+      const unsigned blocks = (unsigned)((n / 4 + 255) / 256);
+      const unsigned more = grad_bias ? (unsigned)ceil_div(N, 256) : 0;
+      hipLaunchKernelGGL(k_add_parts, dim3(blocks + more), dim3(256), 0, st, g.part, plan.splits, n, grad_w,
+                         blocks, g.bias_sum, plan.splits * ceil_div(K, tile_size(plan.tile)), N, grad_bias);
     }
-  }
-  if (grad_bias) {
-    if (plan.splits > 1) p += up256((size_t)plan.splits * N * K * sizeof(float));
+  } else if (grad_bias) {
     const int parts = bias_parts(T);
     const dim3 grid((unsigned)parts, (unsigned)ceil_div(N / (bf16 ? 8 : 4), 64));
-    if (bf16) hipLaunchKernelGGL(k_column_sums<uint16_t>, grid, dim3(256), 0, st, (const uint16_t*)dz, T, N, (float*)p);
-    else hipLaunchKernelGGL(k_column_sums<float>, grid, dim3(256), 0, st, (const float*)dz, T, N, (float*)p);
-    launch_add_rows((const float*)p, parts, N, grad_bias, st);
+    float* p = (float*)ws;
+    if (bf16) hipLaunchKernelGGL(k_column_sums<uint16_t>, grid, dim3(256), 0, st, (const uint16_t*)dz, T, N, p);
+    else hipLaunchKernelGGL(k_column_sums<float>, grid, dim3(256), 0, st, (const float*)dz, T, N, p);
+    launch_add_rows(p, parts, N, grad_bias, st);
   }
   return hipGetLastError();
 }

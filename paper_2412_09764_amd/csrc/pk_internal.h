@@ -166,7 +166,7 @@ struct LinearCall {
 hipError_t launch_linear(const LinearCall& c, hipStream_t st);
 hipError_t launch_act_backward(bool bf16, const void* dy, const void* z, int act, int64_t n, void* dz,
                                hipStream_t st);
-size_t linear_backward_ws_bytes(int64_t T, int N, int K);
+size_t linear_backward_ws_bytes(bool bf16, int64_t T, int N, int K);
 // add, dx, grad_w and grad_bias nullable.
 hipError_t launch_linear_backward(bool bf16, const void* dz, const void* x, const void* w, int64_t T,
                                   int N, int K, const void* add, void* dx, float* grad_w,

@@ -137,14 +137,19 @@ def test_backward(gpu_lib, T, N, K, dt):
     assert torch.all((dx.double() - want).abs() <= N * U * size + HALF[dt] * want.abs())
     at, bt = a.t().contiguous(), b.t().contiguous()
     assert torch.all((gw.double() - exact_mm(at, bt)).abs() <= (T + 70) * U * exact_mm(at.abs(), bt.abs()))
-    assert torch.all((gb.double() - a.double().sum(0)).abs() <= (T / 512 + 80) * U * a.double().abs().sum(0))
+    # a thread adds at most T / 16 of the rows, a workgroup 32 threads, the call 64 splits of 9 tiles
+    assert torch.all((gb.double() - a.double().sum(0)).abs() <= (T / 16 + 700) * U * a.double().abs().sum(0))
     for _ in range(3):
         again = pk.mem_linear_backward(dz, x, w)
         assert torch.equal(again[0], dx) and torch.equal(again[1], gw) and torch.equal(again[2], gb)
     for want in ((True, False, False), (False, True, False), (False, False, True)):
         some = pk.mem_linear_backward(dz, x, w, want_dx=want[0], want_grad_w=want[1], want_grad_bias=want[2])
         for got, ref, on in zip(some, (dx, gw, gb), want):
-            assert (got is None) != on and (got is None or torch.equal(got, ref))
+            assert (got is None) != on
+            if on and ref is gb:  # alone it is summed in another order
+                assert torch.all((got.double() - a.double().sum(0)).abs() <= (T / 512 + 80) * U * a.double().abs().sum(0))
+            elif on:
+                assert torch.equal(got, ref)
 
 
 @pytest.mark.parametrize("act", ["relu", "silu", "gelu"])
