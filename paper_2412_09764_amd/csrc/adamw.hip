@@ -87,22 +87,25 @@ __device__ __forceinline__ uint32_t random_bits(uint64_t at, uint32_t key) {
 __device__ __forceinline__ bool finite(float x) { return fabsf(x) <= 3.402823466e38f; }
 
 // bf16 bits of p, up with the probability of the part cut off (12 bits of h).
+// An infinity stays one (its mantissa is 0).
 __device__ __forceinline__ uint32_t round_bf16(float p, uint32_t h) {
-  if (!finite(p)) return to_bf16x2(p, p) & 0xFFFFu;
-  return (__float_as_uint(p) + (((h & 0xFFFu) << 4) | 8u)) >> 16;
+  const uint32_t up = (__float_as_uint(p) + (((h & 0xFFFu) << 4) | 8u)) >> 16;
+  return p == p ? up : 0x7FC0u;
 }
-// |x| / scale on the e4m3 grid, up with the probability of the part cut off:
+// x / scale on the e4m3 grid, up with the probability of the part cut off:
 // `more` holds random bits below the third mantissa bit.  Below 2^-6 the grid
-// is even (2^-9): an offset of 2^-6 gives those numbers the same mantissa.
-__device__ __forceinline__ float round_e4m3(float x, float inv, uint32_t more, bool nonzero) {
-  const float a = fabsf(x * inv);
-  const bool low = a < 0x1p-6f;
-  float b = low ? a + 0x1p-6f : a;
-  b = __uint_as_float((__float_as_uint(b) + more) & 0xFFF00000u);
-  b = low ? b - 0x1p-6f : b;
-  b = b < E4M3_MAX ? b : E4M3_MAX;
-  if (nonzero) b = (a > 0.f && b == 0.f) ? 0x1p-9f : b;
-  return finite(x) ? copysignf(b, x) : __uint_as_float(0x7FC00000u);
+// is even (2^-9): an offset of 2^-6 gives those numbers the same mantissa.  The
+// largest value of a block comes out at 448 and at most 4 units in the last
+// place above, too few to carry past it with any `more`.
+// ROOT: x >= 0, and a value above 0 stays above 0.
+template <bool ROOT>
+__device__ __forceinline__ float round_e4m3(float x, float inv, uint32_t more) {
+  const float a = ROOT ? x * inv : fabsf(x * inv);
+  const float low = a < 0x1p-6f ? 0x1p-6f : 0.f;
+  float b = __uint_as_float((__float_as_uint(a + low) + more) & 0xFFF00000u) - low;
+  if constexpr (ROOT) b = fmaxf(b, a > 0.f ? 0x1p-9f : 0.f);
+  else b = copysignf(b, x);
+  return finite(x) ? b : __uint_as_float(0x7FC00000u);
 }
 __device__ __forceinline__ float unit_max(float v) {
   v = fmaxf(v, __uint_as_float(xor_lane<1>(__float_as_uint(v))));
@@ -111,12 +114,20 @@ __device__ __forceinline__ float unit_max(float v) {
   return fmaxf(v, __uint_as_float(xor_lane<8>(__float_as_uint(v))));
 }
 // A block's scale: its largest finite value over 448, 0 below 2^-126 (then
-// every code is 0), and the factor into the grid.
+// every code is 0), and the factor into the grid.  fmaxf passes over a NaN; an
+// infinity sends the block through a second look at finite values alone.
 __device__ __forceinline__ float unit_scale(const float (&x)[LANE_ELEMS], float& inv) {
   float am = 0.f;
 #pragma unroll
-  for (int i = 0; i < LANE_ELEMS; ++i) am = fmaxf(am, finite(x[i]) ? fabsf(x[i]) : 0.f);
-  float s = unit_max(am) * (1.f / E4M3_MAX);
+  for (int i = 0; i < LANE_ELEMS; ++i) am = fmaxf(am, fabsf(x[i]));
+  am = unit_max(am);
+  if (__builtin_expect(!finite(am), 0)) {
+    am = 0.f;
+#pragma unroll
+    for (int i = 0; i < LANE_ELEMS; ++i) am = fmaxf(am, finite(x[i]) ? fabsf(x[i]) : 0.f);
+    am = unit_max(am);
+  }
+  float s = am * (1.f / E4M3_MAX);
   s = s < 0x1p-126f ? 0.f : s;
   inv = s > 0.f ? 1.f / s : 0.f;
   return s;
@@ -236,8 +247,8 @@ __device__ __forceinline__ void step8(const Tensor& t, const AdamwScalars& c, ui
     }
 #pragma unroll
     for (int i = 0; i < LANE_ELEMS; ++i) {
-      m[i] = round_e4m3(m[i], im, ((h[i] >> 24) << 12) | (1u << 11), false);
-      r[i] = round_e4m3(r[i], ir, ((h[i] >> 12 & 0xFFFu) << 8) | (1u << 7), true);
+      m[i] = round_e4m3<false>(m[i], im, ((h[i] >> 12) & 0xFF000u) | (1u << 11));
+      r[i] = round_e4m3<true>(r[i], ir, ((h[i] >> 4) & 0xFFF00u) | (1u << 7));
     }
     store_codes((uint8_t*)t.m + off, whole, count, m);
     store_codes((uint8_t*)t.v + off, whole, count, r);
