@@ -70,18 +70,14 @@ struct GemmArgs {
   int out_bf16;
 };
 
-template <int DT>
-__device__ __forceinline__ void mma(uint4 b, uint4 a, f32x16_t& c) {
-  if constexpr (DT == D_BF16) {
-    c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, b),
-                                                __builtin_bit_cast(bf16x8_t, a), c, 0, 0, 0);
-  } else {
-    c = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(b.x), __uint_as_float(a.x), c, 0, 0, 0);
-    c = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(b.y), __uint_as_float(a.y), c, 0, 0, 0);
-    c = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(b.z), __uint_as_float(a.z), c, 0, 0, 0);
-    c = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(b.w), __uint_as_float(a.w), c, 0, 0, 0);
-  }
+__device__ __forceinline__ void mma_bf16(uint4 b, uint4 a, f32x16_t& c) {
+  c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, b),
+                                              __builtin_bit_cast(bf16x8_t, a), c, 0, 0, 0);
 }
+__device__ __forceinline__ void mma_f32(uint32_t b, uint32_t a, f32x16_t& c) {
+  c = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(b), __uint_as_float(a), c, 0, 0, 0);
+}
+__device__ __forceinline__ uint32_t word(uint4 v, int i) { return i == 0 ? v.x : i == 1 ? v.y : i == 2 ? v.z : v.w; }
 // 8 e4m3 codes as bf16 (exact).  The 8-bit matrix instructions align the products
 // of each 8 k to the largest of them and keep 13 bits below it; a sum in fp32 takes
 // the bf16 instruction.  (Measured: beside a product of 2^16 one of 2^2 is lost.)
@@ -406,11 +402,6 @@ __global__ __launch_bounds__(WM* WN* KG * 64) void k_gemm(const GemmArgs g) {
     for (int i = 0; i < L; ++i) load(st, i);
     advance();
   };
-  fill(st0);
-  fill(st1);
-  fill(st2);
-  fill(st3);
-  wait_and_meet<3 * L>();
   // Fragments of the halves 0 and 1 of a stage.
   uint4 fa[2][MI], fb[2][NJ];
   auto read = [&](const unsigned char* st, int h) PK_INLINE {
@@ -419,26 +410,31 @@ __global__ __launch_bounds__(WM* WN* KG * 64) void k_gemm(const GemmArgs g) {
 #pragma unroll
     for (int mi = 0; mi < MI; ++mi) fa[h][mi] = oa.frag(st + group_at, mi, h);
   };
-  // The products of half h, by blocks of A's rows; between them, where asked for,
-  // the loads of a stage into st.
+  // The products of half h, in MI (fp32: 4, e4m3: 2 MI) groups of different sums;
+  // between them, where asked for, the loads of a stage into st.
+  constexpr int GROUPS = DT == D_E4M3 ? 2 * MI : DT == D_F32 ? 4 : MI;
   auto products = [&](int h, bool refill, unsigned char* st) PK_INLINE {
-    constexpr int GROUPS = DT == D_E4M3 ? 2 * MI : MI;
     uint4 b[NJ];
 #pragma unroll
     for (int q = 0; q < GROUPS; ++q) {
-      const int mi = q % MI;
       if constexpr (DT == D_E4M3) {
+        const int mi = q % MI;
         if (mi == 0) {
 #pragma unroll
           for (int nj = 0; nj < NJ; ++nj)
-            b[nj] = q ? widen8(fb[h][nj].z, fb[h][nj].w) : widen8(fb[h][nj].x, fb[h][nj].y);
+            b[nj] = q >= MI ? widen8(fb[h][nj].z, fb[h][nj].w) : widen8(fb[h][nj].x, fb[h][nj].y);
         }
         const uint4 a = q >= MI ? widen8(fa[h][mi].z, fa[h][mi].w) : widen8(fa[h][mi].x, fa[h][mi].y);
 #pragma unroll
-        for (int nj = 0; nj < NJ; ++nj) mma<D_BF16>(b[nj], a, acc[mi][nj]);
+        for (int nj = 0; nj < NJ; ++nj) mma_bf16(b[nj], a, acc[mi][nj]);
+      } else if constexpr (DT == D_F32) {
+#pragma unroll
+        for (int mi = 0; mi < MI; ++mi)
+#pragma unroll
+          for (int nj = 0; nj < NJ; ++nj) mma_f32(word(fb[h][nj], q), word(fa[h][mi], q), acc[mi][nj]);
       } else {
 #pragma unroll
-        for (int nj = 0; nj < NJ; ++nj) mma<DT>(fb[h][nj], fa[h][mi], acc[mi][nj]);
+        for (int nj = 0; nj < NJ; ++nj) mma_bf16(fb[h][nj], fa[h][q], acc[q][nj]);
       }
       if (refill) {
         __builtin_amdgcn_sched_barrier(0);
@@ -456,14 +452,7 @@ __global__ __launch_bounds__(WM* WN* KG * 64) void k_gemm(const GemmArgs g) {
   for (int e = 0; e < BIAS; ++e) bias[e] = 0.f;
   int bias_turn = !AKS || !g.bias_sum || (!g.part && tile_n > 0) ? -1 : g.part ? tile_n : 0;
   const int bias_every = g.part ? g.tiles_n : 1;
-  // One stage: st is visible to all, half 0 of it in registers.  After the
-  // barrier every wave has read st, and next has landed for all.  The reads of
-  // a half are issued before the products of the half before it and return
-  // while these run.
-  auto stage = [&](unsigned char* st, const unsigned char* next) PK_INLINE {
-    read(st, 1);
-    __builtin_amdgcn_sched_barrier(0);
-    products(0, false, st);
+  auto add_bias = [&](const unsigned char* st) PK_INLINE {
     if constexpr (AKS) {
       if (bias_turn == 0) {
         oa.add_rows(st + group_at, wave * 64 + lane, bias);
@@ -471,23 +460,102 @@ __global__ __launch_bounds__(WM* WN* KG * 64) void k_gemm(const GemmArgs g) {
       }
       if (bias_turn > 0) --bias_turn;
     }
-    wait_and_meet<2 * L>();
-    read(next, 0);
-    __builtin_amdgcn_sched_barrier(0);
-    products(1, true, st);
-    advance();
   };
-  read(st0, 0);
-  int s = 0;
-  for (; s + 4 <= steps; s += 4) {
-    stage(st0, st1);
-    stage(st1, st2);
-    stage(st2, st3);
-    stage(st3, st0);
+  if constexpr (NW * KG == 8 && DT != D_F32) {
+    // Two waves share a SIMD, one of the first four and one of the last: while one
+    // of them multiplies a stage the other reads its next one and issues the loads,
+    // and they change places at a barrier, so the matrix cores always have a
+    // wave with all its operands in registers.  Stage s: the first four multiply,
+    // the last four read it; then the first four read stage s + 1 and refill s.
+    auto multiply = [&]() PK_INLINE {
+      __builtin_amdgcn_s_setprio(1);
+      products(0, false, st0);
+      products(1, false, st0);
+      __builtin_amdgcn_s_setprio(0);
+    };
+    auto read_all = [&](const unsigned char* st) PK_INLINE {
+      read(st, 0);
+      read(st, 1);
+      add_bias(st);
+    };
+    auto first = [&](unsigned char* st, const unsigned char* next) PK_INLINE {
+      multiply();
+      wait_and_meet<2 * L>();  // the next stage has landed
+      read_all(next);
+      fill(st);
+      wait_and_meet<63>();  // 63: for LDS alone
+    };
+    auto last = [&](unsigned char* st, unsigned char* before) PK_INLINE {
+      read_all(st);
+      fill(before);
+      wait_and_meet<2 * L>();
+      multiply();
+      wait_and_meet<63>();
+    };
+    fill(st0);
+    fill(st1);
+    fill(st2);
+    int s = 0;
+    if (w < 4) {
+      fill(st3);
+      wait_and_meet<3 * L>();
+      read_all(st0);
+      for (; s + 4 <= steps; s += 4) {
+        first(st0, st1);
+        first(st1, st2);
+        first(st2, st3);
+        first(st3, st0);
+      }
+      if (s < steps) first(st0, st1);
+      if (s + 1 < steps) first(st1, st2);
+      if (s + 2 < steps) first(st2, st3);
+    } else {
+      wait_and_meet<2 * L>();
+      for (; s + 4 <= steps; s += 4) {
+        last(st0, st3);
+        last(st1, st0);
+        last(st2, st1);
+        last(st3, st2);
+      }
+      if (s < steps) last(st0, st3);
+      if (s + 1 < steps) last(st1, st0);
+      if (s + 2 < steps) last(st2, st1);
+    }
+  } else {
+    // One wave a SIMD, or fp32, where the products take so long that waves that
+    // multiply at once hide all else (32768 x 2048 x 2048: 1943 against 2056 us in turns).
+    // One stage: st is visible to all, half 0 of it in registers.  After the
+    // barrier every wave has read st, and next has landed for all.  The reads of
+    // a half are issued before the products of the half before it and return
+    // while these run.
+    auto stage = [&](unsigned char* st, const unsigned char* next) PK_INLINE {
+      read(st, 1);
+      __builtin_amdgcn_sched_barrier(0);
+      products(0, false, st);
+      add_bias(st);
+      wait_and_meet<2 * L>();
+      read(next, 0);
+      __builtin_amdgcn_sched_barrier(0);
+      products(1, true, st);
+      advance();
+    };
+    fill(st0);
+    fill(st1);
+    fill(st2);
+    fill(st3);
+    wait_and_meet<3 * L>();
+    read(st0, 0);
+    int s = 0;
+    for (; s + 4 <= steps; s += 4) {
+      stage(st0, st1);
+      stage(st1, st2);
+      stage(st2, st3);
+      stage(st3, st0);
+    }
+    if (s < steps) stage(st0, st1);
+    if (s + 1 < steps) stage(st1, st2);
+    if (s + 2 < steps) stage(st2, st3);
   }
-  if (s < steps) stage(st0, st1);
-  if (s + 1 < steps) stage(st1, st2);
-  if (s + 2 < steps) stage(st2, st3);
   wait_loads<0>();  // no load may reach LDS after the workgroup has left it
 
   // The sums leave through LDS, 64 rows of a wave's 64 columns at a time (16 KiB a
@@ -788,12 +856,12 @@ void gemm_launch(GemmArgs g, int tile, int splits, hipStream_t st) {
   const dim3 grid((unsigned)(g.tiles_m * g.tiles_n * splits));
   if (tile == TILE_256)
     hipLaunchKernelGGL((k_gemm<DT, AKS, BKS, GRAD, 256, 256, 2, 4, 1>), grid, dim3(512), 0, st, g);
-  else if (tile == TILE_128)
-    hipLaunchKernelGGL((k_gemm<DT, AKS, BKS, GRAD, 128, 128, 2, 2, 1>), grid, dim3(256), 0, st, g);
   else if (tile == TILE_128_K2)
     hipLaunchKernelGGL((k_gemm<DT, AKS, BKS, GRAD, 128, 128, 2, 2, 2>), grid, dim3(512), 0, st, g);
-  else
+  else if (tile == TILE_64)
     hipLaunchKernelGGL((k_gemm<DT, AKS, BKS, GRAD, 64, 64, 1, 1, 4>), grid, dim3(256), 0, st, g);
+  else if constexpr (!GRAD)  // the weight gradient splits k instead
+    hipLaunchKernelGGL((k_gemm<DT, AKS, BKS, GRAD, 128, 128, 2, 2, 1>), grid, dim3(256), 0, st, g);
 }
 template <int DT>
 void few_launch(const GemmArgs& g, hipStream_t st) {
