@@ -145,9 +145,10 @@ def _check(rc: int) -> None:
 
 
 def _dt(t: torch.Tensor) -> int:
-    if t.dtype == torch.float32:
+    dt = t.dtype
+    if dt is torch.float32:
         return F32
-    if t.dtype == torch.bfloat16:
+    if dt is torch.bfloat16:
         return BF16
     raise TypeError(f"unsupported dtype {t.dtype} (float32 or bfloat16)")
 
@@ -169,10 +170,14 @@ def _ptr(t):
 # and torch's stream object alone takes 4 us a call, so the handle is asked for
 # directly (torch has no public call for the handle alone), and the stream
 # context is entered only where a stream is given.
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+_current_device = getattr(torch._C, "_cuda_getDevice", None)
+
+
 def _stream(stream) -> int:
     if stream is not None:
         return stream.cuda_stream
-    return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
+    return _raw_stream(_current_device())
 
 
 def _launches_on_stream(fn):
@@ -181,11 +186,12 @@ def _launches_on_stream(fn):
     then belong to the stream the library launches on, and the fills are
     ordered before the launch on that stream."""
     @functools.wraps(fn)
-    def wrapper(*args, stream=None, **kw):
+    def wrapper(*args, **kw):
+        stream = kw.get("stream")
         if stream is None:
             return fn(*args, **kw)
         with torch.cuda.stream(stream):
-            return fn(*args, stream=stream, **kw)
+            return fn(*args, **kw)
     return wrapper
 
 
@@ -579,9 +585,6 @@ def mem_bag_backward_sparse(dy: torch.Tensor, values: torch.Tensor, idx: torch.T
 
 
 # ------------------------------------------------ norm, projections, optimizer
-_current_device = torch._C._cuda_getDevice if hasattr(torch._C, "_cuda_getDevice") else None
-
-
 def _here(*ts) -> None:
     """The tensors lie, dense, on the device the call launches on."""
     dev = -2  # of no tensor
@@ -614,32 +617,39 @@ def mem_rmsnorm(x: torch.Tensor, weight=None, residual=None, eps: float = 1e-5, 
     Returns (y, h, scale): y in x's dtype and scale None, or with quantize y in
     float8_e4m3fn with scale fp32 [T] (the norm is about y * scale[:, None]); h None
     without a residual or with want_sum False (sum_out may be x or residual)."""
-    L = load()
     _here(x, weight, residual, sum_out, y_out, scale_out)
     shape, xdt = x.shape, x.dtype
     T, D = shape
-    dt = _dt(x)
-    _like(weight, (D,), xdt, "weight")
-    _like(residual, shape, xdt, "residual")
+    dt = ydt = _dt(x)
+    wp = rp = hp = sp = None
+    if weight is not None:
+        _like(weight, (D,), xdt, "weight")
+        wp = weight.data_ptr()
     if residual is None:
         sum_out = None
-    elif sum_out is not None:
-        _like(sum_out, shape, xdt, "sum_out")
-    elif want_sum:
-        sum_out = torch.empty_like(x)
-    ydt = torch.float8_e4m3fn if quantize else xdt
-    if y_out is None:
-        y_out = torch.empty_like(x, dtype=ydt)
     else:
-        _like(y_out, shape, ydt, "y_out")
+        _like(residual, shape, xdt, "residual")
+        rp = residual.data_ptr()
+        if sum_out is not None:
+            _like(sum_out, shape, xdt, "sum_out")
+        elif want_sum:
+            sum_out = torch.empty_like(x)
+        hp = _ptr(sum_out)
     if not quantize:
         scale_out = None
-    elif scale_out is None:
-        scale_out = torch.empty((T,), dtype=torch.float32, device=x.device)
     else:
-        _like(scale_out, (T,), torch.float32, "scale_out")
-    _check(L.mem_rmsnorm(_ptr(x), _ptr(residual), _ptr(weight), dt, T, D, float(eps), _ptr(sum_out),
-                         _ptr(y_out), E4M3 if quantize else dt, _ptr(scale_out), _stream(stream)))
+        xdt, ydt = torch.float8_e4m3fn, E4M3
+        if scale_out is None:
+            scale_out = torch.empty((T,), dtype=torch.float32, device=x.device)
+        else:
+            _like(scale_out, (T,), torch.float32, "scale_out")
+        sp = scale_out.data_ptr()
+    if y_out is None:
+        y_out = torch.empty_like(x, dtype=xdt) if quantize else torch.empty_like(x)
+    else:
+        _like(y_out, shape, xdt, "y_out")
+    _check((_LIB or load()).mem_rmsnorm(x.data_ptr(), rp, wp, dt, T, D, eps, hp, y_out.data_ptr(), ydt,
+                                        sp, _stream(stream)))
     return y_out, sum_out, scale_out
 
 
@@ -706,19 +716,21 @@ def mem_linear(x: torch.Tensor, w: torch.Tensor, bias=None, *, residual=None, ac
     bfloat16 (default: x's, bfloat16 for 8 bits), the dtype of bias and residual too.
     Returns (y, z) with z = x w^T + bias before the activation, None unless want_z.
     y_out may be residual."""
-    L = load()
     _here(x, w, bias, residual, x_scale, w_scale, y_out, z_out)
     T, K = x.shape
     N, xdt = w.shape[0], x.dtype
     _like(w, (N, K), xdt, "w")
+    sx = sw = bp = rp = zp = None
     if xdt is torch.float8_e4m3fn:
         dt = E4M3
         if x_scale is None or w_scale is None:
             raise ValueError("float8_e4m3fn operands need x_scale and w_scale")
         _like(x_scale, (T,), torch.float32, "x_scale")
         _like(w_scale, (N,), torch.float32, "w_scale")
+        sx, sw = x_scale.data_ptr(), w_scale.data_ptr()
     else:
         dt = _dt(x)
+        sx, sw = _ptr(x_scale), _ptr(w_scale)  # refused by the call where given
     if out_dtype is None:
         out_dtype = torch.bfloat16 if dt == E4M3 else xdt
     shape = (T, N)
@@ -728,13 +740,19 @@ def mem_linear(x: torch.Tensor, w: torch.Tensor, bias=None, *, residual=None, ac
         _like(y_out, shape, out_dtype, "y_out")
     if z_out is not None:
         _like(z_out, shape, out_dtype, "z_out")
+        zp = z_out.data_ptr()
     elif want_z:
         z_out = x.new_empty(shape, dtype=out_dtype)
-    _like(bias, (N,), out_dtype, "bias")
-    _like(residual, shape, out_dtype, "residual")
-    _check(L.mem_linear(_ptr(x), _ptr(w), dt, _ptr(x_scale), _ptr(w_scale), _ptr(bias),
-                        _ptr(residual), T, N, K, _act(act), _ptr(z_out), _ptr(y_out), _dt(y_out),
-                        _stream(stream)))
+        zp = z_out.data_ptr()
+    if bias is not None:
+        _like(bias, (N,), out_dtype, "bias")
+        bp = bias.data_ptr()
+    if residual is not None:
+        _like(residual, shape, out_dtype, "residual")
+        rp = residual.data_ptr()
+    _check((_LIB or load()).mem_linear(x.data_ptr(), w.data_ptr(), dt, sx, sw, bp, rp, T, N, K,
+                                       _act(act), zp,
+                                       y_out.data_ptr(), _dt(y_out), _stream(stream)))
     return y_out, z_out
 
 
@@ -853,25 +871,21 @@ def _adamw_tensor(p, g, m, v, sm, sv, gshape) -> tuple:
 
 
 def _adamw_opts(lr, betas, eps, weight_decay, step, seed, grad_scale) -> _AdamwOpts:
-    o = _AdamwOpts(beta1=betas[0], beta2=betas[1], eps=eps, weight_decay=weight_decay,
-                   seed=int(seed) & 0xFFFFFFFFFFFFFFFF)
+    fixed_lr, fixed_step, lr_dev, step_dev, scale = lr, step, None, None, None
     if isinstance(lr, torch.Tensor):
         _like(lr.reshape(-1), (1,), torch.float32, "lr")
         _here(lr)
-        o.lr_dev = lr.data_ptr()
-    else:
-        o.lr = lr
+        fixed_lr, lr_dev = 0.0, lr.data_ptr()
     if isinstance(step, torch.Tensor):
         _like(step.reshape(-1), (1,), torch.int64, "step")
         _here(step)
-        o.step_dev = step.data_ptr()
-    else:
-        o.step = int(step)
+        fixed_step, step_dev = 0, step.data_ptr()
     if grad_scale is not None:
         _like(grad_scale.reshape(-1), (1,), torch.float32, "grad_scale")
         _here(grad_scale)
-        o.grad_scale = grad_scale.data_ptr()
-    return o
+        scale = grad_scale.data_ptr()
+    return _AdamwOpts(fixed_lr, betas[0], betas[1], eps, weight_decay, int(fixed_step),
+                      int(seed) & 0xFFFFFFFFFFFFFFFF, lr_dev, step_dev, scale)
 
 
 @_launches_on_stream
