@@ -25,6 +25,9 @@
  *   - A non-zero return means nothing was enqueued (argument errors are found on
  *     the host before any launch) or a HIP error (PKMEM_ERR_HIP).  No call aborts
  *     or throws; mem_last_error() gives a message for the calling thread.
+ *   - A workspace belongs to its call until the call's work is done: calls that
+ *     may overlap (on two streams, or in two captured graphs that are replayed at
+ *     once) need one each.
  *   - Inputs must be finite.  Indices passed to the bag calls must lie in [0, N)
  *     and are not range-checked (they normally come from mem_search, whose
  *     product-key indices lie in [0, S*S) whatever the scores).
@@ -483,7 +486,7 @@ int mem_linear_backward(const void* dz, const void* x, const void* w, pkmem_dtyp
  * rate, the step number and the gradients' factor (a clipping factor, say) are
  * read when the call runs, so a captured step can be replayed while they
  * move on (lr and step are then not used).  Where *grad_scale is 0 or not
- * finite the whole call changes nothing.
+ * finite, or *step_dev below 1, the whole call changes nothing.
  * Tensors of any length (0: skipped) and alignment; 16-byte aligned ones are
  * fast.  No two may overlap.
  * ------------------------------------------------------------------------ */

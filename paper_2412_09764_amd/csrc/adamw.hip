@@ -260,12 +260,13 @@ __device__ __forceinline__ void step8(const Tensor& t, const AdamwScalars& c, ui
 
 // Scalars that depend on values in device memory (a captured step whose rate
 // and step number move on): one thread forms them for its workgroup.  False:
-// the gradient's scale is 0 or not finite, nothing is changed.
+// the gradient's scale is 0 or not finite or the step number below 1, and
+// nothing is changed.
 template <typename A>
 __device__ __forceinline__ bool scalars(const A& a, AdamwScalars& c, float& gs, uint32_t& key,
                                         AdamwScalars* shared_c, uint32_t* shared_key) {
   gs = a.grad_scale ? *a.grad_scale : 1.f;
-  if (gs == 0.f || !finite(gs)) return false;
+  if (gs == 0.f || !finite(gs) || (a.step_dev && *a.step_dev < 1)) return false;
   c = a.c;
   key = c.key;
   if (a.lr_dev || a.step_dev) {

@@ -164,6 +164,7 @@ def test_grad_scale_and_device_scalars(gpu_lib):
     before = [t.clone() for t in a]
     for s in (0.0, float("inf"), float("nan")):
         call(a, a[1], step=4, grad_scale=torch.tensor(s, device=dev))
+    call(a, a[1], step=torch.zeros(1, dtype=torch.int64, device=dev))  # a step number below 1
     for t, u in zip(a, before):
         if t is not None:
             assert torch.equal(t.view(torch.uint8), u.view(torch.uint8))
