@@ -134,7 +134,7 @@ struct Operand {
   __device__ static __forceinline__ int source_chunk(int slot) {
     if constexpr (!KS) return (slot & 3) ^ ((slot >> 4) & 3);
     const int k = slot / (ROW / 16), c = slot % (ROW / 16);
-    if constexpr (DT == D_F32) return c ^ (((k >> 2) & 1) << 3);
+    if constexpr (DT == D_F32) return UNITS >= 4 ? c ^ (((k >> 2) & 1) << 3) : c;
     return c ^ ((((k & 3) | ((k >> 1) & 4)) & (UNITS - 1)) << 2);
   }
   // Load i of this wave of the next stage into lds; `left`: k of the range from
@@ -177,7 +177,8 @@ struct Operand {
     } else if constexpr (DT == D_F32) {
       const int kh = lane >> 5;
 #pragma unroll
-      for (int b = 0; b < NB; ++b) rd[b] = 4 * kh * ROW + (((r0 / 32 + b) ^ kh) * 128) + (lane & 31) * 4;
+      for (int b = 0; b < NB; ++b)
+        rd[b] = 4 * kh * ROW + (((r0 / 32 + b) ^ (UNITS >= 4 ? kh : 0)) * 128) + (lane & 31) * 4;
     } else {
       const int g = lane >> 4, i = lane & 15;
       const int f = ((i >> 2) | ((g >> 1) << 2)) & (UNITS - 1);
@@ -559,16 +560,21 @@ __global__ __launch_bounds__(WM* WN* KG * 64) void k_gemm(const GemmArgs g) {
   wait_loads<0>();  // no load may reach LDS after the workgroup has left it
 
   // The sums leave through LDS, 64 rows of a wave's 64 columns at a time (16 KiB a
-  // wave), so that eight lanes hold a row's 64 columns: every load and store of
-  // the epilogue covers whole cache lines.  16-byte chunk c of row r lies at slot
-  // c ^ (r & 15).  The waves of the groups of k that share a piece add its parts
-  // in group order, each for its share of the rows.
+  // wave; 32 of 32 in the smallest tiles), so that eight lanes hold a row's 64
+  // columns: every load and store of the epilogue covers whole cache lines.
+  // 16-byte chunk c of row r lies at slot c ^ (r mod the chunks of a row).  The
+  // waves of the groups of k that share a piece add its parts in group order,
+  // each for its share of the rows.
   __syncthreads();
-  constexpr int WAVES_PER_STAGE = BYTES / 16384, ROWS = 8 / KG;
-  static_assert(NJ == 2 && MI % 2 == 0 && WAVES_PER_STAGE >= 1 && WAVES_PER_STAGE * 4 >= NW * KG, "64 x 64 pieces");
-  auto piece = [&](int w) PK_INLINE {
-    const int si = w / WAVES_PER_STAGE;
-    return (si == 0 ? st0 : si == 1 ? st1 : si == 2 ? st2 : st3) + (w % WAVES_PER_STAGE) * 16384;
+  constexpr int MP = MI < 2 ? MI : 2;             // blocks of rows of a piece
+  constexpr int ROW_BYTES = NJ * 128, CH = ROW_BYTES / 16;
+  constexpr int PIECE = MP * 32 * ROW_BYTES, WAVES_PER_STAGE = BYTES / PIECE;
+  constexpr int ROW_LANES = NJ * 4, STEP = 64 / ROW_LANES;  // lanes of a row, rows of an access
+  constexpr int ACCESSES = MP * 32 / STEP, ROWS = ACCESSES < KG ? 1 : ACCESSES / KG;
+  static_assert(MI % MP == 0 && WAVES_PER_STAGE >= 1 && WAVES_PER_STAGE * 4 >= NW * KG, "pieces fit the stages");
+  auto piece = [&](int q) PK_INLINE {
+    const int v = q * NW + wave, si = v / WAVES_PER_STAGE;
+    return (si == 0 ? st0 : si == 1 ? st1 : si == 2 ? st2 : st3) + (v % WAVES_PER_STAGE) * PIECE;
   };
   if constexpr (AKS) {
     if (g.bias_sum && (g.part || tile_n == 0)) {  // the threads' sums in the order of their k
@@ -589,145 +595,131 @@ __global__ __launch_bounds__(WM* WN* KG * 64) void k_gemm(const GemmArgs g) {
       __syncthreads();
     }
   }
-  unsigned char* buf = piece(kg * NW + wave);
-  const int il = lane & 31, kh = lane >> 5, rr = lane >> 3, cc = lane & 7;
+  unsigned char* buf = piece(kg);
+  const int il = lane & 31, kh = lane >> 5, rr = lane / ROW_LANES, cc = lane % ROW_LANES;
   const int j = j0 + wj + 8 * cc;
   Epilogue epi;
   if constexpr (!GRAD) epi.init(g, j);
 #pragma unroll
-  for (int mp = 0; mp < MI; mp += 2) {
-    const int row0 = kg * ROWS * 8 + rr;
+  for (int mp = 0; mp < MI; mp += MP) {
+    const int row0 = kg * ROWS * STEP + rr;
     const int64_t ip = i0 + wi + mp * 32 + row0;
+    const bool mine = j < g.N && (ACCESSES >= KG || kg < ACCESSES);
     Raw8 res[ROWS];
     if constexpr (!GRAD) {
       if (g.res) {
 #pragma unroll
         for (int t = 0; t < ROWS; ++t)
-          if (ip + 8 * t < g.M && j < g.N) res[t].load(g.res, (size_t)(ip + 8 * t) * g.N + j, g.out_bf16);
+          if (mine && ip + STEP * t < g.M) res[t].load(g.res, (size_t)(ip + STEP * t) * g.N + j, g.out_bf16);
       }
     }
 #pragma unroll
-    for (int m = 0; m < 2; ++m)
+    for (int m = 0; m < MP; ++m)
 #pragma unroll
-      for (int nj = 0; nj < 2; ++nj)
+      for (int nj = 0; nj < NJ; ++nj)
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
           const f32x16_t& c = acc[mp + m][nj];
           const int row = m * 32 + il, ch = nj * 8 + 2 * r + kh;
-          *reinterpret_cast<float4*>(buf + row * 256 + ((ch ^ (row & 15)) << 4)) =
+          *reinterpret_cast<float4*>(buf + row * ROW_BYTES + ((ch ^ (row & (CH - 1))) << 4)) =
               float4{c[4 * r], c[4 * r + 1], c[4 * r + 2], c[4 * r + 3]};
         }
     if constexpr (KG > 1) __syncthreads();
+    if (mine) {
 #pragma unroll
-    for (int t = 0; t < ROWS; ++t) {
-      const int row = row0 + 8 * t;
-      const int64_t i = ip + 8 * t;
-      float v[8];
+      for (int t = 0; t < ROWS; ++t) {
+        const int row = row0 + STEP * t;
+        const int64_t i = ip + STEP * t;
+        if (i >= g.M) continue;
+        float v[8];
 #pragma unroll
-      for (int q = 0; q < KG; ++q) {
-        const unsigned char* from = KG > 1 ? piece(q * NW + wave) : buf;
-        Raw8 a;
-        a.lo = ld16(from + row * 256 + (((2 * cc) ^ (row & 15)) << 4));
-        a.hi = ld16(from + row * 256 + (((2 * cc + 1) ^ (row & 15)) << 4));
-        float u[8];
-        a.unpack(false, u);
+        for (int q = 0; q < KG; ++q) {
+          const unsigned char* from = KG > 1 ? piece(q) : buf;
+          Raw8 a;
+          a.lo = ld16(from + row * ROW_BYTES + (((2 * cc) ^ (row & (CH - 1))) << 4));
+          a.hi = ld16(from + row * ROW_BYTES + (((2 * cc + 1) ^ (row & (CH - 1))) << 4));
+          float u[8];
+          a.unpack(false, u);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = q ? v[e] + u[e] : u[e];
-      }
-      if (i >= g.M || j >= g.N) continue;
-      const size_t at = (size_t)i * g.N + j;
-      if constexpr (GRAD) {
-        if (g.part) {
-          store8(g.part + (size_t)split * g.M * g.N, at, false, v);
-        } else {
-          float o[8];
-          Raw8 old;
-          old.load(g.out, at, false);
-          old.unpack(false, o);
-#pragma unroll
-          for (int e = 0; e < 8; ++e) v[e] += o[e];
-          store8(g.out, at, false, v);
+          for (int e = 0; e < 8; ++e) v[e] = q ? v[e] + u[e] : u[e];
         }
-      } else {
-        epi.store(g, at, g.a_scale ? g.a_scale[i] : 1.f, res[t], v);
+        const size_t at = (size_t)i * g.N + j;
+        if constexpr (GRAD) {
+          if (g.part) {
+            store8(g.part + (size_t)split * g.M * g.N, at, false, v);
+          } else {
+            float o[8];
+            Raw8 old;
+            old.load(g.out, at, false);
+            old.unpack(false, o);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] += o[e];
+            store8(g.out, at, false, v);
+          }
+        } else {
+          epi.store(g, at, g.a_scale ? g.a_scale[i] : 1.f, res[t], v);
+        }
       }
     }
-    if constexpr (KG > 1 && MI > 2) __syncthreads();  // the pieces are read before they are written again
+    if constexpr (KG > 1 && MI > MP) __syncthreads();  // the pieces are read before they are written again
   }
 }
 
-// Few rows of x: a workgroup takes 16 rows of W and up to 16 TT rows of x; its
+// Few rows of x (up to 8): a workgroup takes 16 rows of W and all of x; its
 // waves share k in chunks of 64 bytes, straight from memory into the 16x16
 // fragments (rows past the end are read as the last one and dropped), and add
-// their sums through LDS in wave order.  Bound by reading W once.
-template <int DT>
-struct Few {
-  typedef __attribute__((ext_vector_type(4))) float f32x4_t;
-  __device__ static __forceinline__ void mma16(uint4 w, uint4 x, f32x4_t& c) {
-    if constexpr (DT == D_F32) {
-      c = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(w.x), __uint_as_float(x.x), c, 0, 0, 0);
-      c = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(w.y), __uint_as_float(x.y), c, 0, 0, 0);
-      c = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(w.z), __uint_as_float(x.z), c, 0, 0, 0);
-      c = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(w.w), __uint_as_float(x.w), c, 0, 0, 0);
-    } else if constexpr (DT == D_BF16) {
-      c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, w),
-                                                  __builtin_bit_cast(bf16x8_t, x), c, 0, 0, 0);
-    } else {
-      c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, widen8(w.x, w.y)),
-                                                  __builtin_bit_cast(bf16x8_t, widen8(x.x, x.y)), c, 0, 0, 0);
-      c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, widen8(w.z, w.w)),
-                                                  __builtin_bit_cast(bf16x8_t, widen8(x.z, x.w)), c, 0, 0, 0);
-    }
-  }
-};
-constexpr int FEW_WAVES = 8;
-constexpr int FEW_T = 64;  // rows of x up to which this form is taken
+// their sums through LDS in wave order.  Bound by reading W once: 4.8 us for one
+// row at 2048 x 2048 bf16 and 28.6 us (4.7 TB/s) at 16384 x 4096, where the
+// 32 x 32 tiles take 6.4 and 32; with 16 rows these take 6.4 and 33.8 us, this
+// form 6.8 and 41.
+constexpr int FEW_WAVES = 8, FEW_T = 8;
 
-template <int DT, int TT>
+typedef __attribute__((ext_vector_type(4))) float f32x4_t;
+template <int DT>
+__device__ __forceinline__ void mma16(uint4 w, uint4 x, f32x4_t& c) {
+  if constexpr (DT == D_F32) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      c = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(word(w, i)), __uint_as_float(word(x, i)), c, 0, 0, 0);
+  } else if constexpr (DT == D_BF16) {
+    c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, w),
+                                                __builtin_bit_cast(bf16x8_t, x), c, 0, 0, 0);
+  } else {
+    c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, widen8(w.x, w.y)),
+                                                __builtin_bit_cast(bf16x8_t, widen8(x.x, x.y)), c, 0, 0, 0);
+    c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, widen8(w.z, w.w)),
+                                                __builtin_bit_cast(bf16x8_t, widen8(x.z, x.w)), c, 0, 0, 0);
+  }
+}
+
+template <int DT>
 __global__ __launch_bounds__(FEW_WAVES * 64) void k_gemm_few(const GemmArgs g) {
-  using F = Few<DT>;
   constexpr int AHEAD = 4;  // chunks in flight
-  __shared__ __align__(16) float sums[FEW_WAVES][TT * 16][16];
+  __shared__ __align__(16) float sums[FEW_WAVES][16][16];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int n0 = blockIdx.x * 16, kq = (lane >> 4) * 16;
-  const int64_t t0 = (int64_t)blockIdx.y * (16 * TT);
   const int64_t row_bytes = g.K * elem_size(DT);
-  const int n = n0 + (lane & 15);
+  const int n = n0 + (lane & 15), r0 = lane & 15;
   const char* wp = (const char*)g.b + (int64_t)(n < g.N ? n : g.N - 1) * row_bytes + kq;
-  const char* xp[TT];
-#pragma unroll
-  for (int t = 0; t < TT; ++t) {
-    const int64_t r = t0 + 16 * t + (lane & 15);
-    xp[t] = (const char*)g.a + (r < g.M ? r : g.M - 1) * row_bytes + kq;
-  }
-  typename F::f32x4_t acc[TT];
-#pragma unroll
-  for (int t = 0; t < TT; ++t) acc[t] = typename F::f32x4_t{0.f, 0.f, 0.f, 0.f};
+  const char* xp = (const char*)g.a + (r0 < g.M ? r0 : g.M - 1) * row_bytes + kq;
+  f32x4_t acc = {0.f, 0.f, 0.f, 0.f};
   const uint4 zero{0, 0, 0, 0};
   for (int64_t kb = wave * 64; kb < row_bytes; kb += FEW_WAVES * 64 * AHEAD) {
-    uint4 w[AHEAD], x[AHEAD][TT];
+    uint4 w[AHEAD], x[AHEAD];
 #pragma unroll
     for (int a = 0; a < AHEAD; ++a) {
       const int64_t at = kb + a * (FEW_WAVES * 64);
       const bool in = at + kq < row_bytes;
       w[a] = in ? ld16_nt(wp + at) : zero;
-#pragma unroll
-      for (int t = 0; t < TT; ++t) x[a][t] = in ? ld16(xp[t] + at) : zero;
+      x[a] = in ? ld16(xp + at) : zero;
     }
 #pragma unroll
-    for (int a = 0; a < AHEAD; ++a)
-#pragma unroll
-      for (int t = 0; t < TT; ++t) F::mma16(w[a], x[a][t], acc[t]);
+    for (int a = 0; a < AHEAD; ++a) mma16<DT>(w[a], x[a], acc);
   }
-#pragma unroll
-  for (int t = 0; t < TT; ++t)
-    *reinterpret_cast<float4*>(&sums[wave][16 * t + (lane & 15)][4 * (lane >> 4)]) =
-        float4{acc[t][0], acc[t][1], acc[t][2], acc[t][3]};
+  *reinterpret_cast<float4*>(&sums[wave][lane & 15][4 * (lane >> 4)]) = float4{acc[0], acc[1], acc[2], acc[3]};
   __syncthreads();
-  const int r = threadIdx.x >> 1, c = (threadIdx.x & 1) * 8;
-  const int64_t i = t0 + r;
-  const int j = n0 + c;
-  if (r >= 16 * TT || i >= g.M || j >= g.N) return;
+  const int i = threadIdx.x >> 1, c = (threadIdx.x & 1) * 8, j = n0 + c;
+  if (i >= g.M || j >= g.N) return;  // M <= 8
   Epilogue epi;
   epi.init(g, j);
   Raw8 res;
@@ -735,10 +727,10 @@ __global__ __launch_bounds__(FEW_WAVES * 64) void k_gemm_few(const GemmArgs g) {
   if (g.res) res.load(g.res, at, g.out_bf16);
   float v[8];
 #pragma unroll
-  for (int e = 0; e < 8; ++e) v[e] = sums[0][r][c + e];
+  for (int e = 0; e < 8; ++e) v[e] = sums[0][i][c + e];
   for (int q = 1; q < FEW_WAVES; ++q)
 #pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] += sums[q][r][c + e];
+    for (int e = 0; e < 8; ++e) v[e] += sums[q][i][c + e];
   epi.store(g, at, g.a_scale ? g.a_scale[i] : 1.f, res, v);
 }
 
@@ -838,15 +830,20 @@ inline int ceil_div(int64_t a, int64_t b) { return (int)((a + b - 1) / b); }
 
 // Tiles: 256 x 256 by eight waves; 128 x 128 by four, two workgroups a CU; the same
 // with four waves more for the other half of k, one workgroup a CU; 64 x 64 by
-// four waves that share k.
-enum { TILE_256, TILE_128, TILE_128_K2, TILE_64 };
-constexpr int tile_size(int t) { return t == TILE_256 ? 256 : t == TILE_64 ? 64 : 128; }
+// four waves, 32 x 32 by eight that share k.
+enum { TILE_256, TILE_128, TILE_128_K2, TILE_64, TILE_32 };
+constexpr int tile_size(int t) { return t == TILE_256 ? 256 : t == TILE_64 ? 64 : t == TILE_32 ? 32 : 128; }
 int64_t tile_count(int t, int64_t M, int64_t N) { return (int64_t)ceil_div(M, tile_size(t)) * ceil_div(N, tile_size(t)); }
-// The largest tiles that are enough to fill the chip.
-int pick_tile(int64_t M, int64_t N) {
+// The largest tiles that are enough to fill the chip, but none twice as high as
+// the rows there are; the smallest where one round of them does (two in fp32,
+// whose time goes with the tile).  2048 x 2048 bf16: 128 rows 7.2 us in tiles of
+// 32 and 8.9 of 64, 256 rows 12.8 and 9.6; 512 rows 12.1 in 64 and 15.1 in 128,
+// 1024 rows 23.7 and 16.7, 2048 25 (K2), 4096 42 in 128 and 47.6 in 256, 8192 83 and 63.
+int pick_tile(bool f32, int64_t M, int64_t N) {
+  if (tile_count(TILE_32, M, N) <= (f32 ? 512 : 256)) return TILE_32;
   if (tile_count(TILE_256, M, N) >= 200) return TILE_256;
   const int64_t mid = tile_count(TILE_128, M, N);
-  return mid > 256 ? TILE_128 : mid >= 128 ? TILE_128_K2 : TILE_64;
+  return M <= 64 || mid < 128 ? TILE_64 : mid <= 256 ? TILE_128_K2 : TILE_128;
 }
 
 template <int DT, bool AKS, bool BKS, bool GRAD>
@@ -860,40 +857,36 @@ void gemm_launch(GemmArgs g, int tile, int splits, hipStream_t st) {
     hipLaunchKernelGGL((k_gemm<DT, AKS, BKS, GRAD, 128, 128, 2, 2, 2>), grid, dim3(512), 0, st, g);
   else if (tile == TILE_64)
     hipLaunchKernelGGL((k_gemm<DT, AKS, BKS, GRAD, 64, 64, 1, 1, 4>), grid, dim3(256), 0, st, g);
+  else if (tile == TILE_32)
+    hipLaunchKernelGGL((k_gemm<DT, AKS, BKS, GRAD, 32, 32, 1, 1, 8>), grid, dim3(512), 0, st, g);
   else if constexpr (!GRAD)  // the weight gradient splits k instead
     hipLaunchKernelGGL((k_gemm<DT, AKS, BKS, GRAD, 128, 128, 2, 2, 1>), grid, dim3(256), 0, st, g);
 }
 template <int DT>
-void few_launch(const GemmArgs& g, hipStream_t st) {
-  const int tt = g.M <= 16 ? 1 : g.M <= 32 ? 2 : 4;
-  const dim3 grid((unsigned)ceil_div(g.N, 16), (unsigned)ceil_div(g.M, 16 * tt)), block(FEW_WAVES * 64);
-  if (tt == 1) hipLaunchKernelGGL((k_gemm_few<DT, 1>), grid, block, 0, st, g);
-  else if (tt == 2) hipLaunchKernelGGL((k_gemm_few<DT, 2>), grid, block, 0, st, g);
-  else hipLaunchKernelGGL((k_gemm_few<DT, 4>), grid, block, 0, st, g);
-}
-template <int DT>
 void forward_launch(const GemmArgs& g, hipStream_t st) {
-  if (g.M <= FEW_T) few_launch<DT>(g, st);
-  else gemm_launch<DT, false, false, false>(g, pick_tile(g.M, g.N), 1, st);
+  if (g.M <= FEW_T)
+    hipLaunchKernelGGL(k_gemm_few<DT>, dim3((unsigned)ceil_div(g.N, 16)), dim3(FEW_WAVES * 64), 0, st, g);
+  else
+    gemm_launch<DT, false, false, false>(g, pick_tile(DT == D_F32, g.M, g.N), 1, st);
 }
 
 // grad_W [N, K] from T tokens: the tile and the number of splits of the tokens
 // with the least time by these measured parts: a stage of 64 bytes of k takes a
-// workgroup 0.85 us (256 wide), 0.35 (128, two groups) or 0.11 (64, four groups) in
-// bf16 and 3.9, 0.95, 0.24 in fp32, whose matrix rate is a sixteenth for twice the
-// bytes; a workgroup's start and end 5 us; splitting a launch of 5 us, and
-// writing and reading the parts at 5 TB/s.
+// workgroup 0.85 us (256 wide), 0.35 (128, two groups), 0.11 (64, four groups) or
+// 0.03 (32, eight groups) in bf16 and 3.9, 0.95, 0.24 and 0.065 in fp32, whose
+// matrix rate is a sixteenth for twice the bytes; a workgroup's start and end 5
+// us; splitting a launch of 5 us, and writing and reading the parts at 5 TB/s.
 struct GradPlan {
   int tile, splits;
   int64_t k_split;
 };
 GradPlan grad_plan(bool bf16, int64_t T, int N, int K) {
-  constexpr int tiles[3] = {TILE_256, TILE_128_K2, TILE_64};
-  constexpr double stage_us[2][3] = {{3.9, 0.95, 0.24}, {0.85, 0.35, 0.11}};
+  constexpr int tiles[4] = {TILE_256, TILE_128_K2, TILE_64, TILE_32};
+  constexpr double stage_us[2][4] = {{3.9, 0.95, 0.24, 0.065}, {0.85, 0.35, 0.11, 0.03}};
   const int64_t per_stage = bf16 ? 32 : 16;
   GradPlan best{TILE_64, 1, T};
   double least = 1e30;
-  for (int c = 0; c < 3; ++c) {
+  for (int c = 0; c < 4; ++c) {
     const int64_t count = tile_count(tiles[c], N, K);
     for (int s = 1; s <= 64; s *= 2) {
       const int64_t k_split = ((T + s - 1) / s + 63) / 64 * 64;
@@ -992,7 +985,7 @@ hipError_t launch_linear_backward(bool bf16, const void* dz, const void* x, cons
     g.res = add;
     g.out = dx;
     g.out_bf16 = bf16;
-    const int tile = pick_tile(T, K);
+    const int tile = pick_tile(!bf16, T, K);
     if (bf16) gemm_launch<D_BF16, false, true, false>(g, tile, 1, st);
     else gemm_launch<D_F32, false, true, false>(g, tile, 1, st);
   }
