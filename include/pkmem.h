@@ -520,7 +520,7 @@ int mem_adamw(const pkmem_adamw_tensor* tensors, int count, const pkmem_adamw_op
  *              PKMEM_F32 (grad_rows_out); PKMEM_E4M3 states need D % 128 == 0,
  *              their scales are [N, D / 128], the same as mem_adamw's.
  *   D          D % 8 == 0; all buffers 16-byte aligned.
- *   rows       [U] int64, ascending, U <= 2^31 - 1.  Equal neighbours are one
+ *   rows       [U] int64, ascending, U * ceil(D / 128) < 2^31 - 64.  Equal neighbours are one
  *              row whose gradients are added in order; a row outside [0, N)
  *              is passed over (with PKMEM_DEBUG both a row outside and a
  *              descending list are errors). */

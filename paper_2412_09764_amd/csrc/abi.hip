@@ -844,7 +844,7 @@ int mem_adamw_rows(const pkmem_adamw_tensor* table, int64_t N, int D, const int6
       !aligned(table->exp_avg_sq, 16))
     return fail(PKMEM_ERR_INVALID, "%s: buffers must be 16-byte aligned", fn);
   if (U < 0) return fail(PKMEM_ERR_INVALID, "%s: U must be >= 0", fn);
-  if (U > 0x7FFFFFFF || U * (int64_t)((D + 127) / 128) > (int64_t(1) << 35))
+  if (U > 0x7FFFFFFF || U * (int64_t)((D + 127) / 128) > 0x7FFFFFFF - 64)
     return fail(PKMEM_ERR_UNSUPPORTED, "%s: too many rows", fn);
   if (U > 0 && !rows) return fail(PKMEM_ERR_INVALID, "%s: null pointer", fn);
   if (!aligned(rows, 8)) return fail(PKMEM_ERR_INVALID, "%s: rows must be 8-byte aligned", fn);

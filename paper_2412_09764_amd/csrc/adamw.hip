@@ -331,13 +331,13 @@ __global__ __launch_bounds__(BLOCK) void k_adamw_rows(const RowArgs a) {
   float gs;
   uint32_t key;
   if (!scalars(a, c, gs, key, &sc, &skey)) return;
-  const uint64_t units = (uint64_t)a.U * a.per_row;
-  uint64_t unit = (uint64_t)blockIdx.x * (WG_UNITS * PASSES) + threadIdx.x / UNIT_LANES;
+  const uint32_t units = (uint32_t)a.U * (uint32_t)a.per_row;  // below 2^31
+  uint32_t unit = blockIdx.x * (WG_UNITS * PASSES) + threadIdx.x / UNIT_LANES;
 #pragma unroll
   for (int s = 0; s < PASSES; ++s, unit += WG_UNITS) {
     if (unit >= units) break;
-    const int64_t u = (int64_t)(unit / (uint32_t)a.per_row);
-    const int b = (int)(unit - (uint64_t)u * a.per_row);
+    const int64_t u = unit / (uint32_t)a.per_row;
+    const int b = (int)(unit % (uint32_t)a.per_row);
     const int64_t row = a.rows[u];
     if (row < 0 || row >= a.N || (u > 0 && a.rows[u - 1] == row)) continue;
     const int col = b * UNIT + (threadIdx.x % UNIT_LANES) * LANE_ELEMS;
