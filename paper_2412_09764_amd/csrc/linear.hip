@@ -74,9 +74,26 @@ __device__ __forceinline__ void mma_bf16(uint4 b, uint4 a, f32x16_t& c) {
   c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, b),
                                               __builtin_bit_cast(bf16x8_t, a), c, 0, 0, 0);
 }
-__device__ __forceinline__ void mma_f32(uint32_t b, uint32_t a, f32x16_t& c) {
-  c = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(b), __uint_as_float(a), c, 0, 0, 0);
+// Eight fp32 numbers as sums of three bf16 numbers each, 8 bits of mantissa at a
+// time (what is left is below 2^-26 of the number).
+__device__ __forceinline__ void split8(uint4 lo, uint4 hi, uint4 (&part)[3]) {
+  float v[8];
+  Chunk<float>::unpack(lo, v);
+  Chunk<float>::unpack(hi, v + 4);
+#pragma unroll
+  for (int q = 0; q < 3; ++q) {
+    part[q] = Chunk<uint16_t>::pack(v);
+    if (q < 2) {
+      float u[8];
+      Chunk<uint16_t>::unpack(part[q], u);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[e] -= u[e];
+    }
+  }
 }
+// Of the nine products of two numbers in three parts, the six above 2^-24 of the
+// whole, smallest first: the parts of b and of a.
+constexpr int SPLIT_B[6] = {2, 0, 1, 1, 0, 0}, SPLIT_A[6] = {0, 2, 1, 0, 1, 0};
 __device__ __forceinline__ uint32_t word(uint4 v, int i) { return i == 0 ? v.x : i == 1 ? v.y : i == 2 ? v.z : v.w; }
 // 8 e4m3 codes as bf16 (exact).  The 8-bit matrix instructions align the products
 // of each 8 k to the largest of them and keep 13 bits below it; a sum in fp32 takes
@@ -403,39 +420,37 @@ __global__ __launch_bounds__(WM* WN* KG * 64) void k_gemm(const GemmArgs g) {
     for (int i = 0; i < L; ++i) load(st, i);
     advance();
   };
-  // Fragments of the halves 0 and 1 of a stage.
-  uint4 fa[2][MI], fb[2][NJ];
-  auto read = [&](const unsigned char* st, int h) PK_INLINE {
+  // Fragments of the halves 0 and 1 of a stage; in fp32 where every wave multiplies
+  // all the time, of two stages in turn.
+  constexpr bool TURNS = NW * KG == 8;
+  constexpr int SETS = DT == D_F32 && !TURNS ? 2 : 1;
+  uint4 fa[SETS][2][MI], fb[SETS][2][NJ];
+  auto read = [&](const unsigned char* st, int h, int set = 0) PK_INLINE {
 #pragma unroll
-    for (int nj = 0; nj < NJ; ++nj) fb[h][nj] = ob.frag(st + group_at + OA::BYTES, nj, h);
+    for (int nj = 0; nj < NJ; ++nj) fb[set][h][nj] = ob.frag(st + group_at + OA::BYTES, nj, h);
 #pragma unroll
-    for (int mi = 0; mi < MI; ++mi) fa[h][mi] = oa.frag(st + group_at, mi, h);
+    for (int mi = 0; mi < MI; ++mi) fa[set][h][mi] = oa.frag(st + group_at, mi, h);
   };
-  // The products of half h, in MI (fp32: 4, e4m3: 2 MI) groups of different sums;
-  // between them, where asked for, the loads of a stage into st.
-  constexpr int GROUPS = DT == D_E4M3 ? 2 * MI : DT == D_F32 ? 4 : MI;
+  // bf16, e4m3: the products of half h, in MI or 2 MI groups; between them, where
+  // asked for, the loads of a stage into st.
   auto products = [&](int h, bool refill, unsigned char* st) PK_INLINE {
+    constexpr int GROUPS = DT == D_E4M3 ? 2 * MI : MI;
     uint4 b[NJ];
 #pragma unroll
     for (int q = 0; q < GROUPS; ++q) {
+      const int mi = q % MI;
       if constexpr (DT == D_E4M3) {
-        const int mi = q % MI;
         if (mi == 0) {
 #pragma unroll
           for (int nj = 0; nj < NJ; ++nj)
-            b[nj] = q >= MI ? widen8(fb[h][nj].z, fb[h][nj].w) : widen8(fb[h][nj].x, fb[h][nj].y);
+            b[nj] = q ? widen8(fb[0][h][nj].z, fb[0][h][nj].w) : widen8(fb[0][h][nj].x, fb[0][h][nj].y);
         }
-        const uint4 a = q >= MI ? widen8(fa[h][mi].z, fa[h][mi].w) : widen8(fa[h][mi].x, fa[h][mi].y);
+        const uint4 a = q >= MI ? widen8(fa[0][h][mi].z, fa[0][h][mi].w) : widen8(fa[0][h][mi].x, fa[0][h][mi].y);
 #pragma unroll
         for (int nj = 0; nj < NJ; ++nj) mma_bf16(b[nj], a, acc[mi][nj]);
-      } else if constexpr (DT == D_F32) {
-#pragma unroll
-        for (int mi = 0; mi < MI; ++mi)
-#pragma unroll
-          for (int nj = 0; nj < NJ; ++nj) mma_f32(word(fb[h][nj], q), word(fa[h][mi], q), acc[mi][nj]);
       } else {
 #pragma unroll
-        for (int nj = 0; nj < NJ; ++nj) mma_bf16(fb[h][nj], fa[h][q], acc[q][nj]);
+        for (int nj = 0; nj < NJ; ++nj) mma_bf16(fb[0][h][nj], fa[0][h][mi], acc[mi][nj]);
       }
       if (refill) {
         __builtin_amdgcn_sched_barrier(0);
@@ -443,6 +458,22 @@ __global__ __launch_bounds__(WM* WN* KG * 64) void k_gemm(const GemmArgs g) {
         for (int i = q * L / GROUPS; i < (q + 1) * L / GROUPS; ++i) load(st, i);
         __builtin_amdgcn_sched_barrier(0);
       }
+    }
+  };
+  // fp32: the products of a whole stage, six bf16 ones for each.  (The fp32 matrix
+  // instructions take 2.7 times their cycles.)
+  auto products_f32 = [&](int set) PK_INLINE {
+    uint4 b[NJ][3];
+#pragma unroll
+    for (int nj = 0; nj < NJ; ++nj) split8(fb[set][0][nj], fb[set][1][nj], b[nj]);
+#pragma unroll
+    for (int mi = 0; mi < MI; ++mi) {
+      uint4 a[3];
+      split8(fa[set][0][mi], fa[set][1][mi], a);
+#pragma unroll
+      for (int t = 0; t < 6; ++t)
+#pragma unroll
+        for (int nj = 0; nj < NJ; ++nj) mma_bf16(b[nj][SPLIT_B[t]], a[SPLIT_A[t]], acc[mi][nj]);
     }
   };
   // The sums over A's k: when split, the tiles along j take the stages in turn, else
@@ -462,7 +493,7 @@ __global__ __launch_bounds__(WM* WN* KG * 64) void k_gemm(const GemmArgs g) {
       if (bias_turn > 0) --bias_turn;
     }
   };
-  if constexpr (NW * KG == 8 && DT != D_F32) {
+  if constexpr (TURNS) {
     // Two waves share a SIMD, one of the first four and one of the last: while one
     // of them multiplies a stage the other reads its next one and issues the loads,
     // and they change places at a barrier, so the matrix cores always have a
@@ -470,8 +501,12 @@ __global__ __launch_bounds__(WM* WN* KG * 64) void k_gemm(const GemmArgs g) {
     // the last four read it; then the first four read stage s + 1 and refill s.
     auto multiply = [&]() PK_INLINE {
       __builtin_amdgcn_s_setprio(1);
-      products(0, false, st0);
-      products(1, false, st0);
+      if constexpr (DT == D_F32) {
+        products_f32(0);
+      } else {
+        products(0, false, st0);
+        products(1, false, st0);
+      }
       __builtin_amdgcn_s_setprio(0);
     };
     auto read_all = [&](const unsigned char* st) PK_INLINE {
@@ -522,9 +557,37 @@ __global__ __launch_bounds__(WM* WN* KG * 64) void k_gemm(const GemmArgs g) {
       if (s + 1 < steps) last(st1, st0);
       if (s + 2 < steps) last(st2, st1);
     }
+  } else if constexpr (DT == D_F32) {
+    // One stage: it is in the registers of set; next has landed for all after the
+    // barrier, and is read while the products run.
+    auto stage = [&](int set, unsigned char* st, const unsigned char* next) PK_INLINE {
+      wait_and_meet<2 * L>();
+      read(next, 0, set ^ 1);
+      read(next, 1, set ^ 1);
+      __builtin_amdgcn_sched_barrier(0);
+      add_bias(next);
+      fill(st);
+      products_f32(set);
+    };
+    fill(st0);
+    fill(st1);
+    fill(st2);
+    fill(st3);
+    wait_and_meet<3 * L>();
+    read(st0, 0, 0);
+    read(st0, 1, 0);
+    add_bias(st0);
+    int s = 0;
+    for (; s + 4 <= steps; s += 4) {
+      stage(0, st0, st1);
+      stage(1, st1, st2);
+      stage(0, st2, st3);
+      stage(1, st3, st0);
+    }
+    if (s < steps) stage(0, st0, st1);
+    if (s + 1 < steps) stage(1, st1, st2);
+    if (s + 2 < steps) stage(0, st2, st3);
   } else {
-    // One wave a SIMD, or fp32, where the products take so long that waves that
-    // multiply at once hide all else (32768 x 2048 x 2048: 1943 against 2056 us in turns).
     // One stage: st is visible to all, half 0 of it in registers.  After the
     // barrier every wave has read st, and next has landed for all.  The reads of
     // a half are issued before the products of the half before it and return
