@@ -415,7 +415,10 @@ int mem_quantize_rows(const void* x, pkmem_dtype dt, int64_t R, int C, void* q_o
  * A projection of the block: matrix product with its epilogue in one call,
  *   z[t,:] = x[t,:] W^T (times x_scale[t] * w_scale[n]) + bias,
  *   y[t,:] = act(z[t,:]) + res[t,:],
- * sums and epilogue in fp32, one rounding to y_dt.
+ * sums and epilogue in fp32, one rounding to y_dt.  Products are exact for
+ * PKMEM_BF16 and PKMEM_E4M3; PKMEM_F32 operands are taken in three bf16 parts (24
+ * bits of mantissa) and each product is within 2^-23 of itself, for magnitudes
+ * from 2^-110 (below, within 2^-126 of the operand) to 3.38e38.
  *
  *   x  [T, K], w [N, K]  dtype dt: PKMEM_F32, PKMEM_BF16, or PKMEM_E4M3 with
  *           x_scale [T] and w_scale [N] fp32 (mem_rmsnorm's and

@@ -898,8 +898,8 @@ enum { TILE_256, TILE_128, TILE_128_K2, TILE_64, TILE_32 };
 constexpr int tile_size(int t) { return t == TILE_256 ? 256 : t == TILE_64 ? 64 : t == TILE_32 ? 32 : 128; }
 int64_t tile_count(int t, int64_t M, int64_t N) { return (int64_t)ceil_div(M, tile_size(t)) * ceil_div(N, tile_size(t)); }
 // The largest tiles that are enough to fill the chip, but none twice as high as
-// the rows there are; the smallest where one round of them does (two in fp32,
-// whose time goes with the tile).  2048 x 2048 bf16: 128 rows 7.2 us in tiles of
+// the rows there are; the smallest where one round of them does (two in fp32:
+// 300 x 1024 x 1024 takes 14.8 us in them and 16.5 in tiles of 64).  2048 x 2048 bf16: 128 rows 7.2 us in tiles of
 // 32 and 8.9 of 64, 256 rows 12.8 and 9.6; 512 rows 12.1 in 64 and 15.1 in 128,
 // 1024 rows 23.7 and 16.7, 2048 25 (K2), 4096 42 in 128 and 47.6 in 256, 8192 83 and 63.
 int pick_tile(bool f32, int64_t M, int64_t N) {
@@ -935,17 +935,19 @@ void forward_launch(const GemmArgs& g, hipStream_t st) {
 
 // grad_W [N, K] from T tokens: the tile and the number of splits of the tokens
 // with the least time by these measured parts: a stage of 64 bytes of k takes a
-// workgroup 0.85 us (256 wide), 0.35 (128, two groups), 0.11 (64, four groups) or
-// 0.03 (32, eight groups) in bf16 and 3.9, 0.95, 0.24 and 0.065 in fp32, whose
-// matrix rate is a sixteenth for twice the bytes; a workgroup's start and end 5
-// us; splitting a launch of 5 us, and writing and reading the parts at 5 TB/s.
+// workgroup 0.85 us (256 wide), 0.35 (128, two groups), 0.1 (64, four groups) or
+// 0.06 (32, eight groups) in bf16 and 2.3, 0.7, 0.2 and 0.09 in fp32, which takes
+// six products for each; a workgroup's start and end 5 us; splitting a launch of
+// 5 us, and writing and reading the parts at 5 TB/s.  4096 tokens of 1024 x 1024
+// bf16: 18.1 us in tiles of 64, 21.4 in four splits of 128, 48.5 of 32; 4934 of
+// 2048 x 1024 fp32: 127 us in eight splits of 256, 141 of 64.
 struct GradPlan {
   int tile, splits;
   int64_t k_split;
 };
 GradPlan grad_plan(bool bf16, int64_t T, int N, int K) {
   constexpr int tiles[4] = {TILE_256, TILE_128_K2, TILE_64, TILE_32};
-  constexpr double stage_us[2][4] = {{3.9, 0.95, 0.24, 0.065}, {0.85, 0.35, 0.11, 0.03}};
+  constexpr double stage_us[2][4] = {{2.3, 0.7, 0.2, 0.09}, {0.85, 0.35, 0.1, 0.06}};
   const int64_t per_stage = bf16 ? 32 : 16;
   GradPlan best{TILE_64, 1, T};
   double least = 1e30;

@@ -176,6 +176,25 @@ def test_gradients_against_differences(gpu_lib, act):
         assert abs((up - down) / (2 * h) - float(g[at])) <= 72 * 4 * (K * U * 10 / h + h * h / 3) + kink
 
 
+def test_fp32_of_any_scale(gpu_lib):
+    """Powers of two go through the product untouched: operands scaled by 2^e and 2^-e give
+    the same bits, and products far from one in size stay within the bound of fp32."""
+    T, N, K = 200, 136, 264
+    x, w, dz = randn((T, K), F32, 1), randn((N, K), F32, 2), randn((T, N), F32, 3)
+    y, _ = pk.mem_linear(x, w)
+    want = exact_mm(x, w)
+    assert torch.all((y.double() - want).abs() <= (K + 4) * U * exact_mm(x.abs(), w.abs()))
+    dx, gw, _ = pk.mem_linear_backward(dz, x, w)
+    for e in (40, 80, -80):
+        s = 2.0 ** e
+        assert torch.equal(pk.mem_linear(x * s, w / s)[0], y)
+        got = pk.mem_linear_backward(dz * s, x / s, w / s)
+        assert torch.equal(got[0], dx) and torch.equal(got[1], gw)
+    # entries of one row from 2^-30 to 2^30
+    x = x * 2.0 ** torch.randint(-30, 31, x.shape, device="cuda", generator=torch.Generator("cuda").manual_seed(4)).float()
+    assert torch.all((pk.mem_linear(x, w)[0].double() - exact_mm(x, w)).abs() <= (K + 4) * U * exact_mm(x.abs(), w.abs()))
+
+
 def test_special_values(gpu_lib):
     """A NaN or infinity reaches the outputs that use it and no others, also where
     rows and k end inside a tile."""
