@@ -5,7 +5,9 @@
 //
 // Memory bound: parameter and states read and written once, the gradient
 // read once (28 bytes an element in fp32, 12 for a bf16 parameter with 8-bit
-// states).  A lane holds 8 consecutive elements (16- and 32-byte accesses),
+// states).  2^28 elements in fp32 1.48 ms (5.07 TB/s); 2^29 with 8-bit states 1.33
+// ms (4.88 TB/s: the vector arithmetic of quotient, root, hash and two roundings
+// takes nearly as long as the memory); 400001 touched rows of 1024 1.13 ms (4.4).  A lane holds 8 consecutive elements (16- and 32-byte accesses),
 // 16 lanes the 128 elements that share the scales of their 8-bit states, so
 // the largest element of a block is found by four lane exchanges.
 //

@@ -8,12 +8,22 @@
 // read from LDS by transposing reads (bf16) or element by element (fp32), so
 // nothing is transposed in memory.
 //
-// Tiles of 256 x 256 by eight waves (128 x 64 each, 32x32 MFMA: per 32 bytes of
-// k a wave reads 6 fragments for 8 products, three quarters of what LDS gives in
-// that time); where these are too few for the chip, smaller ones whose waves
-// also share k (64 x 64 each).  A stage holds 64 bytes of k; four stages are in LDS, filled by direct loads that
-// run three stages ahead, and the fragments of the next half stage are read
-// while the matrix cores work on the current one.
+// All products are bf16 ones with fp32 sums: e4m3 codes are widened (exactly) as
+// they leave LDS, fp32 operands are split into three bf16 parts of which six
+// products count.
+//
+// Tiles of 256 x 256 by eight waves (128 x 64 each); where these are too few for
+// the chip, smaller ones whose waves also share k.  A stage holds 64 bytes of k;
+// four stages are in LDS, filled by direct loads that run three stages ahead.
+// What bounds them: a 256-wide tile keeps the matrix cores busy 76% of its cycles,
+// at a clock that the power limit holds at 1.6 GHz (8192^3 bf16 at 1.25-1.30
+// PFLOP/s, fp32 0.214); a 128-wide one fetches its operands at the 12-14 TB/s
+// that the L2s give (0.88 PFLOP/s); small products are bound by the latency of a
+// few stages and the launch (64 x 2048 x 2048: 6.3 us).  Measured, bf16 unless said:
+//   32768 x 2048 x 2048 forward 257 us, with residual 288 (memory traffic of the
+//     epilogues, which all workgroups reach at once), fp32 1307;
+//   16384 x 2048 x 1024 dx 60 us, grad_W with its bias 76;
+//   2000 x 2048 x 2048 25 us, e4m3 17-19, fp32 95;  1 x 2048 x 2048 4.8.
 #include "pk_internal.h"
 #include "pk_mfma.h"
 #include "pk_row.h"
@@ -116,9 +126,9 @@ template <int DT, bool KS, int R, int NWAVE>
 struct Operand {
   static constexpr int E = elem_size(DT);
   static constexpr int BYTES = R * STAGE_K;
-  static constexpr int ROW = KS ? R * E : STAGE_K;     // bytes of an LDS row
+  static constexpr int ROW = KS ? R * E : STAGE_K;    // bytes of an LDS row
   static constexpr int LOADS = BYTES / 1024 / NWAVE;  // direct loads per wave and stage
-  static constexpr int STAGE_ROWS = STAGE_K / E;       // k of a stage
+  static constexpr int STAGE_ROWS = STAGE_K / E;      // k of a stage
   static_assert(BYTES % (1024 * NWAVE) == 0, "whole loads");
   static constexpr int UNITS = ROW / 64;
 
@@ -497,8 +507,10 @@ __global__ __launch_bounds__(WM* WN* KG * 64) void k_gemm(const GemmArgs g) {
     // Two waves share a SIMD, one of the first four and one of the last: while one
     // of them multiplies a stage the other reads its next one and issues the loads,
     // and they change places at a barrier, so the matrix cores always have a
-    // wave with all its operands in registers.  Stage s: the first four multiply,
-    // the last four read it; then the first four read stage s + 1 and refill s.
+    // wave with all its operands in registers (against all waves reading and
+    // multiplying at once: 8192^3 878 -> 860 us, 2000 x 2048 x 2048 in e4m3 20 -> 18).
+    // Stage s: the first four multiply, the last four read it; then the first
+    // four read stage s + 1 and refill s.
     auto multiply = [&]() PK_INLINE {
       __builtin_amdgcn_s_setprio(1);
       if constexpr (DT == D_F32) {
