@@ -3,7 +3,8 @@
 The library (include/pkmem.h) implements the product-key search of Sec. 3.1.1
 of "Memory Layers at Scale" (arXiv 2412.09764) followed by the softmax of
 Sec. 3, Eq. (1), and the weighted EmbeddingBag forward and backward of
-Sec. 3.1.4, as hand-written HIP kernels for gfx950.
+Sec. 3.1.4, with the norm, projections and optimizer of the block around them, as
+hand-written HIP kernels for gfx950.
 
 This module only marshals arguments: it checks tensor placement and dtype,
 allocates outputs and workspaces with torch on the current device (on the

@@ -15,7 +15,7 @@
 // Tiles of 256 x 256 by eight waves (128 x 64 each); where these are too few for
 // the chip, smaller ones whose waves also share k.  A stage holds 64 bytes of k;
 // four stages are in LDS, filled by direct loads that run three stages ahead.
-// What bounds them: a 256-wide tile keeps the matrix cores busy 76% of its cycles,
+// What bounds them: a 256-wide tile keeps the matrix cores busy 79% of its cycles,
 // at a clock that the power limit holds at 1.6 GHz (8192^3 bf16 at 1.25-1.30
 // PFLOP/s, fp32 0.214); a 128-wide one fetches its operands at the 12-14 TB/s
 // that the L2s give (0.88 PFLOP/s); small products are bound by the latency of a
