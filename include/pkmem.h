@@ -427,7 +427,8 @@ int mem_quantize_rows(const void* x, pkmem_dtype dt, int64_t R, int C, void* q_o
  *   y_dt    PKMEM_F32 or PKMEM_BF16; dt = PKMEM_F32 needs PKMEM_F32.
  *   act     pkmem_act.
  *   z_out   [T, N] dtype y_dt: z (what mem_act_backward needs); NULL to skip it.
- *   y_out   [T, N] dtype y_dt; may be res (in place), no other input.
+ *   y_out   [T, N] dtype y_dt; may be res (in place), no other buffer (an output
+ *           that starts where an operand does is refused).
  *   N % 8 == 0; K % 8 == 0 (PKMEM_E4M3: K % 16 == 0); N, K <= 2^20; any T
  *   below 2^31.  All buffers 16-byte aligned.  T = 0 is a valid no-op.
  * ------------------------------------------------------------------------ */
@@ -453,7 +454,7 @@ int mem_act_backward(const void* dy, const void* z, pkmem_dtype dt, int act, int
  * the forward's x [T, K] and w [N, K]:
  *   dx_out    [T, K] dtype dt, written: dz W + dx_add, rounded once; dx_add
  *             [T, K] dtype dt (another path's gradient of x) or NULL; dx_out
- *             may be dx_add.
+ *             may be dx_add, no other input.
  *   grad_w    [N, K] fp32, ACCUMULATED: += dz^T x.
  *   grad_bias [N] fp32, ACCUMULATED: += sum_t dz.
  * Each output may be NULL.  (The gradient of the forward's res is dy itself.)

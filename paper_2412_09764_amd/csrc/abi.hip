@@ -761,6 +761,7 @@ int mem_rmsnorm(const void* x, const void* res, const void* weight, pkmem_dtype 
   const bool q = y_dt == PKMEM_E4M3;
   if (T > 0 && (!x || !y_out || (q && !scale_out))) return fail(PKMEM_ERR_INVALID, "%s: null pointer", fn);
   if (!q && scale_out) return fail(PKMEM_ERR_INVALID, "%s: scale_out is for PKMEM_E4M3 only", fn);
+  if (sum_out && sum_out == y_out) return fail(PKMEM_ERR_INVALID, "%s: sum_out and y_out are one buffer", fn);
   if (!aligned(x, 16) || !aligned(res, 16) || !aligned(weight, 16) || !aligned(sum_out, 16) ||
       !aligned(y_out, 16) || !aligned(scale_out, 4))
     return fail(PKMEM_ERR_INVALID, "%s: buffers must be 16-byte aligned (scale_out 4)", fn);
@@ -901,6 +902,9 @@ int mem_linear(const void* x, const void* w, pkmem_dtype dt, const float* x_scal
       !aligned(bias, 16) || !aligned(res, 16) || !aligned(z_out, 16) || !aligned(y_out, 16))
     return fail(PKMEM_ERR_INVALID, "%s: buffers must be 16-byte aligned", fn);
   if (T == 0) return PKMEM_OK;
+  // an output over an operand that other workgroups still read
+  if (y_out == x || y_out == w || z_out == x || z_out == w || z_out == y_out || (z_out && z_out == res))
+    return fail(PKMEM_ERR_INVALID, "%s: an output may not be an operand or the other output (y_out may be res)", fn);
   const pk::LinearCall c{x, w, dt, x_scale, w_scale, bias, res, T, N, K, act, z_out, y_out, y_dt == PKMEM_BF16};
   return hip_status(pk::launch_linear(c, reinterpret_cast<hipStream_t>(stream)), fn);
 }
@@ -941,6 +945,8 @@ int mem_linear_backward(const void* dz, const void* x, const void* w, pkmem_dtyp
     return fail(PKMEM_ERR_WORKSPACE, "%s: workspace of %zu bytes needed, %zu given", fn, need, ws ? ws_bytes : (size_t)0);
   if (!aligned(ws, 256)) return fail(PKMEM_ERR_INVALID, "%s: workspace must be 256-byte aligned", fn);
   if (T == 0 || (!dx_out && !grad_w && !grad_bias)) return PKMEM_OK;
+  if (dx_out && (dx_out == dz || dx_out == x || dx_out == w))
+    return fail(PKMEM_ERR_INVALID, "%s: dx_out may be dx_add, no other input", fn);
   return hip_status(pk::launch_linear_backward(dt == PKMEM_BF16, dz, x, w, T, N, K, dx_add, dx_out,
                                                grad_w, grad_bias, ws,
                                                reinterpret_cast<hipStream_t>(stream)), fn);

@@ -8,6 +8,7 @@ import paper_2412_09764_amd as pk
 OK, INVALID, UNSUPPORTED, WORKSPACE = 0, -1, -2, -3
 F32, BF16, E4M3 = 0, 1, 2
 FAKE, BIG = 0x10000, 1 << 40
+X, W, Y, DX = 0x20000, 0x30000, 0x40000, 0x50000  # buffers that have to differ
 
 
 @pytest.fixture(scope="module")
@@ -19,7 +20,7 @@ def msg(lib):
     return lib.mem_last_error().decode()
 
 
-def linear(lib, x=FAKE, w=FAKE, dt=BF16, sx=None, sw=None, b=None, r=None, T=4, N=64, K=64, act=0, z=None, y=FAKE,
+def linear(lib, x=X, w=W, dt=BF16, sx=None, sw=None, b=None, r=None, T=4, N=64, K=64, act=0, z=None, y=Y,
            ydt=BF16):
     return lib.mem_linear(x, w, dt, sx, sw, b, r, T, N, K, act, z, y, ydt, None)
 
@@ -55,6 +56,11 @@ def linear(lib, x=FAKE, w=FAKE, dt=BF16, sx=None, sw=None, b=None, r=None, T=4, 
     (dict(y=FAKE + 2), INVALID, "aligned"),
     (dict(dt=E4M3, sx=FAKE + 2, sw=FAKE), INVALID, "aligned"),
     (dict(dt=E4M3, sx=FAKE, sw=FAKE + 4), INVALID, "aligned"),
+    (dict(y=X), INVALID, "an output"),
+    (dict(y=W), INVALID, "an output"),
+    (dict(z=X), INVALID, "an output"),
+    (dict(z=Y), INVALID, "an output"),
+    (dict(z=FAKE, r=FAKE), INVALID, "an output"),
 ])
 def test_linear_rejects(lib, kw, code, text):
     assert linear(lib, **kw) == code and text in msg(lib)
@@ -77,7 +83,7 @@ def test_act_backward_rejects(lib, kw, code, text):
     assert text in msg(lib)
 
 
-def bwd(lib, dz=FAKE, x=FAKE, w=FAKE, dt=BF16, T=4, N=64, K=64, add=None, dx=FAKE, gw=FAKE, gb=FAKE, ws=FAKE, n=BIG):
+def bwd(lib, dz=FAKE, x=X, w=W, dt=BF16, T=4, N=64, K=64, add=None, dx=DX, gw=FAKE, gb=FAKE, ws=FAKE, n=BIG):
     return lib.mem_linear_backward(dz, x, w, dt, T, N, K, add, dx, gw, gb, ws, n, None)
 
 
@@ -96,6 +102,9 @@ def bwd(lib, dz=FAKE, x=FAKE, w=FAKE, dt=BF16, T=4, N=64, K=64, add=None, dx=FAK
     (dict(ws=None), WORKSPACE, "workspace"),
     (dict(n=16), WORKSPACE, "workspace"),
     (dict(ws=FAKE + 64), INVALID, "256-byte"),
+    (dict(dx=FAKE), INVALID, "dx_out"),
+    (dict(dx=X), INVALID, "dx_out"),
+    (dict(dx=W), INVALID, "dx_out"),
 ])
 def test_linear_backward_rejects(lib, kw, code, text):
     assert bwd(lib, **kw) == code and text in msg(lib)

@@ -46,6 +46,7 @@ def norm(lib, x=FAKE, res=None, w=FAKE, dt=BF16, T=4, D=64, eps=1e-5, s=None, y=
     (dict(w=FAKE + 2), INVALID, "aligned"),
     (dict(res=FAKE + 4), INVALID, "aligned"),
     (dict(s=FAKE + 8), INVALID, "aligned"),
+    (dict(s=FAKE), INVALID, "one buffer"),
     (dict(ydt=E4M3, sc=FAKE + 2), INVALID, "aligned"),
 ])
 def test_norm_rejects(lib, kw, code, text):
