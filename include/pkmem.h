@@ -377,7 +377,8 @@ int mem_bag_backward_sparse(const void* dy, const void* values, pkmem_dtype v_dt
  *   sum_out [T, D] dtype dt: h; NULL to skip it.  May be x or res (in place).
  *   y_out   [T, D] dtype y_dt, which is dt, or PKMEM_E4M3: y in 8 bits with one
  *           scale a row, y ~ y_out * scale_out[t],
- *           scale = max(max_j |y| / 448, 2^-126), codes to nearest even.
+ *           scale = max(max_j |y| / 448, 2^-126), codes to nearest even.  May be
+ *           x or res where y_dt is dt (in place, without sum_out there).
  *   scale_out [T] fp32: required for PKMEM_E4M3, NULL otherwise.
  * All buffers 16-byte aligned (scale_out 4).  T = 0 is a valid no-op.
  * ------------------------------------------------------------------------ */
@@ -492,7 +493,7 @@ int mem_linear_backward(const void* dz, const void* x, const void* w, pkmem_dtyp
  * move on (lr and step are then not used).  Where *grad_scale is 0 or not
  * finite, or *step_dev below 1, the whole call changes nothing.
  * Tensors of any length (0: skipped) and alignment; 16-byte aligned ones are
- * fast.  No two may overlap.
+ * fast.  No two parameters or states may overlap (refused, by mem_adamw_rows too).
  * ------------------------------------------------------------------------ */
 typedef struct {
   void* param;

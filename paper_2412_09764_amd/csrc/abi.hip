@@ -5,6 +5,8 @@
 #include <stdlib.h>
 #include <string.h>
 
+#include <algorithm>
+
 #include <mutex>
 #include <string>
 #include <utility>
@@ -745,6 +747,41 @@ int check_adamw_tensor(const char* fn, const pkmem_adamw_tensor& t, int i, bool 
   return PKMEM_OK;
 }
 
+// Do two of the buffers that a step writes overlap?  A parameter listed twice
+// would be written by two workgroups at once.
+int check_adamw_overlap(const char* fn, const pkmem_adamw_tensor* ts, int count) {
+  struct Span { uintptr_t begin, end; int i; };
+  Span few[5 * 16];
+  Span* s = count <= 16 ? few : static_cast<Span*>(malloc(sizeof(Span) * 5 * (size_t)count));
+  if (!s) return fail(PKMEM_ERR_UNSUPPORTED, "%s: no host memory for a list of %d", fn, count);
+  size_t n = 0;
+  for (int i = 0; i < count; ++i) {
+    const pkmem_adamw_tensor& t = ts[i];
+    if (t.numel == 0) continue;
+    const bool s8 = t.state_dt == PKMEM_E4M3;
+    const size_t e = (size_t)t.numel, state = e * (s8 ? 1 : 4);
+    const size_t scale = (e + pk::ADAMW_STATE_BLOCK - 1) / pk::ADAMW_STATE_BLOCK * 4;
+    auto add = [&](const void* p, size_t bytes) {
+      s[n++] = Span{reinterpret_cast<uintptr_t>(p), reinterpret_cast<uintptr_t>(p) + bytes, i};
+    };
+    add(t.param, e * esize(t.param_dt));
+    add(t.exp_avg, state);
+    add(t.exp_avg_sq, state);
+    if (s8) {
+      add(t.exp_avg_scale, scale);
+      add(t.exp_avg_sq_scale, scale);
+    }
+  }
+  std::sort(s, s + n, [](const Span& a, const Span& b) { return a.begin < b.begin; });
+  int a = -1, b = -1;
+  for (size_t i = 1; i < n && a < 0; ++i)
+    if (s[i].begin < s[i - 1].end) a = s[i - 1].i, b = s[i].i;
+  if (s != few) free(s);
+  if (a >= 0)
+    return fail(PKMEM_ERR_INVALID, "%s: parameters or states of tensors %d and %d overlap", fn, a < b ? a : b, a < b ? b : a);
+  return PKMEM_OK;
+}
+
 }  // namespace
 
 extern "C" {
@@ -766,6 +803,9 @@ int mem_rmsnorm(const void* x, const void* res, const void* weight, pkmem_dtype 
       !aligned(y_out, 16) || !aligned(scale_out, 4))
     return fail(PKMEM_ERR_INVALID, "%s: buffers must be 16-byte aligned (scale_out 4)", fn);
   if (T == 0) return PKMEM_OK;
+  // rows of 8 bits lie over rows that other waves still read
+  if ((q && (y_out == x || y_out == res)) || y_out == weight || (sum_out && sum_out == weight))
+    return fail(PKMEM_ERR_INVALID, "%s: an output may not be weight, nor y_out in 8 bits x or res", fn);
   return hip_status(pk::launch_rmsnorm(dt == PKMEM_BF16, x, res, weight, T, D, eps, sum_out, y_out,
                                        scale_out, reinterpret_cast<hipStream_t>(stream)), fn);
 }
@@ -807,6 +847,7 @@ int mem_quantize_rows(const void* x, pkmem_dtype dt, int64_t R, int C, void* q_o
   if (!aligned(x, 16) || !aligned(q_out, 16) || !aligned(scale_out, 4))
     return fail(PKMEM_ERR_INVALID, "%s: x and q_out must be 16-byte aligned (scale_out 4)", fn);
   if (R == 0) return PKMEM_OK;
+  if (q_out == x) return fail(PKMEM_ERR_INVALID, "%s: q_out may not be x", fn);
   return hip_status(pk::launch_quantize_rows(dt == PKMEM_BF16, x, R, C, q_out, scale_out,
                                              reinterpret_cast<hipStream_t>(stream)), fn);
 }
@@ -822,6 +863,8 @@ int mem_adamw(const pkmem_adamw_tensor* tensors, int count, const pkmem_adamw_op
     rc = check_adamw_tensor(fn, tensors[i], i, true);
     if (rc) return rc;
   }
+  rc = check_adamw_overlap(fn, tensors, count);
+  if (rc) return rc;
   return hip_status(pk::launch_adamw(tensors, count, *opts, reinterpret_cast<hipStream_t>(stream)), fn);
 }
 
@@ -850,6 +893,8 @@ int mem_adamw_rows(const pkmem_adamw_tensor* table, int64_t N, int D, const int6
   if (U > 0 && !rows) return fail(PKMEM_ERR_INVALID, "%s: null pointer", fn);
   if (!aligned(rows, 8)) return fail(PKMEM_ERR_INVALID, "%s: rows must be 8-byte aligned", fn);
   if (U == 0) return PKMEM_OK;
+  rc = check_adamw_overlap(fn, table, 1);
+  if (rc) return rc;
   hipStream_t st = reinterpret_cast<hipStream_t>(stream);
   if (debug_checks()) {
     uint32_t* flag = nullptr;
@@ -903,7 +948,8 @@ int mem_linear(const void* x, const void* w, pkmem_dtype dt, const float* x_scal
     return fail(PKMEM_ERR_INVALID, "%s: buffers must be 16-byte aligned", fn);
   if (T == 0) return PKMEM_OK;
   // an output over an operand that other workgroups still read
-  if (y_out == x || y_out == w || z_out == x || z_out == w || z_out == y_out || (z_out && z_out == res))
+  if (y_out == x || y_out == w || z_out == x || z_out == w || z_out == y_out || (z_out && z_out == res) ||
+      (bias && (y_out == bias || z_out == bias)))
     return fail(PKMEM_ERR_INVALID, "%s: an output may not be an operand or the other output (y_out may be res)", fn);
   const pk::LinearCall c{x, w, dt, x_scale, w_scale, bias, res, T, N, K, act, z_out, y_out, y_dt == PKMEM_BF16};
   return hip_status(pk::launch_linear(c, reinterpret_cast<hipStream_t>(stream)), fn);
@@ -947,6 +993,8 @@ int mem_linear_backward(const void* dz, const void* x, const void* w, pkmem_dtyp
   if (T == 0 || (!dx_out && !grad_w && !grad_bias)) return PKMEM_OK;
   if (dx_out && (dx_out == dz || dx_out == x || dx_out == w))
     return fail(PKMEM_ERR_INVALID, "%s: dx_out may be dx_add, no other input", fn);
+  if (grad_w && (grad_w == dz || grad_w == x || grad_w == w || grad_w == dx_out || grad_w == grad_bias || grad_w == dx_add))
+    return fail(PKMEM_ERR_INVALID, "%s: grad_w may be no other buffer", fn);
   return hip_status(pk::launch_linear_backward(dt == PKMEM_BF16, dz, x, w, T, N, K, dx_add, dx_out,
                                                grad_w, grad_bias, ws,
                                                reinterpret_cast<hipStream_t>(stream)), fn);

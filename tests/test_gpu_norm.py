@@ -158,3 +158,32 @@ def test_empty_and_refusals(gpu_lib):
         pk.mem_rmsnorm_backward(x, x, grad_weight=torch.zeros(63, device="cuda"))
     with pytest.raises(ValueError):
         pk.mem_rmsnorm_backward(x, x, workspace=torch.empty(16, dtype=torch.uint8, device="cuda"))
+
+
+@pytest.mark.parametrize("dt", DTS, ids=["f32", "bf16"])
+@pytest.mark.parametrize("T,D", [(1, 8), (33, 2056), (257, 512), (3, 8192)])
+def test_norm_in_place(gpu_lib, T, D, dt):
+    x, r = _x(T, D, dt, 11).cuda(), _x(T, D, dt, 12).cuda()
+    w = torch.linspace(0.5, 1.5, D).to(dt).cuda()
+    want, _, _ = pk.mem_rmsnorm(x, w)
+    both, h, _ = pk.mem_rmsnorm(x, w, r)
+    a = x.clone()
+    assert torch.equal(pk.mem_rmsnorm(a, w, y_out=a)[0], want)
+    b, c = x.clone(), r.clone()
+    pk.mem_rmsnorm(b, w, c, sum_out=b, y_out=c)
+    assert torch.equal(b, h) and torch.equal(c, both)
+
+
+def test_outputs_over_inputs_are_refused(gpu_lib):
+    x = torch.zeros((4, 64), device="cuda")
+    with pytest.raises(pk.PkmemError):
+        pk.mem_rmsnorm(x, quantize=True, y_out=x.view(torch.float8_e4m3fn).view(-1)[:256].view(4, 64))
+    with pytest.raises(pk.PkmemError):
+        pk.mem_quantize_rows(x, q_out=x.view(torch.float8_e4m3fn).view(-1)[:256].view(4, 64))
+    g, m, v = (torch.zeros_like(x) for _ in range(3))
+    with pytest.raises(pk.PkmemError):  # a parameter listed twice
+        pk.mem_adamw([x, x], [g, g], [m, m.clone()], [v, v.clone()], lr=1e-3, step=1)
+    with pytest.raises(pk.PkmemError):  # views that share an element
+        f = x.view(-1)
+        cut = lambda t: [t.clone().view(-1)[:100], t.clone().view(-1)[:157]]  # noqa: E731
+        pk.mem_adamw([f[:100], f[99:]], cut(g), cut(m), cut(v), lr=1e-3, step=1)
