@@ -8,7 +8,7 @@
 // a wave per row up to 8 KiB, four waves above.  Memory bound: two reads and
 // two writes per element with the residual, three reads and one write in the
 // backward.  32768 rows of 2048 bf16: forward with residual 78-80 us (6.7 TB/s), to
-// 8 bits 74 (6.3), backward 83 (6.5); four waves a row are no faster there and
+// 8 bits 78 (6.0), backward 83 (6.5); four waves a row are no faster there and
 // slower in the backward (118 us).  Below some 4000 rows a call is bound by its
 // launch (2000 rows: 5 us of kernel).
 #include "pk_internal.h"
@@ -49,7 +49,10 @@ __device__ __forceinline__ float rms_rstd(float ss, int D, float eps) {
 
 // NORM: the norm, else y = x (rows to 8 bits only).  QUANT: y in e4m3 with
 // scale_out[row] = max(max|y| / 448, 2^-126); the lower limit keeps 1 / scale
-// finite, a row of zeros is codes of zero.
+// finite, a row of zeros is codes of zero.  rstd cancels in y / scale, so the codes
+// are those of u = h w (times the power of two of rstd, which keeps it in range)
+// over max|u| / 448: (0.875 u) / (max|u| / 512), where bf16 operands make both
+// sides exact and a value half way between two codes stays there.
 template <typename T, bool NORM, bool QUANT, int NCH, int WPR>
 __global__ __launch_bounds__(BLOCK) void k_rmsnorm(const T* x, const T* res,
                                                    const T* __restrict__ w, int64_t rows, int D,
@@ -90,8 +93,14 @@ __global__ __launch_bounds__(BLOCK) void k_rmsnorm(const T* x, const T* res,
       for (int i = 0; i < N; ++i) ss = fmaf(h[c][i], h[c][i], ss);
     }
   }
+  float mant = 1.f;  // QUANT: y = u * mant
   if constexpr (NORM) {
-    const float rstd = rms_rstd(row_sum<WPR>(ss, red, wave), D, eps);
+    float rstd = rms_rstd(row_sum<WPR>(ss, red, wave), D, eps);
+    if constexpr (QUANT) {
+      const uint32_t bits = __float_as_uint(rstd);
+      mant = __uint_as_float((bits & 0x7FFFFFu) | 0x3F800000u);
+      if (rstd == rstd) rstd = __uint_as_float(bits & 0x7F800000u);
+    }
 #pragma unroll
     for (int c = 0; c < NCH; ++c) {
       const int ch = lr + c * LANES;
@@ -117,9 +126,14 @@ __global__ __launch_bounds__(BLOCK) void k_rmsnorm(const T* x, const T* res,
 #pragma unroll
       for (int i = 0; i < N; ++i) am = fmaxf(am, fabsf(h[c][i]));
     am = row_max<WPR>(am, red, wave);
-    const float s = fmaxf(am * (1.f / E4M3_MAX), 0x1p-126f);
-    if (lr == 0) scale_out[row] = s;
-    const float inv = 1.f / s;
+    const float s = am * mant / E4M3_MAX;
+    const bool low = !(s >= 0x1p-126f);  // the codes are then y / 2^-126
+    if (lr == 0) scale_out[row] = low ? 0x1p-126f : s;
+    const float up = low ? mant : 0.875f, div = low ? 0x1p-126f : am * 0x1p-9f, inv = 1.f / div;
+    auto code = [&](float u) {  // u * up / div, correctly rounded
+      const float n = u * up, q = n * inv;
+      return fmaf(fmaf(-q, div, n), inv, q);
+    };
 #pragma unroll
     for (int c = 0; c < NCH; ++c) {
       const int ch = lr + c * LANES;
@@ -127,7 +141,7 @@ __global__ __launch_bounds__(BLOCK) void k_rmsnorm(const T* x, const T* res,
       uint32_t* out = reinterpret_cast<uint32_t*>((uint8_t*)y_out + base + (size_t)ch * N);
 #pragma unroll
       for (int i = 0; i < N; i += 4)
-        out[i / 4] = to_e4m3x4(h[c][i] * inv, h[c][i + 1] * inv, h[c][i + 2] * inv, h[c][i + 3] * inv);
+        out[i / 4] = to_e4m3x4(code(h[c][i]), code(h[c][i + 1]), code(h[c][i + 2]), code(h[c][i + 3]));
     }
   }
 }

@@ -1,0 +1,88 @@
+"""Rows in 8 bits, code by code.  The scale is max|y| / 448 and a code the e4m3
+number nearest to y / scale = 448 y / max|y|, ties to the even code.  In bf16 rows
+448 y is exact in 64 bits (and in 32), so a quotient half way between two codes is
+seen as such: every code has to be equal, ties among them.  fp32 rows round twice
+(2 u, u = 2^-24, of a quotient) and may differ where a quotient lies that near to
+the middle of two codes."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2412_09764_amd as pk
+from oracle import block_oracle as bo
+
+pytestmark = pytest.mark.gpu
+
+SHAPES = [(64, 8), (50, 264), (300, 2048), (40, 4104), (20, 8192)]
+
+
+def f64(t):
+    return t.detach().cpu().double().numpy()
+
+
+def rows(T, D, dt, seed):
+    """Rows of few mantissa bits (many quotients are ties), of any, of zeros, and of one number."""
+    g = torch.Generator().manual_seed(seed)
+    x = torch.randn((T, D), generator=g)
+    x[::3] = torch.randint(-56, 57, x[::3].shape, generator=g).float() * 0.375
+    x[1] = 0
+    x[2] = 0
+    x[2, D // 3] = -7.3
+    return x.to(dt)
+
+
+def check(q, s, u, exact):
+    """u: what is coded, up to a factor of the row, in 64 bits."""
+    top = np.abs(u).max(-1)
+    some = top > 0
+    t = 448 * u[some] / top[some, None]
+    want, got = bo.to_e4m3(t), f64(q)[some]
+    assert not f64(q)[~some].any() and np.all(f64(s)[~some] == 2.0 ** -126)
+    if exact:
+        assert np.array_equal(got, want)
+    else:
+        below, above = bo.to_e4m3(t * (1 - 2.0 ** -22)), bo.to_e4m3(np.clip(t * (1 + 2.0 ** -22), -448, 448))
+        assert np.all((got == want) | (got == below) | (got == above))
+        assert np.mean(got != want) < 1e-3
+
+
+@pytest.mark.parametrize("dt", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("T,D", SHAPES)
+def test_quantize_rows(gpu_lib, T, D, dt):
+    x = rows(T, D, dt, 1)
+    q, s = pk.mem_quantize_rows(x.cuda())
+    check(q, s, f64(x), dt == torch.bfloat16)
+    want = np.maximum(np.abs(f64(x)).max(-1) / 448, 2.0 ** -126).astype(np.float32)
+    assert np.array_equal(s.cpu().numpy(), want)  # one division, rounded once
+
+
+@pytest.mark.parametrize("weighted", [False, True])
+@pytest.mark.parametrize("dt", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("T,D", SHAPES)
+def test_norm(gpu_lib, T, D, dt, weighted):
+    x, r = rows(T, D, dt, 2), rows(T, D, dt, 3)
+    w = (1 + 0.25 * torch.randint(-2, 3, (D,), generator=torch.Generator().manual_seed(4))).to(dt) if weighted else None
+    q, h, s = pk.mem_rmsnorm(x.cuda(), None if w is None else w.cuda(), r.cuda(), quantize=True)
+    u = f64(h) * (f64(w) if weighted else 1.0)
+    check(q, s, u, dt == torch.bfloat16)
+    y = bo.rmsnorm(f64(h), f64(w) if weighted else 1.0, 1e-5)
+    want = np.maximum(np.abs(y).max(-1) / 448, 2.0 ** -126)
+    # 76 u of the mean square count half in its root, which adds 3 u; three roundings more
+    assert np.all(np.abs(f64(s) - want) <= 44 * 2.0 ** -24 * want)
+
+
+def test_sizes_at_the_ends_of_fp32(gpu_lib):
+    """Rows near the largest and smallest numbers keep finite scales; below 448 * 2^-126 the
+    scale stays at 2^-126 and the codes get small."""
+    base = torch.tensor([1.0, -0.5, 0.25, 1 / 3, -1 / 7, 0.0, 0.01, 0.75])
+    sizes = [3e38, 1e37, 1e20, 1.0, 1e-20, 1e-35, 3e-36, 1e-37, 2e-38]
+    x = torch.stack([base * v for v in sizes])
+    q, s = pk.mem_quantize_rows(x.cuda())
+    sw = np.maximum(np.abs(f64(x)).max(-1) / 448, 2.0 ** -126)
+    assert np.all(np.abs(f64(s) - sw) <= 2.0 ** -24 * sw)
+    err = np.abs(f64(q) * f64(s)[:, None] - f64(x))
+    assert np.all(err <= (2.0 ** -4 + 2.0 ** -21) * np.abs(f64(x)) + 2.0 ** -10 * sw[:, None])
+    n, _, sn = pk.mem_rmsnorm(x[2:7].cuda(), eps=0.0, quantize=True)
+    big = pk.mem_rmsnorm((x[3:4] * 1e18).cuda(), torch.full((8,), 1e18, device="cuda"), eps=0.0, quantize=True)
+    for codes, scale in ((n, sn), (big[0], big[2])):
+        assert torch.isfinite(codes.float()).all() and torch.isfinite(scale).all() and torch.all(scale > 0)
