@@ -84,7 +84,7 @@ def test_norm_eps_zero_and_tiny(gpu_lib):
     assert not q[0].float().any() and float(s[0]) == 2.0 ** -126
 
 
-def test_norm_in_place(gpu_lib):
+def test_norm_and_gradient_in_place(gpu_lib):
     x, r = _x(70, 1032, torch.bfloat16, 7).cuda(), _x(70, 1032, torch.bfloat16, 8).cuda()
     y, h, _ = pk.mem_rmsnorm(x, None, r)
     for into in (x.clone(), r.clone()):
