@@ -285,15 +285,25 @@ __global__ __launch_bounds__(1024) void k_add_rows(const float* __restrict__ par
     else { F(8, 4); }                                                     \
   } while (0)
 
+// One launch holds fewer than 2^32 threads: more rows go in several.
+constexpr int64_t LAUNCH_WORKGROUPS = 1 << 23;
+
 template <typename T, bool NORM, bool QUANT>
 void norm_launch(const void* x, const void* res, const void* w, int64_t rows, int D, float eps,
                  void* sum_out, void* y_out, float* scale_out, hipStream_t st) {
   const int C = D / Chunk<T>::N;
-#define PK_F(NCH, WPR)                                                                           \
-  hipLaunchKernelGGL((k_rmsnorm<T, NORM, QUANT, NCH, WPR>),                                      \
-                     dim3((unsigned)(WPR == 1 ? (rows + 3) / 4 : rows)), dim3(BLOCK), 0, st,     \
-                     (const T*)x, (const T*)res, (const T*)w, rows, D, eps, (T*)sum_out, y_out,  \
-                     scale_out)
+  auto slice = [&](auto* p, int64_t row) { return p ? p + (size_t)row * D : p; };
+#define PK_F(NCH, WPR)                                                                             \
+  constexpr int64_t per_wg = WPR == 1 ? 4 : 1, most = per_wg * LAUNCH_WORKGROUPS;                  \
+  for (int64_t r = 0; r < rows; r += most) {                                                       \
+    const int64_t n = rows - r < most ? rows - r : most;                                           \
+    hipLaunchKernelGGL((k_rmsnorm<T, NORM, QUANT, NCH, WPR>),                                      \
+                       dim3((unsigned)((n + per_wg - 1) / per_wg)), dim3(BLOCK), 0, st,            \
+                       slice((const T*)x, r), slice((const T*)res, r), (const T*)w, n, D, eps,     \
+                       slice((T*)sum_out, r),                                                      \
+                       (void*)slice((char*)y_out, r * (QUANT ? 1 : (int64_t)sizeof(T))),           \
+                       QUANT ? scale_out + r : nullptr);                                           \
+  }
   PK_NORM_DISPATCH(C, PK_F);
 #undef PK_F
 }
