@@ -38,6 +38,8 @@ constexpr int UNIT = ADAMW_STATE_BLOCK;           // 128 elements: 16 lanes
 constexpr int UNIT_LANES = UNIT / LANE_ELEMS;
 constexpr int WG_UNITS = BLOCK / UNIT_LANES;      // units per workgroup and pass
 constexpr int PASSES = 2;                         // passes of a workgroup
+// Workgroups of one launch, which holds fewer than 2^32 threads.
+constexpr uint64_t LAUNCH_WORKGROUPS = (1 << 24) - 1;
 
 struct Tensor {
   void* p;
@@ -73,6 +75,7 @@ struct RowArgs {
   const int64_t* rows;
   int64_t U, N;
   int D, per_row;  // per_row = ceil(D / 128)
+  uint32_t first;  // first unit of this launch
 };
 
 __host__ __device__ __forceinline__ uint32_t mix32(uint32_t x) {
@@ -334,7 +337,7 @@ __global__ __launch_bounds__(BLOCK) void k_adamw_rows(const RowArgs a) {
   uint32_t key;
   if (!scalars(a, c, gs, key, &sc, &skey)) return;
   const uint32_t units = (uint32_t)a.U * (uint32_t)a.per_row;  // below 2^31
-  uint32_t unit = blockIdx.x * (WG_UNITS * PASSES) + threadIdx.x / UNIT_LANES;
+  uint32_t unit = a.first + blockIdx.x * (WG_UNITS * PASSES) + threadIdx.x / UNIT_LANES;
 #pragma unroll
   for (int s = 0; s < PASSES; ++s, unit += WG_UNITS) {
     if (unit >= units) break;
@@ -456,13 +459,17 @@ hipError_t launch_adamw_rows(const pkmem_adamw_tensor& t, int64_t N, int D, cons
   a.N = N;
   a.D = D;
   a.per_row = (D + UNIT - 1) / UNIT;
-  const uint64_t units = (uint64_t)U * a.per_row;
-  const dim3 grid((unsigned)((units + WG_UNITS * PASSES - 1) / (WG_UNITS * PASSES))), block(BLOCK);
   const bool p16 = t.param_dt == PKMEM_BF16, s8 = t.state_dt == PKMEM_E4M3;
-  if (p16 && s8) hipLaunchKernelGGL((k_adamw_rows<uint16_t, true>), grid, block, 0, st, a);
-  else if (p16) hipLaunchKernelGGL((k_adamw_rows<uint16_t, false>), grid, block, 0, st, a);
-  else if (s8) hipLaunchKernelGGL((k_adamw_rows<float, true>), grid, block, 0, st, a);
-  else hipLaunchKernelGGL((k_adamw_rows<float, false>), grid, block, 0, st, a);
+  const uint64_t units = (uint64_t)U * a.per_row, most = LAUNCH_WORKGROUPS * WG_UNITS * PASSES;
+  for (uint64_t first = 0; first < units; first += most) {
+    const uint64_t n = units - first < most ? units - first : most;
+    const dim3 grid((unsigned)((n + WG_UNITS * PASSES - 1) / (WG_UNITS * PASSES))), block(BLOCK);
+    a.first = (uint32_t)first;
+    if (p16 && s8) hipLaunchKernelGGL((k_adamw_rows<uint16_t, true>), grid, block, 0, st, a);
+    else if (p16) hipLaunchKernelGGL((k_adamw_rows<uint16_t, false>), grid, block, 0, st, a);
+    else if (s8) hipLaunchKernelGGL((k_adamw_rows<float, true>), grid, block, 0, st, a);
+    else hipLaunchKernelGGL((k_adamw_rows<float, false>), grid, block, 0, st, a);
+  }
   return hipGetLastError();
 }
 
