@@ -492,8 +492,8 @@ int mem_linear_backward(const void* dz, const void* x, const void* w, pkmem_dtyp
  * read when the call runs, so a captured step can be replayed while they
  * move on (lr and step are then not used).  Where *grad_scale is 0 or not
  * finite, or *step_dev below 1, the whole call changes nothing.
- * Tensors of any length (0: skipped) and alignment; 16-byte aligned ones are
- * fast.  No two parameters or states may overlap (refused, by mem_adamw_rows too).
+ * Tensors of any length up to 2^36 - 2^12 (0: skipped) and any alignment; 16-byte
+ * aligned ones are fast.  No two parameters or states may overlap (refused, by mem_adamw_rows too).
  * ------------------------------------------------------------------------ */
 typedef struct {
   void* param;

@@ -862,6 +862,8 @@ int mem_adamw(const pkmem_adamw_tensor* tensors, int count, const pkmem_adamw_op
   for (int i = 0; i < count; ++i) {
     rc = check_adamw_tensor(fn, tensors[i], i, true);
     if (rc) return rc;
+    if (tensors[i].numel > pk::ADAMW_MAX_NUMEL)
+      return fail(PKMEM_ERR_UNSUPPORTED, "%s: tensor %d: more than 2^36 - 2^12 elements", fn, i);
   }
   rc = check_adamw_overlap(fn, tensors, count);
   if (rc) return rc;

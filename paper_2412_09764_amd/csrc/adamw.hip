@@ -40,6 +40,7 @@ constexpr int WG_UNITS = BLOCK / UNIT_LANES;      // units per workgroup and pas
 constexpr int PASSES = 2;                         // passes of a workgroup
 // Workgroups of one launch, which holds fewer than 2^32 threads.
 constexpr uint64_t LAUNCH_WORKGROUPS = (1 << 24) - 1;
+static_assert(ADAMW_MAX_NUMEL == LAUNCH_WORKGROUPS * WG_UNITS * PASSES * UNIT, "a tensor fits one launch");
 
 struct Tensor {
   void* p;
@@ -433,7 +434,7 @@ hipError_t launch_adamw(const pkmem_adamw_tensor* tensors, int count, const pkme
         continue;
       const uint64_t units = ((uint64_t)t.numel + UNIT - 1) / UNIT;
       const uint64_t need = (units + WG_UNITS * PASSES - 1) / (WG_UNITS * PASSES);
-      if (a.count == MAX_TENSORS || blocks + need > 0x7FFFFFFFull) {
+      if (a.count == MAX_TENSORS || blocks + need > LAUNCH_WORKGROUPS) {
         const hipError_t e = flush();
         if (e != hipSuccess) return e;
       }

@@ -174,6 +174,8 @@ hipError_t launch_linear_backward(bool bf16, const void* dz, const void* x, cons
 
 // ---- optimizer (adamw.hip) -------------------------------------------------
 constexpr int ADAMW_STATE_BLOCK = 128;  // elements that share the scales of 8-bit states
+// Elements of one tensor of mem_adamw: as many as one launch takes, about 2^36.
+constexpr int64_t ADAMW_MAX_NUMEL = ((int64_t(1) << 24) - 1) * 4096;
 // A step's scalars in the precision that the kernels use them in.
 struct AdamwScalars {
   float beta1, rest1, beta2, rest2, eps, decay, rate, root2;
