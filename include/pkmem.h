@@ -430,8 +430,8 @@ int mem_quantize_rows(const void* x, pkmem_dtype dt, int64_t R, int C, void* q_o
  *   z_out   [T, N] dtype y_dt: z (what mem_act_backward needs); NULL to skip it.
  *   y_out   [T, N] dtype y_dt; may be res (in place), no other buffer (an output
  *           that starts where an operand does is refused).
- *   N % 8 == 0; K % 8 == 0 (PKMEM_E4M3: K % 16 == 0); N, K <= 2^20; any T
- *   below 2^31.  All buffers 16-byte aligned.  T = 0 is a valid no-op.
+ *   N % 8 == 0; K % 8 == 0 (PKMEM_E4M3: K % 16 == 0); N, K <= 2^20; T < 2^31 and
+ *   ceil(T / 256) * ceil(N / 256) < 2^23.  All buffers 16-byte aligned.  T = 0 is a valid no-op.
  * ------------------------------------------------------------------------ */
 typedef enum {
   PKMEM_ACT_NONE = 0,
@@ -460,7 +460,8 @@ int mem_act_backward(const void* dy, const void* z, pkmem_dtype dt, int act, int
  *   grad_bias [N] fp32, ACCUMULATED: += sum_t dz.
  * Each output may be NULL.  (The gradient of the forward's res is dy itself.)
  * Bitwise deterministic: the tokens are split by their number alone and the
- * parts added in order.  Limits as mem_linear's.  Workspace:
+ * parts added in order.  Limits as mem_linear's, with K in place of N in the
+ * last one and N in place of T too.  Workspace:
  * mem_linear_backward_workspace_size(T, N, K, dt) bytes, 256-byte aligned.
  * ------------------------------------------------------------------------ */
 size_t mem_linear_backward_workspace_size(int64_t T, int N, int K, pkmem_dtype dt);

@@ -914,6 +914,9 @@ int mem_adamw_rows(const pkmem_adamw_tensor* table, int64_t N, int D, const int6
 
 namespace {
 
+// A product with rows x cols results, in 256-wide tiles of 512 threads: fewer than 2^32 a launch.
+bool tiles_fit(int64_t rows, int cols) { return (rows + 255) / 256 * ((cols + 255) / 256) < (int64_t(1) << 23); }
+
 int check_linear_shapes(const char* fn, pkmem_dtype dt, bool e4m3, int64_t T, int N, int K) {
   if (!dtype_ok(dt) && !(e4m3 && dt == PKMEM_E4M3)) return fail(PKMEM_ERR_INVALID, "%s: unknown dtype %d", fn, (int)dt);
   if (T < 0) return fail(PKMEM_ERR_INVALID, "%s: T must be >= 0", fn);
@@ -922,9 +925,6 @@ int check_linear_shapes(const char* fn, pkmem_dtype dt, bool e4m3, int64_t T, in
   if (N < 8 || N % 8 != 0) return fail(PKMEM_ERR_UNSUPPORTED, "%s: N must be a positive multiple of 8 (got %d)", fn, N);
   if (K < ka || K % ka != 0) return fail(PKMEM_ERR_UNSUPPORTED, "%s: K must be a positive multiple of %d (got %d)", fn, ka, K);
   if (N > (1 << 20) || K > (1 << 20)) return fail(PKMEM_ERR_UNSUPPORTED, "%s: N and K must be <= 2^20", fn);
-  // 128 x 128 tiles of the largest grid, and what split products add to it
-  if (((T + 127) / 128) * ((int64_t)(N > K ? N : K) / 128 + 1) > (int64_t(1) << 30))
-    return fail(PKMEM_ERR_UNSUPPORTED, "%s: too many tiles", fn);
   return PKMEM_OK;
 }
 
@@ -938,6 +938,7 @@ int mem_linear(const void* x, const void* w, pkmem_dtype dt, const float* x_scal
   const char* fn = "mem_linear";
   int rc = check_linear_shapes(fn, dt, true, T, N, K);
   if (rc) return rc;
+  if (!tiles_fit(T, N)) return fail(PKMEM_ERR_UNSUPPORTED, "%s: 2^23 tiles of 256 x 256 or more", fn);
   if (!dtype_ok(y_dt) || (dt == PKMEM_F32 && y_dt != PKMEM_F32))
     return fail(PKMEM_ERR_INVALID, "%s: y_dt must be PKMEM_F32 or PKMEM_BF16 (PKMEM_F32 for fp32 operands)", fn);
   if (act < PKMEM_ACT_NONE || act > PKMEM_ACT_GELU) return fail(PKMEM_ERR_INVALID, "%s: unknown activation %d", fn, act);
@@ -984,6 +985,7 @@ int mem_linear_backward(const void* dz, const void* x, const void* w, pkmem_dtyp
   const char* fn = "mem_linear_backward";
   int rc = check_linear_shapes(fn, dt, false, T, N, K);
   if (rc) return rc;
+  if (!tiles_fit(T, K) || !tiles_fit(N, K)) return fail(PKMEM_ERR_UNSUPPORTED, "%s: 2^23 tiles of 256 x 256 or more", fn);
   if (T > 0 && (!dz || (dx_out && !w) || (grad_w && !x))) return fail(PKMEM_ERR_INVALID, "%s: null pointer", fn);
   if (!aligned(dz, 16) || !aligned(x, 16) || !aligned(w, 16) || !aligned(dx_add, 16) ||
       !aligned(dx_out, 16) || !aligned(grad_w, 16) || !aligned(grad_bias, 4))

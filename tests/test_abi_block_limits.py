@@ -29,3 +29,24 @@ def test_adamw_elements(lib, numel, rc, at):
     assert lib.mem_adamw(ctypes.addressof(ts), 2, ctypes.addressof(o), None) == rc
     if rc == UNSUPPORTED:
         assert f"tensor {at}" in lib.mem_last_error().decode()
+
+
+P = [1 << e for e in range(40, 47)]  # far apart
+
+
+@pytest.mark.parametrize("T,N,K,rc", [
+    ((1 << 31) - 256, 256, 8, HIP), ((1 << 31) - 255, 8, 8, UNSUPPORTED), ((1 << 31) - 1, 8, 1 << 20, UNSUPPORTED),
+    (1 << 30, 512, 8, UNSUPPORTED), ((1 << 30) - 256, 512, 8, HIP), (1 << 30, 8, 1 << 10, HIP)])
+@pytest.mark.parametrize("dt", [F32, BF16])
+def test_linear_tiles(lib, T, N, K, rc, dt):
+    assert lib.mem_linear(P[0], P[1], dt, None, None, None, None, T, N, K, 0, None, P[2], dt, None) == rc
+    assert rc != UNSUPPORTED or "tiles" in lib.mem_last_error().decode()
+
+
+@pytest.mark.parametrize("T,N,K,rc", [
+    ((1 << 31) - 256, 8, 256, HIP), ((1 << 31) - 255, 8, 8, UNSUPPORTED), (1 << 30, 8, 512, UNSUPPORTED),
+    (64, 1 << 20, 1 << 20, UNSUPPORTED), (64, 1 << 20, 1 << 19, UNSUPPORTED), (64, 1 << 19, (1 << 20) - 256, HIP)])
+@pytest.mark.parametrize("dt", [F32, BF16])
+def test_linear_backward_tiles(lib, T, N, K, rc, dt):
+    assert lib.mem_linear_backward(P[0], P[1], P[2], dt, T, N, K, None, P[3], P[4], P[5], P[6], 1 << 45, None) == rc
+    assert rc != UNSUPPORTED or "tiles" in lib.mem_last_error().decode()
