@@ -14,16 +14,22 @@ inline int ceil_div(int64_t a, int64_t b) { return (int)((a + b - 1) / b); }
 enum { TILE_256, TILE_128, TILE_128_K2, TILE_64, TILE_32 };
 constexpr int tile_size(int t) { return t == TILE_256 ? 256 : t == TILE_64 ? 64 : t == TILE_32 ? 32 : 128; }
 inline int64_t tile_count(int t, int64_t M, int64_t N) { return (int64_t)ceil_div(M, tile_size(t)) * ceil_div(N, tile_size(t)); }
-// The largest tiles that are enough to fill the chip, but none twice as high as
-// the rows there are; the smallest where one round of them does (two in fp32:
-// 300 x 1024 x 1024 takes 14.8 us in them and 16.5 in tiles of 64).  2048 x 2048 bf16: 128 rows 7.2 us in tiles of
-// 32 and 8.9 of 64, 256 rows 12.8 and 9.6; 512 rows 12.1 in 64 and 15.1 in 128,
-// 1024 rows 23.7 and 16.7, 2048 25 (K2), 4096 42 in 128 and 47.6 in 256, 8192 83 and 63.
+// The largest tiles that are enough to fill the chip; the smallest where one round
+// of them does (two in fp32: 300 x 1024 x 1024 takes 14.8 us in them and 16.5 in
+// tiles of 64).  2048 x 2048 bf16: 128 rows 7.2 us in tiles of 32 and 8.9 of 64, 256
+// rows 12.8 and 9.6; 512 rows 12.1 in 64 and 15.1 in 128, 1024 rows 23.7 and 16.7,
+// 2048 25 (K2), 4096 42 in 128 and 47.6 in 256, 8192 83 and 63.
+// Rows that leave half of a 256-wide tile empty take narrower ones: 128 x 131072 x 256
+// 35.7 us in 256 and 24.3 in 128, 65 x 51200 x 1024 24.4 and 23.3, fp32 137.9 and 78.
+// Up to 64 rows the same holds of 128 until there are many tiles: 64 x 16384 x 2048
+// 17.7 us in 64 and 20.5 in 128, 64 x 32768 x 2048 32.0 and 25.6; fp32 64 x 32768 x 2048
+// 68 and 90, 64 x 51200 x 1024 70 and 78, 64 x 131072 x 256 64 and 49.
 inline int pick_tile(bool f32, int64_t M, int64_t N) {
   if (tile_count(TILE_32, M, N) <= (f32 ? 512 : 256)) return TILE_32;
-  if (tile_count(TILE_256, M, N) >= 200) return TILE_256;
+  if (M > 128 && tile_count(TILE_256, M, N) >= 200) return TILE_256;
   const int64_t mid = tile_count(TILE_128, M, N);
-  return M <= 64 || mid < 128 ? TILE_64 : mid <= 256 ? TILE_128_K2 : TILE_128;
+  if (mid < 128 || (M <= 64 && mid <= (f32 ? 512 : 192))) return TILE_64;
+  return mid <= 256 ? TILE_128_K2 : TILE_128;
 }
 
 // grad_W [N, K] from T tokens: the tile and the number of splits of the tokens

@@ -30,3 +30,14 @@ def test_every_kernel_is_reached(plan):
     wanted |= {("grad_w", dt, t, split) for dt in types for t in TILES if t != "128" for split in (False, True)}
     assert not wanted - reached, sorted(wanted - reached)
     assert not reached - wanted, sorted(reached - wanted)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "e4m3"])
+def test_few_rows_of_wide_products(plan, dtype):
+    """No 256-wide tiles for up to 128 rows, and 128-wide ones for up to 64 only where a wide
+    product has more than 192 of them."""
+    for M in (9, 16, 33, 64, 65, 100, 128, 129, 200):
+        for N in (8, 2048, 16384, 24576, 25608, 51200, 131072, 1 << 20):
+            tile = plan.product(dtype, M, N)
+            assert tile != "256" or M > 128, (M, N)
+            assert not tile.startswith("128") or M > 64 or -(-N // 128) > 192, (M, N)
