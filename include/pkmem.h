@@ -380,7 +380,8 @@ int mem_bag_backward_sparse(const void* dy, const void* values, pkmem_dtype v_dt
  *           scale = max(max_j |y| / 448, 2^-126), codes to nearest even.  May be
  *           x or res where y_dt is dt (in place, without sum_out there).
  *   scale_out [T] fp32: required for PKMEM_E4M3, NULL otherwise.
- * All buffers 16-byte aligned (scale_out 4).  T = 0 is a valid no-op.
+ * All buffers 16-byte aligned (scale_out 4).  An output that shares bytes with
+ * another buffer in any other way is refused.  T = 0 is a valid no-op.
  * ------------------------------------------------------------------------ */
 int mem_rmsnorm(const void* x, const void* res, const void* weight, pkmem_dtype dt, int64_t T,
                 int D, float eps, void* sum_out, void* y_out, pkmem_dtype y_dt, float* scale_out,
@@ -391,6 +392,7 @@ int mem_rmsnorm(const void* x, const void* res, const void* weight, pkmem_dtype 
  * (recomputed from h as the forward did) and g = dy * weight:
  *   dx_out      [T, D] dtype dt, written: rstd * (g - xh * mean(g * xh)) + dsum;
  *               the gradient of x and of res alike.  May be dy, h or dsum.
+ *               Outputs and workspace that share other bytes are refused.
  *   grad_weight [D] fp32, ACCUMULATED: += sum_t dy * xh; NULL to skip it.
  *               Bitwise deterministic (partial rows added in a fixed order).
  *   dy, h       [T, D] dtype dt: the gradient of y; x (without res) or sum_out.
@@ -407,7 +409,8 @@ int mem_rmsnorm_backward(const void* dy, const void* h, const void* weight, pkme
 /* ------------------------------------------------------------------------ *
  * Rows in 8 bits: q_out [R, C] PKMEM_E4M3 and scale_out [R] fp32 of
  * x [R, C] dtype dt, as mem_rmsnorm writes them (for weights and activations
- * of mem_linear's 8-bit products).  C % 8 == 0, rows of at most 32 KiB.
+ * of mem_linear's 8-bit products).  C % 8 == 0, rows of at most 32 KiB.  No two
+ * buffers may share bytes (refused).
  * ------------------------------------------------------------------------ */
 int mem_quantize_rows(const void* x, pkmem_dtype dt, int64_t R, int C, void* q_out,
                       float* scale_out, pkmem_stream_t stream);

@@ -6,7 +6,7 @@
 #include <string.h>
 
 #include <algorithm>
-
+#include <initializer_list>
 #include <mutex>
 #include <string>
 #include <utility>
@@ -704,6 +704,26 @@ namespace {
 
 constexpr size_t NORM_ROW_BYTES = 32 << 10;  // a row fits the registers of one workgroup
 
+struct Bytes {
+  const void* p;
+  size_t n;
+};
+
+bool share(const Bytes& a, const Bytes& b) {
+  const uintptr_t x = reinterpret_cast<uintptr_t>(a.p), y = reinterpret_cast<uintptr_t>(b.p);
+  return x && y && a.n && b.n && x < y + b.n && y < x + a.n;
+}
+
+// Does an output share bytes with one of the buffers `apart`, or with one of `in_place`
+// that it is not itself?  Other workgroups may still read what it would overwrite.
+bool over(const Bytes& out, std::initializer_list<Bytes> apart, std::initializer_list<Bytes> in_place = {}) {
+  for (const Bytes& b : apart)
+    if (share(out, b)) return true;
+  for (const Bytes& b : in_place)
+    if (share(out, b) && !(out.p == b.p && out.n == b.n)) return true;
+  return false;
+}
+
 int check_rows_shape(const char* fn, pkmem_dtype dt, int64_t T, int D) {
   if (!dtype_ok(dt)) return fail(PKMEM_ERR_INVALID, "%s: unknown dtype %d", fn, (int)dt);
   if (T < 0) return fail(PKMEM_ERR_INVALID, "%s: the number of rows must be >= 0", fn);
@@ -803,9 +823,11 @@ int mem_rmsnorm(const void* x, const void* res, const void* weight, pkmem_dtype 
       !aligned(y_out, 16) || !aligned(scale_out, 4))
     return fail(PKMEM_ERR_INVALID, "%s: buffers must be 16-byte aligned (scale_out 4)", fn);
   if (T == 0) return PKMEM_OK;
-  // rows of 8 bits lie over rows that other waves still read
-  if ((q && (y_out == x || y_out == res)) || y_out == weight || (sum_out && sum_out == weight))
-    return fail(PKMEM_ERR_INVALID, "%s: an output may not be weight, nor y_out in 8 bits x or res", fn);
+  const size_t rows = (size_t)T * D * esize(dt);
+  const Bytes bx{x, rows}, br{res, rows}, bw{weight, D * esize(dt)}, bs{sum_out, rows}, bc{scale_out, (size_t)T * 4},
+      by{y_out, q ? (size_t)T * D : rows};
+  if (over(bs, {bw, by, bc}, {bx, br}) || over(by, {bw, bc}, {bx, br}) || over(bc, {bx, br, bw}))
+    return fail(PKMEM_ERR_INVALID, "%s: an output may not be weight or share bytes with another buffer (but be x or res itself, y_out in 8 bits not even that)", fn);
   return hip_status(pk::launch_rmsnorm(dt == PKMEM_BF16, x, res, weight, T, D, eps, sum_out, y_out,
                                        scale_out, reinterpret_cast<hipStream_t>(stream)), fn);
 }
@@ -833,6 +855,11 @@ int mem_rmsnorm_backward(const void* dy, const void* h, const void* weight, pkme
     if (!aligned(ws, 256)) return fail(PKMEM_ERR_INVALID, "%s: workspace must be 256-byte aligned", fn);
   }
   if (T == 0) return PKMEM_OK;
+  const size_t rows = (size_t)T * D * esize(dt);
+  const Bytes bdy{dy, rows}, bh{h, rows}, bd{dsum, rows}, bx{dx_out, rows}, bw{weight, D * esize(dt)},
+      bg{grad_weight, (size_t)D * 4}, bws{grad_weight ? ws : nullptr, mem_rmsnorm_backward_workspace_size(T, D)};
+  if (over(bx, {bw, bg, bws}, {bdy, bh, bd}) || over(bg, {bdy, bh, bd, bw, bws}) || over(bws, {bdy, bh, bd, bw}))
+    return fail(PKMEM_ERR_INVALID, "%s: dx_out may be dy, h or dsum itself; outputs and workspace may share no other bytes", fn);
   return hip_status(pk::launch_rmsnorm_backward(dt == PKMEM_BF16, dy, h, weight, dsum, T, D, eps,
                                                 dx_out, grad_weight, reinterpret_cast<float*>(ws),
                                                 reinterpret_cast<hipStream_t>(stream)), fn);
@@ -847,7 +874,9 @@ int mem_quantize_rows(const void* x, pkmem_dtype dt, int64_t R, int C, void* q_o
   if (!aligned(x, 16) || !aligned(q_out, 16) || !aligned(scale_out, 4))
     return fail(PKMEM_ERR_INVALID, "%s: x and q_out must be 16-byte aligned (scale_out 4)", fn);
   if (R == 0) return PKMEM_OK;
-  if (q_out == x) return fail(PKMEM_ERR_INVALID, "%s: q_out may not be x", fn);
+  const Bytes bx{x, (size_t)R * C * esize(dt)}, bq{q_out, (size_t)R * C}, bs{scale_out, (size_t)R * 4};
+  if (over(bq, {bx, bs}) || over(bs, {bx}))
+    return fail(PKMEM_ERR_INVALID, "%s: q_out may not be x, nor any two buffers share bytes", fn);
   return hip_status(pk::launch_quantize_rows(dt == PKMEM_BF16, x, R, C, q_out, scale_out,
                                              reinterpret_cast<hipStream_t>(stream)), fn);
 }

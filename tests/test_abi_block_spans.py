@@ -1,0 +1,88 @@
+"""Outputs that share any bytes with what the norm, projection and optimizer calls read or
+write besides, not only those that start at the same place, are refused on the host (fake
+pointers, nothing is launched)."""
+import ctypes
+
+import pytest
+import torch
+
+import paper_2412_09764_amd as pk
+
+OK, INVALID, HIP = 0, -1, -4
+F32, BF16, E4M3 = 0, 1, 2
+PLACES = [1 << e for e in range(32, 44)]  # far apart
+T, D = 6, 64
+
+
+@pytest.fixture(scope="module")
+def lib():
+    if torch.cuda.is_available():
+        pytest.skip("fake device pointers: host-only test")
+    return pk.load()
+
+
+def verdict(lib, rc, bad):
+    """An accepted call ends in a HIP error on a host without a GPU."""
+    assert rc == (INVALID if bad else HIP), lib.mem_last_error().decode()
+
+
+def overlaps(sizes, writes, itself=()):
+    """(kwargs, refused?) for buffers of these sizes in bytes: each pair with a write in it
+    overlapping by 16 bytes at either end, inside one another, or starting at one place.
+    itself: pairs that may be one buffer."""
+    at = dict(zip(sizes, PLACES))
+    yield at, False
+    for a in writes:
+        for b in sizes:
+            if a == b:
+                continue
+            yield {**at, a: at[b]}, not ((a, b) in itself and sizes[a] == sizes[b])
+            yield {**at, a: at[b] + sizes[b] - 16}, True
+            yield {**at, b: at[a] + sizes[a] - 16}, True
+            yield {**at, a: at[b] + sizes[b]}, False
+            yield {**at, b: at[a] + sizes[a]}, False
+
+
+def cases(sizes, writes, itself=()):
+    return list(overlaps(sizes, writes, itself))
+
+
+@pytest.mark.parametrize("dt,ydt", [(F32, F32), (BF16, BF16), (F32, E4M3), (BF16, E4M3)])
+def test_norm(lib, dt, ydt):
+    e = 4 if dt == F32 else 2
+    rows = T * D * e
+    sizes = dict(x=rows, res=rows, w=D * e, s=rows, y=T * D if ydt == E4M3 else rows)
+    itself = [("s", "x"), ("s", "res")] + ([("y", "x"), ("y", "res")] if ydt != E4M3 else [])
+    for a, bad in cases(sizes, ("s", "y"), itself):
+        verdict(lib, lib.mem_rmsnorm(a["x"], a["res"], a["w"], dt, T, D, 1e-5, a["s"], a["y"], ydt,
+                                     1 << 50 if ydt == E4M3 else None, None), bad)
+    if ydt == E4M3:
+        a = dict(zip(sizes, PLACES))
+        for b in sizes:
+            for place in (a[b], a[b] + sizes[b] - 4, a[b] - T * 4 + 4):
+                verdict(lib, lib.mem_rmsnorm(a["x"], a["res"], a["w"], dt, T, D, 1e-5, a["s"], a["y"], ydt, place, None), True)
+
+
+@pytest.mark.parametrize("dt", [F32, BF16])
+def test_norm_backward(lib, dt):
+    e = 4 if dt == F32 else 2
+    rows = T * D * e
+    sizes = dict(dy=rows, h=rows, ds=rows, w=D * e, dx=rows, gw=D * 4, ws=lib.mem_rmsnorm_backward_workspace_size(T, D))
+    assert sizes["ws"] % 256 == 0
+    for a, bad in cases(sizes, ("dx", "gw", "ws"), [("dx", "dy"), ("dx", "h"), ("dx", "ds")]):
+        if a["ws"] % 256:
+            continue
+        verdict(lib, lib.mem_rmsnorm_backward(a["dy"], a["h"], a["w"], dt, T, D, 1e-5, a["ds"], a["dx"], a["gw"], a["ws"],
+                                              sizes["ws"], None), bad)
+    a = dict(zip(sizes, PLACES))
+    # without a weight gradient the workspace is not used
+    verdict(lib, lib.mem_rmsnorm_backward(a["dy"], a["h"], a["w"], dt, T, D, 1e-5, a["ds"], a["dx"], None, a["h"], 1 << 20, None), False)
+
+
+@pytest.mark.parametrize("dt", [F32, BF16])
+def test_quantize_rows(lib, dt):
+    sizes = dict(x=T * D * (4 if dt == F32 else 2), q=T * D, s=T * 4)
+    for a, bad in cases(sizes, ("q", "s")):
+        if a["q"] % 16 or a["x"] % 16:
+            continue
+        verdict(lib, lib.mem_quantize_rows(a["x"], dt, T, D, a["q"], a["s"], None), bad)
