@@ -431,8 +431,8 @@ int mem_quantize_rows(const void* x, pkmem_dtype dt, int64_t R, int C, void* q_o
  *   y_dt    PKMEM_F32 or PKMEM_BF16; dt = PKMEM_F32 needs PKMEM_F32.
  *   act     pkmem_act.
  *   z_out   [T, N] dtype y_dt: z (what mem_act_backward needs); NULL to skip it.
- *   y_out   [T, N] dtype y_dt; may be res (in place), no other buffer (an output
- *           that starts where an operand does is refused).
+ *   y_out   [T, N] dtype y_dt; may be res (in place).  An output that shares bytes
+ *           with another buffer in any other way is refused.
  *   N % 8 == 0; K % 8 == 0 (PKMEM_E4M3: K % 16 == 0); N, K <= 2^20; T < 2^31 and
  *   ceil(T / 256) * ceil(N / 256) < 2^23.  All buffers 16-byte aligned.  T = 0 is a valid no-op.
  * ------------------------------------------------------------------------ */
@@ -449,7 +449,8 @@ int mem_linear(const void* x, const void* w, pkmem_dtype dt, const float* x_scal
 
 /* Gradient of the activation, element-wise: dz_out = dy * act'(z) over [T, N]
  * dtype dt (PKMEM_F32 or PKMEM_BF16), rounded once; pass it to
- * mem_linear_backward.  N % 8 == 0; 16-byte aligned; dz_out may be dy or z. */
+ * mem_linear_backward.  N % 8 == 0; 16-byte aligned; dz_out may be dy or z
+ * (sharing bytes with them in any other way is refused). */
 int mem_act_backward(const void* dy, const void* z, pkmem_dtype dt, int act, int64_t T, int N,
                      void* dz_out, pkmem_stream_t stream);
 
@@ -458,7 +459,8 @@ int mem_act_backward(const void* dy, const void* z, pkmem_dtype dt, int act, int
  * the forward's x [T, K] and w [N, K]:
  *   dx_out    [T, K] dtype dt, written: dz W + dx_add, rounded once; dx_add
  *             [T, K] dtype dt (another path's gradient of x) or NULL; dx_out
- *             may be dx_add, no other input.
+ *             may be dx_add.  Outputs and workspace that share other bytes
+ *             are refused.
  *   grad_w    [N, K] fp32, ACCUMULATED: += dz^T x.
  *   grad_bias [N] fp32, ACCUMULATED: += sum_t dz.
  * Each output may be NULL.  (The gradient of the forward's res is dy itself.)

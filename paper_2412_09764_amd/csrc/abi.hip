@@ -979,10 +979,11 @@ int mem_linear(const void* x, const void* w, pkmem_dtype dt, const float* x_scal
       !aligned(bias, 16) || !aligned(res, 16) || !aligned(z_out, 16) || !aligned(y_out, 16))
     return fail(PKMEM_ERR_INVALID, "%s: buffers must be 16-byte aligned", fn);
   if (T == 0) return PKMEM_OK;
-  // an output over an operand that other workgroups still read
-  if (y_out == x || y_out == w || z_out == x || z_out == w || z_out == y_out || (z_out && z_out == res) ||
-      (bias && (y_out == bias || z_out == bias)))
-    return fail(PKMEM_ERR_INVALID, "%s: an output may not be an operand or the other output (y_out may be res)", fn);
+  const size_t e = dt == PKMEM_E4M3 ? 1 : esize(dt), ye = esize(y_dt), out = (size_t)T * N * ye;
+  const Bytes bx{x, (size_t)T * K * e}, bw{w, (size_t)N * K * e}, bsx{x_scale, (size_t)T * 4}, bsw{w_scale, (size_t)N * 4},
+      bb{bias, N * ye}, br{res, out}, bz{z_out, out}, by{y_out, out};
+  if (over(by, {bx, bw, bsx, bsw, bb, bz}, {br}) || over(bz, {bx, bw, bsx, bsw, bb, br}))
+    return fail(PKMEM_ERR_INVALID, "%s: an output may share no bytes with an operand or the other output (y_out may be res itself)", fn);
   const pk::LinearCall c{x, w, dt, x_scale, w_scale, bias, res, T, N, K, act, z_out, y_out, y_dt == PKMEM_BF16};
   return hip_status(pk::launch_linear(c, reinterpret_cast<hipStream_t>(stream)), fn);
 }
@@ -999,6 +1000,9 @@ int mem_act_backward(const void* dy, const void* z, pkmem_dtype dt, int act, int
   if (!aligned(dy, 16) || !aligned(z, 16) || !aligned(dz_out, 16))
     return fail(PKMEM_ERR_INVALID, "%s: buffers must be 16-byte aligned", fn);
   if (T == 0) return PKMEM_OK;
+  const size_t n = (size_t)T * N * esize(dt);
+  if (over({dz_out, n}, {}, {{dy, n}, {z, n}}))
+    return fail(PKMEM_ERR_INVALID, "%s: dz_out may be dy or z itself and share no other bytes with them", fn);
   return hip_status(pk::launch_act_backward(dt == PKMEM_BF16, dy, z, act, T * N, dz_out,
                                             reinterpret_cast<hipStream_t>(stream)), fn);
 }
@@ -1024,10 +1028,13 @@ int mem_linear_backward(const void* dz, const void* x, const void* w, pkmem_dtyp
     return fail(PKMEM_ERR_WORKSPACE, "%s: workspace of %zu bytes needed, %zu given", fn, need, ws ? ws_bytes : (size_t)0);
   if (!aligned(ws, 256)) return fail(PKMEM_ERR_INVALID, "%s: workspace must be 256-byte aligned", fn);
   if (T == 0 || (!dx_out && !grad_w && !grad_bias)) return PKMEM_OK;
-  if (dx_out && (dx_out == dz || dx_out == x || dx_out == w))
-    return fail(PKMEM_ERR_INVALID, "%s: dx_out may be dx_add, no other input", fn);
-  if (grad_w && (grad_w == dz || grad_w == x || grad_w == w || grad_w == dx_out || grad_w == grad_bias || grad_w == dx_add))
-    return fail(PKMEM_ERR_INVALID, "%s: grad_w may be no other buffer", fn);
+  const size_t e = esize(dt);
+  const Bytes bz{dz, (size_t)T * N * e}, bx{x, (size_t)T * K * e}, bw{w, (size_t)N * K * e}, ba{dx_add, bx.n}, bdx{dx_out, bx.n},
+      bgw{grad_w, (size_t)N * K * 4}, bgb{grad_bias, (size_t)N * 4}, bws{grad_w || grad_bias ? ws : nullptr, need};
+  if (over(bdx, {bz, bx, bw}, {ba}))
+    return fail(PKMEM_ERR_INVALID, "%s: dx_out may be dx_add itself and share no other bytes with an input", fn);
+  if (over(bgw, {bz, bx, bw, ba, bdx, bgb}) || over(bgb, {bz, bx, bw, ba, bdx}) || over(bws, {bz, bx, bw, ba, bdx, bgw, bgb}))
+    return fail(PKMEM_ERR_INVALID, "%s: grad_w, grad_bias and workspace: each may share bytes with no other buffer", fn);
   return hip_status(pk::launch_linear_backward(dt == PKMEM_BF16, dz, x, w, T, N, K, dx_add, dx_out,
                                                grad_w, grad_bias, ws,
                                                reinterpret_cast<hipStream_t>(stream)), fn);

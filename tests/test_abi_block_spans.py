@@ -86,3 +86,39 @@ def test_quantize_rows(lib, dt):
         if a["q"] % 16 or a["x"] % 16:
             continue
         verdict(lib, lib.mem_quantize_rows(a["x"], dt, T, D, a["q"], a["s"], None), bad)
+
+
+@pytest.mark.parametrize("dt,ydt", [(F32, F32), (BF16, BF16), (BF16, F32), (E4M3, BF16), (E4M3, F32)])
+def test_linear(lib, dt, ydt):
+    N, K, e, ye = 32, 48, {F32: 4, BF16: 2, E4M3: 1}[dt], 4 if ydt == F32 else 2
+    n = 64  # tokens: the scales are a whole number of 16 bytes
+    out = n * N * ye
+    sizes = dict(x=n * K * e, w=N * K * e, sx=n * 4, sw=N * 4, b=N * ye, r=out, z=out, y=out)
+    if dt != E4M3:
+        del sizes["sx"], sizes["sw"]
+    for a, bad in cases(sizes, ("z", "y"), [("y", "r")]):
+        verdict(lib, lib.mem_linear(a["x"], a["w"], dt, a.get("sx"), a.get("sw"), a["b"], a["r"], n, N, K, 1, a["z"],
+                                    a["y"], ydt, None), bad)
+
+
+@pytest.mark.parametrize("dt", [F32, BF16])
+def test_act_backward(lib, dt):
+    n = T * D * (4 if dt == F32 else 2)
+    for a, bad in cases(dict(dy=n, z=n, dz=n), ("dz",), [("dz", "dy"), ("dz", "z")]):
+        verdict(lib, lib.mem_act_backward(a["dy"], a["z"], dt, 2, T, D, a["dz"], None), bad)
+
+
+@pytest.mark.parametrize("dt", [F32, BF16])
+@pytest.mark.parametrize("n", [64, 4096])  # one split of the tokens, and several
+def test_linear_backward(lib, dt, n):
+    N, K, e = 32, 48, 4 if dt == F32 else 2
+    ws = lib.mem_linear_backward_workspace_size(n, N, K, dt)
+    sizes = dict(dz=n * N * e, x=n * K * e, w=N * K * e, add=n * K * e, dx=n * K * e, gw=N * K * 4, gb=N * 4, ws=ws)
+    for a, bad in cases(sizes, ("dx", "gw", "gb", "ws"), [("dx", "add")]):
+        if a["ws"] % 256:
+            continue
+        verdict(lib, lib.mem_linear_backward(a["dz"], a["x"], a["w"], dt, n, N, K, a["add"], a["dx"], a["gw"], a["gb"],
+                                             a["ws"], ws, None), bad)
+    a = dict(zip(sizes, PLACES))
+    # dx alone uses no workspace
+    verdict(lib, lib.mem_linear_backward(a["dz"], a["x"], a["w"], dt, n, N, K, None, a["dx"], None, None, a["x"], ws, None), False)
