@@ -499,7 +499,8 @@ int mem_linear_backward(const void* dz, const void* x, const void* w, pkmem_dtyp
  * move on (lr and step are then not used).  Where *grad_scale is 0 or not
  * finite, or *step_dev below 1, the whole call changes nothing.
  * Tensors of any length up to 2^36 - 2^12 (0: skipped) and any alignment; 16-byte
- * aligned ones are fast.  No two parameters or states may overlap (refused, by mem_adamw_rows too).
+ * aligned ones are fast.  No parameter or state may overlap another one, a gradient or a
+ * device scalar, nor in mem_adamw_rows the list of rows (refused).
  * ------------------------------------------------------------------------ */
 typedef struct {
   void* param;

@@ -767,39 +767,54 @@ int check_adamw_tensor(const char* fn, const pkmem_adamw_tensor& t, int i, bool 
   return PKMEM_OK;
 }
 
-// Do two of the buffers that a step writes overlap?  A parameter listed twice
-// would be written by two workgroups at once.
-int check_adamw_overlap(const char* fn, const pkmem_adamw_tensor* ts, int count) {
-  struct Span { uintptr_t begin, end; int i; };
-  Span few[5 * 16];
-  Span* s = count <= 16 ? few : static_cast<Span*>(malloc(sizeof(Span) * 5 * (size_t)count));
+// Does a buffer that a step writes overlap another that it writes or reads?  A
+// parameter listed twice would be written by two workgroups at once, a state over a
+// gradient be overwritten before another workgroup reads it.  rows: mem_adamw_rows's list.
+int check_adamw_overlap(const char* fn, const pkmem_adamw_tensor* ts, int count, const pkmem_adamw_opts& o,
+                        size_t grad_elems = 0, Bytes rows = {}) {
+  struct Span { uintptr_t begin, end; int i; bool write; };
+  constexpr int EACH = 6, MORE = 4, FEW = 16;
+  Span few[EACH * FEW + MORE];
+  Span* s = count <= FEW ? few : static_cast<Span*>(malloc(sizeof(Span) * (EACH * (size_t)count + MORE)));
   if (!s) return fail(PKMEM_ERR_UNSUPPORTED, "%s: no host memory for a list of %d", fn, count);
   size_t n = 0;
+  auto add = [&](const void* p, size_t bytes, int i, bool write) {
+    if (p && bytes) s[n++] = Span{reinterpret_cast<uintptr_t>(p), reinterpret_cast<uintptr_t>(p) + bytes, i, write};
+  };
   for (int i = 0; i < count; ++i) {
     const pkmem_adamw_tensor& t = ts[i];
     if (t.numel == 0) continue;
     const bool s8 = t.state_dt == PKMEM_E4M3;
     const size_t e = (size_t)t.numel, state = e * (s8 ? 1 : 4);
-    const size_t scale = (e + pk::ADAMW_STATE_BLOCK - 1) / pk::ADAMW_STATE_BLOCK * 4;
-    auto add = [&](const void* p, size_t bytes) {
-      s[n++] = Span{reinterpret_cast<uintptr_t>(p), reinterpret_cast<uintptr_t>(p) + bytes, i};
-    };
-    add(t.param, e * esize(t.param_dt));
-    add(t.exp_avg, state);
-    add(t.exp_avg_sq, state);
-    if (s8) {
-      add(t.exp_avg_scale, scale);
-      add(t.exp_avg_sq_scale, scale);
-    }
+    const size_t scale = s8 ? (e + pk::ADAMW_STATE_BLOCK - 1) / pk::ADAMW_STATE_BLOCK * 4 : 0;
+    add(t.param, e * esize(t.param_dt), i, true);
+    add(t.exp_avg, state, i, true);
+    add(t.exp_avg_sq, state, i, true);
+    add(t.exp_avg_scale, scale, i, true);
+    add(t.exp_avg_sq_scale, scale, i, true);
+    add(t.grad, (rows.p ? grad_elems : e) * esize(t.grad_dt), i, false);
   }
+  add(o.lr_dev, 4, -1, false);
+  add(o.step_dev, 8, -1, false);
+  add(o.grad_scale, 4, -1, false);
+  add(rows.p, rows.n, -1, false);
   std::sort(s, s + n, [](const Span& a, const Span& b) { return a.begin < b.begin; });
-  int a = -1, b = -1;
-  for (size_t i = 1; i < n && a < 0; ++i)
-    if (s[i].begin < s[i - 1].end) a = s[i - 1].i, b = s[i].i;
+  // the furthest ends of what is written and of what is read so far
+  Span wrote{0, 0, -1, true}, read{0, 0, -1, false};
+  int a = -2, b = -2;
+  bool both = false;
+  for (size_t i = 0; i < n && a == -2; ++i) {
+    if (s[i].begin < wrote.end) a = wrote.i, b = s[i].i, both = s[i].write;
+    else if (s[i].write && s[i].begin < read.end) a = s[i].i, b = read.i;
+    Span& last = s[i].write ? wrote : read;
+    if (s[i].end > last.end) last = s[i];
+  }
   if (s != few) free(s);
-  if (a >= 0)
+  if (a == -2) return PKMEM_OK;
+  if (both)
     return fail(PKMEM_ERR_INVALID, "%s: parameters or states of tensors %d and %d overlap", fn, a < b ? a : b, a < b ? b : a);
-  return PKMEM_OK;
+  return b < 0 ? fail(PKMEM_ERR_INVALID, "%s: a parameter or state of tensor %d overlaps a device scalar or the list of rows", fn, a)
+               : fail(PKMEM_ERR_INVALID, "%s: a parameter or state of tensor %d overlaps the gradient of tensor %d", fn, a, b);
 }
 
 }  // namespace
@@ -894,7 +909,7 @@ int mem_adamw(const pkmem_adamw_tensor* tensors, int count, const pkmem_adamw_op
     if (tensors[i].numel > pk::ADAMW_MAX_NUMEL)
       return fail(PKMEM_ERR_UNSUPPORTED, "%s: tensor %d: more than 2^36 - 2^12 elements", fn, i);
   }
-  rc = check_adamw_overlap(fn, tensors, count);
+  rc = check_adamw_overlap(fn, tensors, count, *opts);
   if (rc) return rc;
   return hip_status(pk::launch_adamw(tensors, count, *opts, reinterpret_cast<hipStream_t>(stream)), fn);
 }
@@ -924,7 +939,7 @@ int mem_adamw_rows(const pkmem_adamw_tensor* table, int64_t N, int D, const int6
   if (U > 0 && !rows) return fail(PKMEM_ERR_INVALID, "%s: null pointer", fn);
   if (!aligned(rows, 8)) return fail(PKMEM_ERR_INVALID, "%s: rows must be 8-byte aligned", fn);
   if (U == 0) return PKMEM_OK;
-  rc = check_adamw_overlap(fn, table, 1);
+  rc = check_adamw_overlap(fn, table, 1, *opts, (size_t)U * D, {rows, (size_t)U * 8});
   if (rc) return rc;
   hipStream_t st = reinterpret_cast<hipStream_t>(stream);
   if (debug_checks()) {

@@ -122,3 +122,51 @@ def test_linear_backward(lib, dt, n):
     a = dict(zip(sizes, PLACES))
     # dx alone uses no workspace
     verdict(lib, lib.mem_linear_backward(a["dz"], a["x"], a["w"], dt, n, N, K, None, a["dx"], None, None, a["x"], ws, None), False)
+
+
+def adamw(lib, tensors, **opts):
+    ts = (pk._AdamwTensor * len(tensors))(*tensors)
+    o = pk._AdamwOpts(1e-3, 0.9, 0.999, 1e-8, 0.1, 1, 0, **opts)
+    return lib.mem_adamw(ctypes.addressof(ts), len(tensors), ctypes.addressof(o), None)
+
+
+@pytest.mark.parametrize("gd", [F32, BF16])
+@pytest.mark.parametrize("sd", [F32, E4M3])
+def test_adamw(lib, gd, sd):
+    n = 1024
+    state, scale = (n, n // 128 * 4) if sd == E4M3 else (n * 4, 0)
+    sizes = dict(param=n * 4, exp_avg=state, exp_avg_sq=state, grad=n * (4 if gd == F32 else 2), lr_dev=4, step_dev=8, grad_scale=4)
+    if scale:
+        sizes.update(exp_avg_scale=scale, exp_avg_sq_scale=scale)
+    scalars = ("lr_dev", "step_dev", "grad_scale")
+    far = pk._AdamwTensor(1 << 20, 1 << 21, 1 << 22, 1 << 23, None, None, 64, F32, F32, F32)
+    for a, bad in cases(sizes, [w for w in sizes if w not in scalars and w != "grad"]):
+        own = {k: v for k, v in a.items() if k not in scalars}
+        if any(v % 16 for v in a.values()):
+            continue
+        t = pk._AdamwTensor(numel=n, param_dt=F32, grad_dt=gd, state_dt=sd, **own)
+        verdict(lib, adamw(lib, [far, t], **{k: a[k] for k in scalars}), bad)
+
+
+def test_adamw_among_tensors(lib):
+    """Gradients may be shared; one tensor's state over another's gradient may not."""
+    make = lambda i, g: pk._AdamwTensor(PLACES[3 * i], g, PLACES[3 * i + 1], PLACES[3 * i + 2], None, None, 1000, F32, F32, F32)  # noqa: E731
+    verdict(lib, adamw(lib, [make(0, 1 << 50), make(1, 1 << 50), make(2, (1 << 50) + 400)]), False)
+    for place in (PLACES[0], PLACES[1] + 3996, PLACES[2] - 3996):
+        verdict(lib, adamw(lib, [make(0, 1 << 50), make(1, place)]), True)
+        verdict(lib, adamw(lib, [make(1, place), make(2, 1 << 50), make(0, 1 << 50)]), True)
+        assert "gradient" in lib.mem_last_error().decode()
+    # a long gradient that begins in front of several short ones
+    long = pk._AdamwTensor(1 << 55, 1 << 50, 1 << 56, 1 << 57, None, None, 1 << 20, F32, F32, F32)
+    inside = pk._AdamwTensor((1 << 50) + (1 << 21), 1 << 51, 1 << 52, 1 << 53, None, None, 64, F32, F32, F32)
+    verdict(lib, adamw(lib, [long, make(0, (1 << 50) + 64), inside]), True)
+
+
+def test_adamw_rows(lib):
+    n, d, u = 64, 128, 32
+    sizes = dict(param=n * d * 4, exp_avg=n * d, exp_avg_sq=n * d, exp_avg_scale=n * 4, exp_avg_sq_scale=n * 4,
+                 grad=u * d * 4, rows=u * 8)
+    for a, bad in cases(sizes, [w for w in sizes if w not in ("grad", "rows")]):
+        t = pk._AdamwTensor(numel=n * d, param_dt=F32, grad_dt=F32, state_dt=E4M3, **{k: v for k, v in a.items() if k != "rows"})
+        o = pk._AdamwOpts(1e-3, 0.9, 0.999, 1e-8, 0.1, 1, 0)
+        verdict(lib, lib.mem_adamw_rows(ctypes.addressof(t), n, d, a["rows"], u, ctypes.addressof(o), None), bad)
