@@ -429,7 +429,10 @@ int mem_quantize_rows(const void* x, pkmem_dtype dt, int64_t R, int C, void* q_o
  *           mem_quantize_rows' scales; NULL for the other dtypes).
  *   bias [N], res [T, N] dtype y_dt; NULL: none.
  *   y_dt    PKMEM_F32 or PKMEM_BF16; dt = PKMEM_F32 needs PKMEM_F32.
- *   act     pkmem_act.
+ *   act     pkmem_act: in fp32 within (1.5 z^2 + 36) 2^-24 of its value, in bf16
+ *           (fast exponentials and reciprocals) within 2^-12 of it before the
+ *           rounding; values below 2^-118 may become 0.  mem_act_backward's the same,
+ *           of the sizes of a derivative's terms.
  *   z_out   [T, N] dtype y_dt: z (what mem_act_backward needs); NULL to skip it.
  *   y_out   [T, N] dtype y_dt; may be res (in place).  An output that shares bytes
  *           with another buffer in any other way is refused.
