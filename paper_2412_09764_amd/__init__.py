@@ -617,7 +617,8 @@ def mem_rmsnorm(x: torch.Tensor, weight=None, residual=None, eps: float = 1e-5, 
 
     Returns (y, h, scale): y in x's dtype and scale None, or with quantize y in
     float8_e4m3fn with scale fp32 [T] (the norm is about y * scale[:, None]); h None
-    without a residual or with want_sum False (sum_out may be x or residual)."""
+    without a residual or with want_sum False unless sum_out is given (it may be x or
+    residual)."""
     _here(x, weight, residual, sum_out, y_out, scale_out)
     shape, xdt = x.shape, x.dtype
     T, D = shape
@@ -626,18 +627,17 @@ def mem_rmsnorm(x: torch.Tensor, weight=None, residual=None, eps: float = 1e-5, 
     if weight is not None:
         _like(weight, (D,), xdt, "weight")
         wp = weight.data_ptr()
-    if residual is None:
-        sum_out = None
-    else:
+    if residual is not None:
         _like(residual, shape, xdt, "residual")
         rp = residual.data_ptr()
-        if sum_out is not None:
-            _like(sum_out, shape, xdt, "sum_out")
-        elif want_sum:
+        if sum_out is None and want_sum:
             sum_out = torch.empty_like(x)
-        hp = _ptr(sum_out)
+    if sum_out is not None:
+        _like(sum_out, shape, xdt, "sum_out")
+        hp = sum_out.data_ptr()
     if not quantize:
-        scale_out = None
+        if scale_out is not None:
+            raise ValueError("scale_out is for quantize")
     else:
         xdt, ydt = torch.float8_e4m3fn, E4M3
         if scale_out is None:
