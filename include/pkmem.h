@@ -367,7 +367,8 @@ int mem_bag_backward_sparse(const void* dy, const void* values, pkmem_dtype v_dt
  *   h[t,:] = x[t,:] + res[t,:]   added in fp32 and rounded once to dt: the
  *                                stream as stored is what is normalised;
  *   y[t,:] = h[t,:] * rstd[t] * weight,  rstd = 1 / sqrt(mean(h^2) + eps) in
- *            fp32 (0 where mean + eps == 0), rounded once to y_dt.
+ *            fp32 (0 where mean + eps is 0 or past the largest number: rows
+ *            with numbers beyond 1.8e19 give 0), rounded once to y_dt.
  *
  *   x       [T, D] dtype dt (PKMEM_F32 or PKMEM_BF16).
  *   res     [T, D] dtype dt; NULL: h = x.
@@ -377,7 +378,8 @@ int mem_bag_backward_sparse(const void* dy, const void* values, pkmem_dtype v_dt
  *   sum_out [T, D] dtype dt: h; NULL to skip it.  May be x or res (in place).
  *   y_out   [T, D] dtype y_dt, which is dt, or PKMEM_E4M3: y in 8 bits with one
  *           scale a row, y ~ y_out * scale_out[t],
- *           scale = max(max_j |y| / 448, 2^-126), codes to nearest even.  May be
+ *           scale = max(max_j |y| / 448, 2^-126), codes the numbers nearest to
+ *           448 y / max_j |y|, ties to even (exact for bf16 rows).  May be
  *           x or res where y_dt is dt (in place, without sum_out there).
  *   scale_out [T] fp32: required for PKMEM_E4M3, NULL otherwise.
  * All buffers 16-byte aligned (scale_out 4).  An output that shares bytes with
@@ -422,7 +424,8 @@ int mem_quantize_rows(const void* x, pkmem_dtype dt, int64_t R, int C, void* q_o
  * sums and epilogue in fp32, one rounding to y_dt.  Products are exact for
  * PKMEM_BF16 and PKMEM_E4M3; PKMEM_F32 operands are taken in three bf16 parts (24
  * bits of mantissa) and each product is within 2^-23 of itself, for magnitudes
- * from 2^-110 (below, within 2^-126 of the operand) to 3.38e38.
+ * from 2^-110 (below, within 2^-126 of the operand) to 3.38e38; an infinity
+ * gives NaN there (for up to 8 tokens, whose products are fp32 ones, infinity).
  *
  *   x  [T, K], w [N, K]  dtype dt: PKMEM_F32, PKMEM_BF16, or PKMEM_E4M3 with
  *           x_scale [T] and w_scale [N] fp32 (mem_rmsnorm's and
@@ -490,8 +493,9 @@ int mem_linear_backward(const void* dz, const void* x, const void* w, pkmem_dtyp
  *   grad_dt   PKMEM_F32 or PKMEM_BF16.
  *   state_dt  PKMEM_F32, or PKMEM_E4M3: exp_avg holds m, exp_avg_sq holds
  *             sqrt(v), each as numel codes and ceil(numel / 128) fp32 scales,
- *             one for each 128 consecutive elements (largest / 448), rounded at
- *             random like bf16 parameters; a root above 0 stays above 0.  States
+ *             one for each 128 consecutive elements (largest / 448; a block whose
+ *             largest is below 448 * 2^-126 becomes 0), rounded at random like
+ *             bf16 parameters; else a root above 0 stays above 0.  States
  *             that are all zero start a run.  An element that is not finite
  *             is stored as NaN and leaves its neighbours' scale alone.
  * The random bits are a hash of (seed, step, position in the list, element):
@@ -517,7 +521,8 @@ typedef struct {
 } pkmem_adamw_tensor;
 
 typedef struct {
-  double lr, beta1, beta2, eps, weight_decay; /* betas in [0, 1), others >= 0 */
+  double lr, beta1, beta2, eps, weight_decay; /* betas in [0, 1), others >= 0; with eps = 0 an element
+                                                   whose gradients were all 0 becomes NaN */
   int64_t step;                               /* 1 for the first */
   uint64_t seed;
   const float* lr_dev;

@@ -5,11 +5,14 @@
 //
 // Memory bound: parameter and states read and written once, the gradient
 // read once (28 bytes an element in fp32, 12 for a bf16 parameter with 8-bit
-// states).  2^28 elements in fp32 1.48 ms (5.07 TB/s); 2^29 with 8-bit states 1.33
-// ms (4.88 TB/s: the vector arithmetic of quotient, root, hash and two roundings
-// takes nearly as long as the memory); 400001 touched rows of 1024 1.13 ms (4.4).  A lane holds 8 consecutive elements (16- and 32-byte accesses),
-// 16 lanes the 128 elements that share the scales of their 8-bit states, so
-// the largest element of a block is found by four lane exchanges.
+// states), and the memory moves those bytes and no others (counters).  Median and
+// least of several runs: 2^28 elements in fp32 1.48 ms (5.09 TB/s); 2^29 with 8-bit
+// states 1.36 and 1.31 ms (4.8 TB/s: the vector arithmetic of quotient, root, hash and
+// two roundings takes nearly as long as the memory; up to 1.5 ms a call in a kernel
+// trace); 400001 touched rows of 1024 1.17 and 1.11 ms (4.2; up to 1.3).  A lane holds
+// 8 consecutive elements (16- and 32-byte accesses), 16 lanes the 128 elements that
+// share the scales of their 8-bit states, so the largest element of a block is found
+// by four lane exchanges.
 //
 // 8-bit states hold m and r = sqrt(v) in e4m3 with one fp32 scale per 128
 // elements (largest / 448).  The root halves the range of exponents that v
@@ -364,7 +367,7 @@ __global__ __launch_bounds__(BLOCK) void k_adamw_rows(const RowArgs a) {
   }
 }
 
-// Strictly ascending row numbers in [0, N)?
+// Ascending row numbers (equal neighbours allowed) in [0, N)?
 __global__ __launch_bounds__(BLOCK) void k_check_rows(const int64_t* __restrict__ rows, int64_t U,
                                                       int64_t N, uint32_t* __restrict__ bad) {
   for (int64_t i = (int64_t)blockIdx.x * BLOCK + threadIdx.x; i < U; i += (int64_t)gridDim.x * BLOCK) {

@@ -16,14 +16,15 @@
 // the chip, smaller ones whose waves also share k.  A stage holds 64 bytes of k;
 // four stages are in LDS, filled by direct loads that run three stages ahead.
 // What bounds them: a 256-wide tile keeps the matrix cores busy 79% of its cycles,
-// at a clock that the power limit holds at 1.6 GHz (8192^3 bf16 at 1.25-1.30
-// PFLOP/s, fp32 0.214); a 128-wide one fetches its operands at the 12-14 TB/s
-// that the L2s give (0.88 PFLOP/s); small products are bound by the latency of a
-// few stages and the launch (64 x 2048 x 2048: 6.3 us).  Measured, bf16 unless said:
-//   32768 x 2048 x 2048 forward 257 us, with residual 288 (memory traffic of the
-//     epilogues, which all workgroups reach at once), fp32 1307;
-//   16384 x 2048 x 1024 dx 60 us, grad_W with its bias 76;
-//   2000 x 2048 x 2048 25 us, e4m3 17-19, fp32 95;  1 x 2048 x 2048 4.8.
+// at a clock that the power limit holds near 1.6 GHz (8192^3 bf16 at 1.27
+// PFLOP/s, fp32 0.211); a 128-wide one fetches its operands at the 12-14 TB/s
+// that the L2s gave in large products (0.88 PFLOP/s); small products are bound by the
+// latency of a few stages and the launch (64 x 2048 x 2048: 6.8 us).  Median of calls in
+// a graph, bf16 unless said:
+//   32768 x 2048 x 2048 forward 272 us (least 258), with residual 295 (290; memory
+//     traffic of the epilogues, which all workgroups reach at once), fp32 1336;
+//   16384 x 2048 x 1024 dx 62 us, grad_W with its bias 79;
+//   2000 x 2048 x 2048 26 us, e4m3 19, fp32 100;  1 x 2048 x 2048 5.8.
 #include "pk_internal.h"
 #include "pk_linear_plan.h"
 #include "pk_mfma.h"
@@ -760,10 +761,10 @@ __global__ __launch_bounds__(WM* WN* KG * 64) void k_gemm(const GemmArgs g) {
 // Few rows of x (up to 8): a workgroup takes 16 rows of W and all of x; its
 // waves share k in chunks of 64 bytes, straight from memory into the 16x16
 // fragments (rows past the end are read as the last one and dropped), and add
-// their sums through LDS in wave order.  Bound by reading W once: 4.8 us for one
-// row at 2048 x 2048 bf16 and 28.6 us (4.7 TB/s) at 16384 x 4096, where the
-// 32 x 32 tiles take 6.4 and 32; with 16 rows these take 6.4 and 33.8 us, this
-// form 6.8 and 41.
+// their sums through LDS in wave order.  Bound by reading W once: 5.8 us for one
+// row at 2048 x 2048 bf16 in a graph (5.2 of kernel) and 30 us (4.4 TB/s) at
+// 16384 x 4096.  Timed from the host, the 32 x 32 tiles took 6.4 and 32 us where this
+// form took 4.8 and 28.6; with 16 rows 6.4 and 33.8, this form 6.8 and 41.
 constexpr int FEW_WAVES = 8, FEW_T = 8;
 
 typedef __attribute__((ext_vector_type(4))) float f32x4_t;

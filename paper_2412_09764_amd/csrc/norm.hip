@@ -7,10 +7,11 @@
 // Every kernel reads a row once into registers, 16 bytes per lane and load:
 // a wave per row up to 8 KiB, four waves above.  Memory bound: two reads and
 // two writes per element with the residual, three reads and one write in the
-// backward.  32768 rows of 2048 bf16: forward with residual 78-80 us (6.7 TB/s), to
-// 8 bits 78 (6.0), backward 83 (6.5); four waves a row are no faster there and
-// slower in the backward (118 us).  Below some 4000 rows a call is bound by its
-// launch (2000 rows: 5 us of kernel).
+// backward, and the memory moves those bytes and no others (counters).  32768 rows of
+// 2048 bf16: forward with residual 80 us called again and again (6.7 TB/s), 93 and at
+// least 79 in turn with its backward, which takes 95 and at least 92 (5.7); to 8 bits
+// 79 (5.9).  Four waves a row are no faster there and slower in the backward (118
+// us).  Below some 4000 rows a call is bound by its launch (2000 rows: 7.5 us of kernel).
 #include "pk_internal.h"
 #include "pk_row.h"
 
