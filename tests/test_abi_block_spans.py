@@ -21,7 +21,7 @@ def lib():
     return pk.load()
 
 
-def verdict(lib, rc, bad):
+def expect(lib, rc, bad):
     """An accepted call ends in a HIP error on a host without a GPU."""
     assert rc == (INVALID if bad else HIP), lib.mem_last_error().decode()
 
@@ -54,13 +54,13 @@ def test_norm(lib, dt, ydt):
     sizes = dict(x=rows, res=rows, w=D * e, s=rows, y=T * D if ydt == E4M3 else rows)
     itself = [("s", "x"), ("s", "res")] + ([("y", "x"), ("y", "res")] if ydt != E4M3 else [])
     for a, bad in cases(sizes, ("s", "y"), itself):
-        verdict(lib, lib.mem_rmsnorm(a["x"], a["res"], a["w"], dt, T, D, 1e-5, a["s"], a["y"], ydt,
+        expect(lib, lib.mem_rmsnorm(a["x"], a["res"], a["w"], dt, T, D, 1e-5, a["s"], a["y"], ydt,
                                      1 << 50 if ydt == E4M3 else None, None), bad)
     if ydt == E4M3:
         a = dict(zip(sizes, PLACES))
         for b in sizes:
             for place in (a[b], a[b] + sizes[b] - 4, a[b] - T * 4 + 4):
-                verdict(lib, lib.mem_rmsnorm(a["x"], a["res"], a["w"], dt, T, D, 1e-5, a["s"], a["y"], ydt, place, None), True)
+                expect(lib, lib.mem_rmsnorm(a["x"], a["res"], a["w"], dt, T, D, 1e-5, a["s"], a["y"], ydt, place, None), True)
 
 
 @pytest.mark.parametrize("dt", [F32, BF16])
@@ -72,11 +72,11 @@ def test_norm_backward(lib, dt):
     for a, bad in cases(sizes, ("dx", "gw", "ws"), [("dx", "dy"), ("dx", "h"), ("dx", "ds")]):
         if a["ws"] % 256:
             continue
-        verdict(lib, lib.mem_rmsnorm_backward(a["dy"], a["h"], a["w"], dt, T, D, 1e-5, a["ds"], a["dx"], a["gw"], a["ws"],
+        expect(lib, lib.mem_rmsnorm_backward(a["dy"], a["h"], a["w"], dt, T, D, 1e-5, a["ds"], a["dx"], a["gw"], a["ws"],
                                               sizes["ws"], None), bad)
     a = dict(zip(sizes, PLACES))
     # without a weight gradient the workspace is not used
-    verdict(lib, lib.mem_rmsnorm_backward(a["dy"], a["h"], a["w"], dt, T, D, 1e-5, a["ds"], a["dx"], None, a["h"], 1 << 20, None), False)
+    expect(lib, lib.mem_rmsnorm_backward(a["dy"], a["h"], a["w"], dt, T, D, 1e-5, a["ds"], a["dx"], None, a["h"], 1 << 20, None), False)
 
 
 @pytest.mark.parametrize("dt", [F32, BF16])
@@ -85,7 +85,7 @@ def test_quantize_rows(lib, dt):
     for a, bad in cases(sizes, ("q", "s")):
         if a["q"] % 16 or a["x"] % 16:
             continue
-        verdict(lib, lib.mem_quantize_rows(a["x"], dt, T, D, a["q"], a["s"], None), bad)
+        expect(lib, lib.mem_quantize_rows(a["x"], dt, T, D, a["q"], a["s"], None), bad)
 
 
 @pytest.mark.parametrize("dt,ydt", [(F32, F32), (BF16, BF16), (BF16, F32), (E4M3, BF16), (E4M3, F32)])
@@ -97,7 +97,7 @@ def test_linear(lib, dt, ydt):
     if dt != E4M3:
         del sizes["sx"], sizes["sw"]
     for a, bad in cases(sizes, ("z", "y"), [("y", "r")]):
-        verdict(lib, lib.mem_linear(a["x"], a["w"], dt, a.get("sx"), a.get("sw"), a["b"], a["r"], n, N, K, 1, a["z"],
+        expect(lib, lib.mem_linear(a["x"], a["w"], dt, a.get("sx"), a.get("sw"), a["b"], a["r"], n, N, K, 1, a["z"],
                                     a["y"], ydt, None), bad)
 
 
@@ -105,7 +105,7 @@ def test_linear(lib, dt, ydt):
 def test_act_backward(lib, dt):
     n = T * D * (4 if dt == F32 else 2)
     for a, bad in cases(dict(dy=n, z=n, dz=n), ("dz",), [("dz", "dy"), ("dz", "z")]):
-        verdict(lib, lib.mem_act_backward(a["dy"], a["z"], dt, 2, T, D, a["dz"], None), bad)
+        expect(lib, lib.mem_act_backward(a["dy"], a["z"], dt, 2, T, D, a["dz"], None), bad)
 
 
 @pytest.mark.parametrize("dt", [F32, BF16])
@@ -117,11 +117,11 @@ def test_linear_backward(lib, dt, n):
     for a, bad in cases(sizes, ("dx", "gw", "gb", "ws"), [("dx", "add")]):
         if a["ws"] % 256:
             continue
-        verdict(lib, lib.mem_linear_backward(a["dz"], a["x"], a["w"], dt, n, N, K, a["add"], a["dx"], a["gw"], a["gb"],
+        expect(lib, lib.mem_linear_backward(a["dz"], a["x"], a["w"], dt, n, N, K, a["add"], a["dx"], a["gw"], a["gb"],
                                              a["ws"], ws, None), bad)
     a = dict(zip(sizes, PLACES))
     # dx alone uses no workspace
-    verdict(lib, lib.mem_linear_backward(a["dz"], a["x"], a["w"], dt, n, N, K, None, a["dx"], None, None, a["x"], ws, None), False)
+    expect(lib, lib.mem_linear_backward(a["dz"], a["x"], a["w"], dt, n, N, K, None, a["dx"], None, None, a["x"], ws, None), False)
 
 
 def adamw(lib, tensors, **opts):
@@ -145,21 +145,21 @@ def test_adamw(lib, gd, sd):
         if any(v % 16 for v in a.values()):
             continue
         t = pk._AdamwTensor(numel=n, param_dt=F32, grad_dt=gd, state_dt=sd, **own)
-        verdict(lib, adamw(lib, [far, t], **{k: a[k] for k in scalars}), bad)
+        expect(lib, adamw(lib, [far, t], **{k: a[k] for k in scalars}), bad)
 
 
 def test_adamw_among_tensors(lib):
     """Gradients may be shared; one tensor's state over another's gradient may not."""
     make = lambda i, g: pk._AdamwTensor(PLACES[3 * i], g, PLACES[3 * i + 1], PLACES[3 * i + 2], None, None, 1000, F32, F32, F32)  # noqa: E731
-    verdict(lib, adamw(lib, [make(0, 1 << 50), make(1, 1 << 50), make(2, (1 << 50) + 400)]), False)
+    expect(lib, adamw(lib, [make(0, 1 << 50), make(1, 1 << 50), make(2, (1 << 50) + 400)]), False)
     for place in (PLACES[0], PLACES[1] + 3996, PLACES[2] - 3996):
-        verdict(lib, adamw(lib, [make(0, 1 << 50), make(1, place)]), True)
-        verdict(lib, adamw(lib, [make(1, place), make(2, 1 << 50), make(0, 1 << 50)]), True)
+        expect(lib, adamw(lib, [make(0, 1 << 50), make(1, place)]), True)
+        expect(lib, adamw(lib, [make(1, place), make(2, 1 << 50), make(0, 1 << 50)]), True)
         assert "gradient" in lib.mem_last_error().decode()
     # a long gradient that begins in front of several short ones
     long = pk._AdamwTensor(1 << 55, 1 << 50, 1 << 56, 1 << 57, None, None, 1 << 20, F32, F32, F32)
     inside = pk._AdamwTensor((1 << 50) + (1 << 21), 1 << 51, 1 << 52, 1 << 53, None, None, 64, F32, F32, F32)
-    verdict(lib, adamw(lib, [long, make(0, (1 << 50) + 64), inside]), True)
+    expect(lib, adamw(lib, [long, make(0, (1 << 50) + 64), inside]), True)
 
 
 def test_adamw_rows(lib):
@@ -169,4 +169,4 @@ def test_adamw_rows(lib):
     for a, bad in cases(sizes, [w for w in sizes if w not in ("grad", "rows")]):
         t = pk._AdamwTensor(numel=n * d, param_dt=F32, grad_dt=F32, state_dt=E4M3, **{k: v for k, v in a.items() if k != "rows"})
         o = pk._AdamwOpts(1e-3, 0.9, 0.999, 1e-8, 0.1, 1, 0)
-        verdict(lib, lib.mem_adamw_rows(ctypes.addressof(t), n, d, a["rows"], u, ctypes.addressof(o), None), bad)
+        expect(lib, lib.mem_adamw_rows(ctypes.addressof(t), n, d, a["rows"], u, ctypes.addressof(o), None), bad)
