@@ -379,7 +379,7 @@ int mem_bag_backward_sparse(const void* dy, const void* values, pkmem_dtype v_dt
  *   y_out   [T, D] dtype y_dt, which is dt, or PKMEM_E4M3: y in 8 bits with one
  *           scale a row, y ~ y_out * scale_out[t],
  *           scale = max(max_j |y| / 448, 2^-126), codes the numbers nearest to
- *           448 y / max_j |y|, ties to even (exact for bf16 rows).  May be
+ *           448 y / max_j |y|, ties to even.  May be
  *           x or res where y_dt is dt (in place, without sum_out there).
  *   scale_out [T] fp32: required for PKMEM_E4M3, NULL otherwise.
  * All buffers 16-byte aligned (scale_out 4).  An output that shares bytes with

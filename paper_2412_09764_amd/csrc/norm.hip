@@ -12,6 +12,8 @@
 // least 79 in turn with its backward, which takes 95 and at least 92 (5.7); to 8 bits
 // 79 (5.9).  Four waves a row are no faster there and slower in the backward (118
 // us).  Below some 4000 rows a call is bound by its launch (2000 rows: 7.5 us of kernel).
+#include <type_traits>
+
 #include "pk_internal.h"
 #include "pk_row.h"
 
@@ -31,14 +33,18 @@ __device__ __forceinline__ float row_sum(float v, float* red, int wave) {
   __syncthreads();  // red is free again
   return v;
 }
-template <int WPR>
-__device__ __forceinline__ float row_max(float v, float* red, int wave) {
+__device__ __forceinline__ float larger(float a, float b) { return fmaxf(a, b); }
+__device__ __forceinline__ double larger(double a, double b) { return fmax(a, b); }
+__device__ __forceinline__ float size_of(float v) { return fabsf(v); }
+__device__ __forceinline__ double size_of(double v) { return fabs(v); }
+template <int WPR, typename U>
+__device__ __forceinline__ U row_max(U v, U* red, int wave) {
 #pragma unroll
-  for (int m = 32; m >= 1; m >>= 1) v = fmaxf(v, __shfl_xor(v, m, WAVE));
+  for (int m = 32; m >= 1; m >>= 1) v = larger(v, __shfl_xor(v, m, WAVE));
   if constexpr (WPR == 1) return v;
   if ((threadIdx.x & 63) == 0) red[wave] = v;
   __syncthreads();
-  v = fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
+  v = larger(larger(red[0], red[1]), larger(red[2], red[3]));
   __syncthreads();
   return v;
 }
@@ -51,9 +57,11 @@ __device__ __forceinline__ float rms_rstd(float ss, int D, float eps) {
 // NORM: the norm, else y = x (rows to 8 bits only).  QUANT: y in e4m3 with
 // scale_out[row] = max(max|y| / 448, 2^-126); the lower limit keeps 1 / scale
 // finite, a row of zeros is codes of zero.  rstd cancels in y / scale, so the codes
-// are those of u = h w (times the power of two of rstd, which keeps it in range)
-// over max|u| / 448: (0.875 u) / (max|u| / 512), where bf16 operands make both
-// sides exact and a value half way between two codes stays there.
+// are those of u / (max|u| / 448) with u = h w (times the power of two of rstd, which
+// keeps it in range).  u is exact: in fp32, where h and w are bf16 or there is no w,
+// with the divisor in two parts and the quotient corrected by its remainder; in fp64
+// for the norm of fp32 rows.  Either way the quotient is rounded once before it is
+// rounded to a code, and a value half way between two codes stays there.
 template <typename T, bool NORM, bool QUANT, int NCH, int WPR>
 __global__ __launch_bounds__(BLOCK) void k_rmsnorm(const T* x, const T* res,
                                                    const T* __restrict__ w, int64_t rows, int D,
@@ -61,6 +69,7 @@ __global__ __launch_bounds__(BLOCK) void k_rmsnorm(const T* x, const T* res,
                                                    float* __restrict__ scale_out) {
   using Ch = Chunk<T>;
   constexpr int N = Ch::N, LANES = WAVE * WPR;
+  using U = typename std::conditional<NORM && sizeof(T) == 4, double, float>::type;
   __shared__ float red[4];
   const int wave = threadIdx.x / WAVE;
   const int lr = WPR == 1 ? (int)(threadIdx.x & 63) : (int)threadIdx.x;
@@ -95,6 +104,7 @@ __global__ __launch_bounds__(BLOCK) void k_rmsnorm(const T* x, const T* res,
     }
   }
   float mant = 1.f;  // QUANT: y = u * mant
+  U u[QUANT ? NCH : 1][N];
   if constexpr (NORM) {
     float rstd = rms_rstd(row_sum<WPR>(ss, red, wave), D, eps);
     if constexpr (QUANT) {
@@ -111,8 +121,16 @@ __global__ __launch_bounds__(BLOCK) void k_rmsnorm(const T* x, const T* res,
       for (int i = 0; i < N; ++i) g[i] = 1.f;
       if (w && ch < C) Ch::unpack(ld16(w + (size_t)ch * N), g);
 #pragma unroll
-      for (int i = 0; i < N; ++i) h[c][i] = h[c][i] * rstd * g[i];
+      for (int i = 0; i < N; ++i) {
+        if constexpr (QUANT) u[c][i] = (U)(h[c][i] * rstd) * g[i];
+        else h[c][i] = h[c][i] * rstd * g[i];
+      }
     }
+  } else {
+#pragma unroll
+    for (int c = 0; c < NCH; ++c)
+#pragma unroll
+      for (int i = 0; i < N; ++i) u[c][i] = h[c][i];
   }
   if constexpr (!QUANT) {
 #pragma unroll
@@ -121,19 +139,23 @@ __global__ __launch_bounds__(BLOCK) void k_rmsnorm(const T* x, const T* res,
       if (ch < C) *reinterpret_cast<uint4*>((T*)y_out + base + (size_t)ch * N) = Ch::pack(h[c]);
     }
   } else {
-    float am = 0.f;
+    __shared__ U top[4];
+    U am = 0;
 #pragma unroll
     for (int c = 0; c < NCH; ++c)
 #pragma unroll
-      for (int i = 0; i < N; ++i) am = fmaxf(am, fabsf(h[c][i]));
-    am = row_max<WPR>(am, red, wave);
-    const float s = am * mant / E4M3_MAX;
+      for (int i = 0; i < N; ++i) am = larger(am, size_of(u[c][i]));
+    am = row_max<WPR>(am, top, wave);
+    const float s = (float)(am * mant / (U)E4M3_MAX);
     const bool low = !(s >= 0x1p-126f);  // the codes are then y / 2^-126
     if (lr == 0) scale_out[row] = low ? 0x1p-126f : s;
-    const float up = low ? mant : 0.875f, div = low ? 0x1p-126f : am * 0x1p-9f, inv = 1.f / div;
-    auto code = [&](float u) {  // u * up / div, correctly rounded
-      const float n = u * up, q = n * inv;
-      return fmaf(fmaf(-q, div, n), inv, q);
+    const U num = low ? (U)0x1p-126f : am, den = low ? mant : E4M3_MAX;
+    const U div = num / den, inv = 1 / div;
+    const U rest = sizeof(U) == 8 ? 0 : fmaf(-div, den, num) * __builtin_amdgcn_rcpf(den);
+    auto code = [&](U v) -> float {
+      if constexpr (sizeof(U) == 8) return (float)(v * inv);
+      const float q = v * inv;
+      return fmaf(fmaf(-q, rest, fmaf(-q, div, v)), inv, q);
     };
 #pragma unroll
     for (int c = 0; c < NCH; ++c) {
@@ -142,7 +164,7 @@ __global__ __launch_bounds__(BLOCK) void k_rmsnorm(const T* x, const T* res,
       uint32_t* out = reinterpret_cast<uint32_t*>((uint8_t*)y_out + base + (size_t)ch * N);
 #pragma unroll
       for (int i = 0; i < N; i += 4)
-        out[i / 4] = to_e4m3x4(code(h[c][i]), code(h[c][i + 1]), code(h[c][i + 2]), code(h[c][i + 3]));
+        out[i / 4] = to_e4m3x4(code(u[c][i]), code(u[c][i + 1]), code(u[c][i + 2]), code(u[c][i + 3]));
     }
   }
 }

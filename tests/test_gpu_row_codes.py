@@ -1,9 +1,9 @@
 """Rows in 8 bits, code by code.  The scale is max|y| / 448 and a code the e4m3
 number nearest to y / scale = 448 y / max|y|, ties to the even code.  In bf16 rows
 448 y is exact in 64 bits (and in 32), so a quotient half way between two codes is
-seen as such: every code has to be equal, ties among them.  fp32 rows round twice
-(2 u, u = 2^-24, of a quotient) and may differ where a quotient lies that near to
-the middle of two codes."""
+seen as such: every code has to be equal, ties among them.  fp32 rows may differ here
+where a quotient lies within 2^-22 of the middle of two codes (of few values, against the
+NumPy grid; test_gpu_row_codes_exact.py asks for every code of many)."""
 import numpy as np
 import pytest
 import torch
