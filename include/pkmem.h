@@ -482,6 +482,77 @@ int mem_linear_backward(const void* dz, const void* x, const void* w, pkmem_dtyp
                         float* grad_bias, void* ws, size_t ws_bytes, pkmem_stream_t stream);
 
 /* ------------------------------------------------------------------------ *
+ * Layer norm with the residual's addition: mem_rmsnorm's place in blocks that centre
+ * their stream.
+ *   h[t,:] = x[t,:] + res[t,:]   added in fp32 and rounded once to dt: the stream as
+ *                                stored is what is normalised;
+ *   y[t,:] = (h[t,:] - mean[t]) * rstd[t] * weight + bias, mean and biased variance
+ *            over the row in fp32 (deviations from a first mean correct both),
+ *            rstd = 1 / sqrt(variance + eps) (0 where that sum is 0 or past the largest
+ *            number: rows with deviations beyond 1e18 may give bias), rounded once to dt.
+ *
+ *   x       [T, D] dtype dt (PKMEM_F32 or PKMEM_BF16).
+ *   res     [T, D] dtype dt; NULL: h = x.
+ *   weight  [D] dtype dt; NULL: ones.   bias [D] dtype dt; NULL: zeros.
+ *   D, eps  as for mem_rmsnorm.
+ *   sum_out [T, D] dtype dt: h; NULL to skip it.  May be x or res (in place).
+ *   y_out   [T, D] dtype dt.  May be x or res (in place, without sum_out there).
+ * All buffers 16-byte aligned.  An output that shares bytes with another buffer in any
+ * other way is refused.  T = 0 is a valid no-op.
+ * ------------------------------------------------------------------------ */
+int mem_layernorm(const void* x, const void* res, const void* weight, const void* bias, pkmem_dtype dt,
+                  int64_t T, int D, float eps, void* sum_out, void* y_out, pkmem_stream_t stream);
+
+/* ------------------------------------------------------------------------ *
+ * Backward of mem_layernorm.  With xh = (h - mean) * rstd (recomputed from h as the
+ * forward did) and g = dy * weight:
+ *   dx_out      [T, D] dtype dt, written: rstd * (g - mean(g) - xh * mean(g * xh)) + dsum;
+ *               the gradient of x and of res alike.  May be dy, h or dsum.
+ *   grad_weight [D] fp32, ACCUMULATED: += sum_t dy * xh; NULL to skip it.
+ *   grad_bias   [D] fp32, ACCUMULATED: += sum_t dy; NULL to skip it.
+ *               Both bitwise deterministic (partial rows added in a fixed order).
+ *   dy, h       [T, D] dtype dt: the gradient of y; x (without res) or sum_out.
+ *   dsum        [T, D] dtype dt: what reaches h along the stream; NULL: none.
+ * Outputs and workspace that share other bytes are refused.  Workspace:
+ * mem_layernorm_backward_workspace_size(T, D) bytes, 256-byte aligned (not needed,
+ * and may be NULL, without both gradients).
+ * ------------------------------------------------------------------------ */
+size_t mem_layernorm_backward_workspace_size(int64_t T, int D);
+
+int mem_layernorm_backward(const void* dy, const void* h, const void* weight, pkmem_dtype dt, int64_t T,
+                           int D, float eps, const void* dsum, void* dx_out, float* grad_weight,
+                           float* grad_bias, void* ws, size_t ws_bytes, pkmem_stream_t stream);
+
+/* ------------------------------------------------------------------------ *
+ * The gated feed-forward part of a block: gate and up projection, activation and
+ * product in one call,
+ *   z[t,:] = x[t,:] W^T (times x_scale[t] * w_scale[n]) + bias,
+ *   y[t,j] = act(z[t,j]) * z[t,N+j]     for j < N,
+ * sums and epilogue in fp32, one rounding to y_dt (y from z as summed, not as stored).
+ *   x       [T, K], w [2 N, K] dtype dt: rows 0 .. N-1 of w are the gate's, rows N .. 2N-1 the
+ *           up projection's.  x_scale [T] and w_scale [2 N] for PKMEM_E4M3, as mem_linear's.
+ *   bias    [2 N] dtype y_dt; NULL: none.
+ *   act     pkmem_act, with mem_linear's precision.
+ *   z_out   [T, 2 N] dtype y_dt: z (what mem_glu_backward needs); NULL to skip it.
+ *   y_out   [T, N] dtype y_dt.
+ * Types, exactness of products and limits as mem_linear's with 2 N in place of N;
+ * N % 8 == 0 and N <= 2^19.  No output may share bytes with another buffer (refused).
+ * All buffers 16-byte aligned.  T = 0 is a valid no-op.
+ * ------------------------------------------------------------------------ */
+int mem_glu(const void* x, const void* w, pkmem_dtype dt, const float* x_scale, const float* w_scale,
+            const void* bias, int64_t T, int N, int K, int act, void* z_out, void* y_out,
+            pkmem_dtype y_dt, pkmem_stream_t stream);
+
+/* Backward of the activation and the product, element-wise: from dy [T, N] and z [T, 2 N]
+ * dtype dt (PKMEM_F32 or PKMEM_BF16),
+ *   dz_out[t,j] = dy[t,j] z[t,N+j] act'(z[t,j]),   dz_out[t,N+j] = dy[t,j] act(z[t,j]),
+ * in fp32, rounded once.  dz_out [T, 2 N] is what mem_linear_backward takes, with 2 N for
+ * its N: one call gives dx, the gradient of both projections and of their biases.
+ * dz_out may be z (sharing bytes with dy or z in any other way is refused). */
+int mem_glu_backward(const void* dy, const void* z, pkmem_dtype dt, int act, int64_t T, int N,
+                     void* dz_out, pkmem_stream_t stream);
+
+/* ------------------------------------------------------------------------ *
  * AdamW (decoupled weight decay) over many tensors in few launches.  With
  * g = grad * *grad_scale (1 where grad_scale is NULL), t = step:
  *   m = beta1 m + (1 - beta1) g;   v = beta2 v + (1 - beta2) g^2
@@ -561,7 +632,8 @@ int mem_adamw_rows(const pkmem_adamw_tensor* table, int64_t N, int D, const int6
  *   "bag_backward_atomic", "sort_by_row",
  *   "bag_backward_rows", "softmax_backward" (mem_bag_backward[_sparse])
  *   "rmsnorm", "rmsnorm_backward", "quantize_rows", "linear", "act_backward",
- *   "linear_backward", "adamw", "adamw_rows"
+ *   "linear_backward", "adamw", "adamw_rows", "layernorm", "layernorm_backward",
+ *   "glu", "glu_backward", "quantize_blocks", "linear_blocks"
  *                                          (the calls of these names)
  * ("sort_by_row" spans the whole radix sort and segment pass.)
  * mem_timer_stop() stops recording.  mem_timer_read(ms_out, kernel_out, cap)

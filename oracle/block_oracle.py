@@ -62,6 +62,25 @@ def rmsnorm_backward(dy, h, w, eps, dsum=None):
     return (dx if dsum is None else dx + dsum), (dy * xh).sum(0)
 
 
+def _layer_stats(h, eps):
+    d = h - h.mean(-1, keepdims=True)
+    var = (d * d).mean(-1, keepdims=True) + eps
+    return d, np.where(var == 0, 0.0, 1 / np.sqrt(np.where(var == 0, 1.0, var)))
+
+
+def layernorm(h, w, b, eps):
+    d, rstd = _layer_stats(h, eps)
+    return d * rstd * w + b
+
+
+def layernorm_backward(dy, h, w, eps, dsum=None):
+    """(dx, grad_weight, grad_bias) of sum(dy * layernorm(h)), plus dsum into dx."""
+    d, rstd = _layer_stats(h, eps)
+    xh, g = d * rstd, dy * w
+    dx = rstd * (g - g.mean(-1, keepdims=True) - xh * (g * xh).mean(-1, keepdims=True))
+    return (dx if dsum is None else dx + dsum), (dy * xh).sum(0), dy.sum(0)
+
+
 # -------------------------------------------------------------- projections ----
 _erf = np.vectorize(math.erf, otypes=[float])
 
@@ -100,6 +119,38 @@ def linear_backward(dz, x, w, add=None):
     """(dx, grad_w, grad_bias)."""
     dx = dz @ w
     return (dx if add is None else dx + add), dz.T @ x, dz.sum(0)
+
+
+def glu(x, w, b, name):
+    """(act(gate) * up, z) with z = x w^T + b, its first half the gate."""
+    z = x @ w.T + b
+    n = z.shape[1] // 2
+    return act(z[:, :n], name) * z[:, n:], z
+
+
+def glu_backward(dy, z, name):
+    n = z.shape[1] // 2
+    gate, up = z[:, :n], z[:, n:]
+    return np.concatenate([dy * up * act_grad(gate, name), dy * act(gate, name)], 1)
+
+
+# ------------------------------------------------------------ 8 bits in blocks ----
+def quantize_blocks(x, rows):
+    """(values on the grid, scale of each element, scales [column block, row block]) of x in
+    blocks of `rows` x 128: scale = max(max|x| / 448, 2^-126)."""
+    R, C = x.shape
+    q, each = np.empty_like(x), np.empty_like(x)
+    s = np.empty((-(-C // BLOCK), -(-R // rows)))
+    for j in range(s.shape[0]):
+        for i in range(s.shape[1]):
+            at = np.s_[i * rows:(i + 1) * rows, j * BLOCK:(j + 1) * BLOCK]
+            big = np.abs(x[at]).max()
+            low = big < E4M3_MAX * 2.0 ** -126
+            s[j, i] = 2.0 ** -126 if low else big / E4M3_MAX
+            each[at] = s[j, i]
+            # 448 x / max: exact where it lies on a border
+            q[at] = to_e4m3(x[at] * 2.0 ** 126 if low else x[at] * E4M3_MAX / big)
+    return q, each, s
 
 
 # -------------------------------------------------------------------- AdamW ----

@@ -33,6 +33,7 @@ __all__ = [
     "BWD_MODES", "F32", "BF16", "mem_timer_start", "mem_timer_stop", "mem_timer_read",
     "E4M3", "mem_rmsnorm", "mem_rmsnorm_backward", "mem_quantize_rows",
     "mem_linear", "mem_act_backward", "mem_linear_backward", "ACTIVATIONS",
+    "mem_layernorm", "mem_layernorm_backward", "mem_glu", "mem_glu_backward",
     "mem_adamw", "mem_adamw_rows", "mem_adamw_state", "ADAMW_STATE_BLOCK",
 ]
 
@@ -122,6 +123,16 @@ def load() -> ctypes.CDLL:
     L.mem_linear_backward_workspace_size.restype = SZ
     L.mem_linear_backward.argtypes = [P, P, P, I32, I64, I32, I32, P, P, P, P, P, SZ, P]
     L.mem_linear_backward.restype = I32
+    L.mem_layernorm.argtypes = [P, P, P, P, I32, I64, I32, F32, P, P, P]
+    L.mem_layernorm.restype = I32
+    L.mem_layernorm_backward_workspace_size.argtypes = [I64, I32]
+    L.mem_layernorm_backward_workspace_size.restype = SZ
+    L.mem_layernorm_backward.argtypes = [P, P, P, I32, I64, I32, F32, P, P, P, P, P, SZ, P]
+    L.mem_layernorm_backward.restype = I32
+    L.mem_glu.argtypes = [P, P, I32, P, P, P, I64, I32, I32, I32, P, P, I32, P]
+    L.mem_glu.restype = I32
+    L.mem_glu_backward.argtypes = [P, P, I32, I32, I64, I32, P, P]
+    L.mem_glu_backward.restype = I32
     L.mem_adamw.argtypes = [P, I32, P, P]
     L.mem_adamw.restype = I32
     L.mem_adamw_rows.argtypes = [P, I64, I32, P, I64, P, P]
@@ -808,6 +819,135 @@ def mem_linear_backward(dz: torch.Tensor, x: torch.Tensor, w: torch.Tensor, *, d
                                  0 if ws is None else ws.numel() * ws.element_size(),
                                  _stream(stream)))
     return dx, grad_w, grad_bias
+
+
+@_launches_on_stream
+def mem_layernorm(x: torch.Tensor, weight=None, bias=None, residual=None, eps: float = 1e-5, *,
+                  sum_out=None, y_out=None, want_sum: bool = True, stream=None):
+    """Layer norm of h = x + residual ([T, D]; residual may be None).
+
+    Returns (y, h), both in x's dtype; h None without a residual or with want_sum False
+    unless sum_out is given (it may be x or residual)."""
+    _here(x, weight, bias, residual, sum_out, y_out)
+    shape, xdt = x.shape, x.dtype
+    T, D = shape
+    dt = _dt(x)
+    wp = bp = rp = hp = None
+    if weight is not None:
+        _like(weight, (D,), xdt, "weight")
+        wp = weight.data_ptr()
+    if bias is not None:
+        _like(bias, (D,), xdt, "bias")
+        bp = bias.data_ptr()
+    if residual is not None:
+        _like(residual, shape, xdt, "residual")
+        rp = residual.data_ptr()
+        if sum_out is None and want_sum:
+            sum_out = torch.empty_like(x)
+    if sum_out is not None:
+        _like(sum_out, shape, xdt, "sum_out")
+        hp = sum_out.data_ptr()
+    if y_out is None:
+        y_out = torch.empty_like(x)
+    else:
+        _like(y_out, shape, xdt, "y_out")
+    _check((_LIB or load()).mem_layernorm(x.data_ptr(), rp, wp, bp, dt, T, D, eps, hp, y_out.data_ptr(),
+                                          _stream(stream)))
+    return y_out, sum_out
+
+
+@_launches_on_stream
+def mem_layernorm_backward(dy: torch.Tensor, h: torch.Tensor, weight=None, eps: float = 1e-5, *,
+                           dsum=None, dx=None, grad_weight=None, grad_bias=None,
+                           want_grad_weight: bool = True, want_grad_bias: bool = True,
+                           workspace=None, stream=None):
+    """Backward of mem_layernorm: dy the gradient of y, h what was normalised (its sum, or x
+    without a residual), dsum what reaches h along the stream (or None).  Returns (dx [T, D]
+    in dy's dtype, the gradient of x and residual alike; grad_weight and grad_bias fp32 [D],
+    ACCUMULATED: zeros are allocated if none is given)."""
+    L = load()
+    _here(dy, h, weight, dsum, dx, grad_weight, grad_bias, workspace)
+    T, D = dy.shape
+    dt = _dt(dy)
+    _like(h, (T, D), dy.dtype, "h")
+    _like(weight, (D,), dy.dtype, "weight")
+    _like(dsum, (T, D), dy.dtype, "dsum")
+    if dx is None:
+        dx = torch.empty_like(dy)
+    _like(dx, (T, D), dy.dtype, "dx")
+    if grad_weight is None and want_grad_weight:
+        grad_weight = torch.zeros((D,), dtype=torch.float32, device=dy.device)
+    if grad_bias is None and want_grad_bias:
+        grad_bias = torch.zeros((D,), dtype=torch.float32, device=dy.device)
+    _like(grad_weight, (D,), torch.float32, "grad_weight")
+    _like(grad_bias, (D,), torch.float32, "grad_bias")
+    ws = None
+    if grad_weight is not None or grad_bias is not None:
+        ws = _workspace(int(L.mem_layernorm_backward_workspace_size(T, D)), dy.device, workspace)
+    _check(L.mem_layernorm_backward(_ptr(dy), _ptr(h), _ptr(weight), dt, T, D, float(eps), _ptr(dsum),
+                                    _ptr(dx), _ptr(grad_weight), _ptr(grad_bias), _ptr(ws),
+                                    0 if ws is None else ws.numel() * ws.element_size(),
+                                    _stream(stream)))
+    return dx, grad_weight, grad_bias
+
+
+@_launches_on_stream
+def mem_glu(x: torch.Tensor, w: torch.Tensor, bias=None, *, act="silu", x_scale=None, w_scale=None,
+            out_dtype=None, y_out=None, z_out=None, want_z: bool = False, stream=None):
+    """The gated feed-forward part: with z = x w^T + bias, act(z[:, :N]) * z[:, N:].
+
+    x [T, K]; w [2 N, K] (the gate's N rows, then the up projection's), bias [2 N]; act, 8-bit
+    operands with x_scale [T] and w_scale [2 N], and out_dtype as for mem_linear.
+    Returns (y [T, N], z [T, 2 N], None unless want_z)."""
+    _here(x, w, bias, x_scale, w_scale, y_out, z_out)
+    T, K = x.shape
+    N2, xdt = w.shape[0], x.dtype
+    _like(w, (N2, K), xdt, "w")
+    if N2 % 2:
+        raise ValueError("w must have a gate's and as many of an up projection's rows")
+    sx = sw = bp = zp = None
+    if xdt is torch.float8_e4m3fn:
+        dt = E4M3
+        if x_scale is None or w_scale is None:
+            raise ValueError("float8_e4m3fn operands need x_scale and w_scale")
+        _like(x_scale, (T,), torch.float32, "x_scale")
+        _like(w_scale, (N2,), torch.float32, "w_scale")
+    else:
+        dt = _dt(x)
+    sx, sw = _ptr(x_scale), _ptr(w_scale)  # refused by the call beside other operands
+    if out_dtype is None:
+        out_dtype = torch.bfloat16 if dt == E4M3 else xdt
+    if y_out is None:
+        y_out = x.new_empty((T, N2 // 2), dtype=out_dtype)
+    else:
+        _like(y_out, (T, N2 // 2), out_dtype, "y_out")
+    if z_out is None and want_z:
+        z_out = x.new_empty((T, N2), dtype=out_dtype)
+    if z_out is not None:
+        _like(z_out, (T, N2), out_dtype, "z_out")
+        zp = z_out.data_ptr()
+    if bias is not None:
+        _like(bias, (N2,), out_dtype, "bias")
+        bp = bias.data_ptr()
+    _check((_LIB or load()).mem_glu(x.data_ptr(), w.data_ptr(), dt, sx, sw, bp, T, N2 // 2, K, _act(act),
+                                    zp, y_out.data_ptr(), _dt(y_out), _stream(stream)))
+    return y_out, z_out
+
+
+@_launches_on_stream
+def mem_glu_backward(dy: torch.Tensor, z: torch.Tensor, act="silu", *, dz_out=None, stream=None):
+    """dz [T, 2 N] of mem_glu from dy [T, N] and its z [T, 2 N]; dz_out may be z.  Then
+    mem_linear_backward(dz, x, w) gives the gradients of x, w and bias."""
+    L = load()
+    _here(dy, z, dz_out)
+    T, N = dy.shape
+    dt = _dt(dy)
+    _like(z, (T, 2 * N), dy.dtype, "z")
+    if dz_out is None:
+        dz_out = torch.empty_like(z)
+    _like(dz_out, (T, 2 * N), dy.dtype, "dz_out")
+    _check(L.mem_glu_backward(_ptr(dy), _ptr(z), dt, _act(act), T, N, _ptr(dz_out), _stream(stream)))
+    return dz_out
 
 
 class _AdamwTensor(ctypes.Structure):  # pkmem_adamw_tensor

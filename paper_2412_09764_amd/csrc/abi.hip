@@ -896,6 +896,61 @@ int mem_quantize_rows(const void* x, pkmem_dtype dt, int64_t R, int C, void* q_o
                                              reinterpret_cast<hipStream_t>(stream)), fn);
 }
 
+int mem_layernorm(const void* x, const void* res, const void* weight, const void* bias, pkmem_dtype dt,
+                  int64_t T, int D, float eps, void* sum_out, void* y_out, pkmem_stream_t stream) {
+  const char* fn = "mem_layernorm";
+  int rc = check_rows_shape(fn, dt, T, D);
+  if (rc) return rc;
+  if (!(eps >= 0.f && eps <= 3.0e38f)) return fail(PKMEM_ERR_INVALID, "%s: eps must be finite and >= 0", fn);
+  if (T > 0 && (!x || !y_out)) return fail(PKMEM_ERR_INVALID, "%s: null pointer", fn);
+  if (sum_out && sum_out == y_out) return fail(PKMEM_ERR_INVALID, "%s: sum_out and y_out are one buffer", fn);
+  if (!aligned(x, 16) || !aligned(res, 16) || !aligned(weight, 16) || !aligned(bias, 16) || !aligned(sum_out, 16) ||
+      !aligned(y_out, 16))
+    return fail(PKMEM_ERR_INVALID, "%s: buffers must be 16-byte aligned", fn);
+  if (T == 0) return PKMEM_OK;
+  const size_t rows = (size_t)T * D * esize(dt);
+  const Bytes bx{x, rows}, br{res, rows}, bw{weight, D * esize(dt)}, bb{bias, D * esize(dt)}, bs{sum_out, rows}, by{y_out, rows};
+  if (over(bs, {bw, bb, by}, {bx, br}) || over(by, {bw, bb}, {bx, br}))
+    return fail(PKMEM_ERR_INVALID, "%s: an output may be x or res itself and share no other bytes with a buffer", fn);
+  return hip_status(pk::launch_layernorm(dt == PKMEM_BF16, x, res, weight, bias, T, D, eps, sum_out, y_out,
+                                         reinterpret_cast<hipStream_t>(stream)), fn);
+}
+
+size_t mem_layernorm_backward_workspace_size(int64_t T, int D) {
+  if (T < 0 || D < 1) return 0;
+  return align256(pk::layernorm_backward_ws_bytes(T, D));
+}
+
+int mem_layernorm_backward(const void* dy, const void* h, const void* weight, pkmem_dtype dt, int64_t T, int D,
+                           float eps, const void* dsum, void* dx_out, float* grad_weight, float* grad_bias,
+                           void* ws, size_t ws_bytes, pkmem_stream_t stream) {
+  const char* fn = "mem_layernorm_backward";
+  int rc = check_rows_shape(fn, dt, T, D);
+  if (rc) return rc;
+  if (!(eps >= 0.f && eps <= 3.0e38f)) return fail(PKMEM_ERR_INVALID, "%s: eps must be finite and >= 0", fn);
+  if (T > 0 && (!dy || !h || !dx_out)) return fail(PKMEM_ERR_INVALID, "%s: null pointer", fn);
+  if (!aligned(dy, 16) || !aligned(h, 16) || !aligned(weight, 16) || !aligned(dsum, 16) || !aligned(dx_out, 16) ||
+      !aligned(grad_weight, 4) || !aligned(grad_bias, 4))
+    return fail(PKMEM_ERR_INVALID, "%s: buffers must be 16-byte aligned (grad_weight, grad_bias 4)", fn);
+  const bool grads = grad_weight || grad_bias;
+  const size_t need = mem_layernorm_backward_workspace_size(T, D);
+  if (grads) {
+    if (need > 0 && (!ws || ws_bytes < need))
+      return fail(PKMEM_ERR_WORKSPACE, "%s: workspace of %zu bytes needed, %zu given", fn, need, ws ? ws_bytes : (size_t)0);
+    if (!aligned(ws, 256)) return fail(PKMEM_ERR_INVALID, "%s: workspace must be 256-byte aligned", fn);
+  }
+  if (T == 0) return PKMEM_OK;
+  const size_t rows = (size_t)T * D * esize(dt);
+  const Bytes bdy{dy, rows}, bh{h, rows}, bd{dsum, rows}, bx{dx_out, rows}, bw{weight, D * esize(dt)},
+      bgw{grad_weight, (size_t)D * 4}, bgb{grad_bias, (size_t)D * 4}, bws{grads ? ws : nullptr, need};
+  if (over(bx, {bw, bgw, bgb, bws}, {bdy, bh, bd}) || over(bgw, {bdy, bh, bd, bw, bgb, bws}) ||
+      over(bgb, {bdy, bh, bd, bw, bws}) || over(bws, {bdy, bh, bd, bw}))
+    return fail(PKMEM_ERR_INVALID, "%s: dx_out may be dy, h or dsum itself; outputs and workspace may share no other bytes", fn);
+  return hip_status(pk::launch_layernorm_backward(dt == PKMEM_BF16, dy, h, weight, dsum, T, D, eps, dx_out, grad_weight,
+                                                  grad_bias, reinterpret_cast<float*>(ws),
+                                                  reinterpret_cast<hipStream_t>(stream)), fn);
+}
+
 int mem_adamw(const pkmem_adamw_tensor* tensors, int count, const pkmem_adamw_opts* opts,
               pkmem_stream_t stream) {
   const char* fn = "mem_adamw";
@@ -1053,6 +1108,53 @@ int mem_linear_backward(const void* dz, const void* x, const void* w, pkmem_dtyp
   return hip_status(pk::launch_linear_backward(dt == PKMEM_BF16, dz, x, w, T, N, K, dx_add, dx_out,
                                                grad_w, grad_bias, ws,
                                                reinterpret_cast<hipStream_t>(stream)), fn);
+}
+
+int mem_glu(const void* x, const void* w, pkmem_dtype dt, const float* x_scale, const float* w_scale, const void* bias,
+            int64_t T, int N, int K, int act, void* z_out, void* y_out, pkmem_dtype y_dt, pkmem_stream_t stream) {
+  const char* fn = "mem_glu";
+  int rc = check_linear_shapes(fn, dt, true, T, N, K);
+  if (rc) return rc;
+  if (N > (1 << 19)) return fail(PKMEM_ERR_UNSUPPORTED, "%s: N must be <= 2^19", fn);
+  if (!tiles_fit(T, 2 * N)) return fail(PKMEM_ERR_UNSUPPORTED, "%s: 2^23 tiles of 256 x 256 or more", fn);
+  if (!dtype_ok(y_dt) || (dt == PKMEM_F32 && y_dt != PKMEM_F32))
+    return fail(PKMEM_ERR_INVALID, "%s: y_dt must be PKMEM_F32 or PKMEM_BF16 (PKMEM_F32 for fp32 operands)", fn);
+  if (act < PKMEM_ACT_NONE || act > PKMEM_ACT_GELU) return fail(PKMEM_ERR_INVALID, "%s: unknown activation %d", fn, act);
+  if (dt != PKMEM_E4M3 && (x_scale || w_scale))
+    return fail(PKMEM_ERR_INVALID, "%s: scales belong to PKMEM_E4M3 operands", fn);
+  if (T > 0 && (!x || !w || !y_out || (dt == PKMEM_E4M3 && (!x_scale || !w_scale))))
+    return fail(PKMEM_ERR_INVALID, "%s: null pointer", fn);
+  if (!aligned(x, 16) || !aligned(w, 16) || !aligned(x_scale, 4) || !aligned(w_scale, 16) || !aligned(bias, 16) ||
+      !aligned(z_out, 16) || !aligned(y_out, 16))
+    return fail(PKMEM_ERR_INVALID, "%s: buffers must be 16-byte aligned", fn);
+  if (T == 0) return PKMEM_OK;
+  const size_t e = dt == PKMEM_E4M3 ? 1 : esize(dt), ye = esize(y_dt), out = (size_t)T * N * ye;
+  const Bytes bx{x, (size_t)T * K * e}, bw{w, 2 * (size_t)N * K * e}, bsx{x_scale, (size_t)T * 4},
+      bsw{w_scale, 2 * (size_t)N * 4}, bb{bias, 2 * N * ye}, bz{z_out, 2 * out}, by{y_out, out};
+  if (over(by, {bx, bw, bsx, bsw, bb, bz}) || over(bz, {bx, bw, bsx, bsw, bb}))
+    return fail(PKMEM_ERR_INVALID, "%s: an output may share no bytes with another buffer", fn);
+  const pk::LinearCall c{x, w, dt, x_scale, w_scale, bias, nullptr, T, N, K, act, z_out, y_out, y_dt == PKMEM_BF16};
+  return hip_status(pk::launch_glu(c, reinterpret_cast<hipStream_t>(stream)), fn);
+}
+
+int mem_glu_backward(const void* dy, const void* z, pkmem_dtype dt, int act, int64_t T, int N, void* dz_out,
+                     pkmem_stream_t stream) {
+  const char* fn = "mem_glu_backward";
+  if (!dtype_ok(dt)) return fail(PKMEM_ERR_INVALID, "%s: unknown dtype %d", fn, (int)dt);
+  if (act < PKMEM_ACT_NONE || act > PKMEM_ACT_GELU) return fail(PKMEM_ERR_INVALID, "%s: unknown activation %d", fn, act);
+  if (T < 0) return fail(PKMEM_ERR_INVALID, "%s: T must be >= 0", fn);
+  if (T > 0x7FFFFFFF) return fail(PKMEM_ERR_UNSUPPORTED, "%s: T must be < 2^31", fn);
+  if (N < 8 || N % 8 != 0 || N > (1 << 19))
+    return fail(PKMEM_ERR_UNSUPPORTED, "%s: N must be a positive multiple of 8, at most 2^19 (got %d)", fn, N);
+  if (T > 0 && (!dy || !z || !dz_out)) return fail(PKMEM_ERR_INVALID, "%s: null pointer", fn);
+  if (!aligned(dy, 16) || !aligned(z, 16) || !aligned(dz_out, 16))
+    return fail(PKMEM_ERR_INVALID, "%s: buffers must be 16-byte aligned", fn);
+  if (T == 0) return PKMEM_OK;
+  const size_t n = (size_t)T * N * esize(dt);
+  if (over({dz_out, 2 * n}, {{dy, n}}, {{z, 2 * n}}))
+    return fail(PKMEM_ERR_INVALID, "%s: dz_out may be z itself and share no other bytes with dy or z", fn);
+  return hip_status(pk::launch_glu_backward(dt == PKMEM_BF16, dy, z, act, T, N, dz_out,
+                                            reinterpret_cast<hipStream_t>(stream)), fn);
 }
 
 }  // extern "C"

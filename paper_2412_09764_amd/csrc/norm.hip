@@ -15,24 +15,12 @@
 #include <type_traits>
 
 #include "pk_internal.h"
-#include "pk_row.h"
+#include "pk_norm.h"
 
 namespace pk {
 
 namespace {
 
-constexpr int BLOCK = 256;
-
-template <int WPR>
-__device__ __forceinline__ float row_sum(float v, float* red, int wave) {
-  v = group_sum<WAVE>(v);
-  if constexpr (WPR == 1) return v;
-  if ((threadIdx.x & 63) == 0) red[wave] = v;
-  __syncthreads();
-  v = (red[0] + red[1]) + (red[2] + red[3]);
-  __syncthreads();  // red is free again
-  return v;
-}
 __device__ __forceinline__ float larger(float a, float b) { return fmaxf(a, b); }
 __device__ __forceinline__ double larger(double a, double b) { return fmax(a, b); }
 __device__ __forceinline__ float size_of(float v) { return fabsf(v); }
@@ -296,21 +284,6 @@ __global__ __launch_bounds__(1024) void k_add_rows(const float* __restrict__ par
   }
 }
 
-// Chunks per lane and waves per row for rows of C chunks: one wave up to 512
-// chunks (8 KiB), a workgroup of four above.
-#define PK_NORM_DISPATCH(C, F)                                            \
-  do {                                                                    \
-    if ((C) <= 64) { F(1, 1); }                                           \
-    else if ((C) <= 128) { F(2, 1); }                                     \
-    else if ((C) <= 256) { F(4, 1); }                                     \
-    else if ((C) <= 512) { F(8, 1); }                                     \
-    else if ((C) <= 1024) { F(4, 4); }                                    \
-    else { F(8, 4); }                                                     \
-  } while (0)
-
-// One launch holds fewer than 2^32 threads: more rows go in several.
-constexpr int64_t LAUNCH_WORKGROUPS = 1 << 23;
-
 template <typename T, bool NORM, bool QUANT>
 void norm_launch(const void* x, const void* res, const void* w, int64_t rows, int D, float eps,
                  void* sum_out, void* y_out, float* scale_out, hipStream_t st) {
@@ -329,13 +302,6 @@ void norm_launch(const void* x, const void* res, const void* w, int64_t rows, in
   }
   PK_NORM_DISPATCH(C, PK_F);
 #undef PK_F
-}
-
-// Workgroups of the backward, fixed by the number of rows: the parts that
-// grad_weight is added up from do not depend on the machine.
-int norm_parts(int64_t rows) {
-  const int64_t b = (rows + 3) / 4;
-  return (int)(b < 512 ? b : 512);
 }
 
 template <typename T>

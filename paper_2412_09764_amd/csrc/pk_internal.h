@@ -148,6 +148,16 @@ hipError_t launch_rmsnorm_backward(bool bf16, const void* dy, const void* h, con
 // out[c] += the sum over p of part[p, c], in a fixed order.
 void launch_add_rows(const float* part, int parts, int cols, float* out, hipStream_t st);
 
+// ---- layer norm (layernorm.hip) --------------------------------------------
+// res, w, b, sum_out nullable.
+hipError_t launch_layernorm(bool bf16, const void* x, const void* res, const void* w, const void* b,
+                            int64_t rows, int D, float eps, void* sum_out, void* y_out, hipStream_t st);
+size_t layernorm_backward_ws_bytes(int64_t rows, int D);
+// w, dsum, grad_weight, grad_bias nullable; part: the workspace where there is a gradient.
+hipError_t launch_layernorm_backward(bool bf16, const void* dy, const void* h, const void* w,
+                                     const void* dsum, int64_t rows, int D, float eps, void* dx,
+                                     float* grad_weight, float* grad_bias, float* part, hipStream_t st);
+
 // ---- projections (linear.hip) ----------------------------------------------
 struct LinearCall {
   const void* x;
@@ -171,6 +181,12 @@ size_t linear_backward_ws_bytes(bool bf16, int64_t T, int N, int K);
 hipError_t launch_linear_backward(bool bf16, const void* dz, const void* x, const void* w, int64_t T,
                                   int N, int K, const void* add, void* dx, float* grad_w,
                                   float* grad_bias, void* ws, hipStream_t st);
+
+// ---- gated feed-forward part (glu.hip) -------------------------------------
+// w [2 N, K], w_scale and bias [2 N], z [T, 2 N]; no res.
+hipError_t launch_glu(const LinearCall& c, hipStream_t st);
+hipError_t launch_glu_backward(bool bf16, const void* dy, const void* z, int act, int64_t T, int N, void* dz,
+                               hipStream_t st);
 
 // ---- optimizer (adamw.hip) -------------------------------------------------
 constexpr int ADAMW_STATE_BLOCK = 128;  // elements that share the scales of 8-bit states

@@ -1,0 +1,60 @@
+// What the norms of rows share: sums over the lanes that hold a row, and how rows are
+// laid on waves and workgroups.
+#pragma once
+
+#include "pk_row.h"
+
+namespace pk {
+
+constexpr int BLOCK = 256;
+
+template <int WPR>
+__device__ __forceinline__ float row_sum(float v, float* red, int wave) {
+  v = group_sum<WAVE>(v);
+  if constexpr (WPR == 1) return v;
+  if ((threadIdx.x & 63) == 0) red[wave] = v;
+  __syncthreads();
+  v = (red[0] + red[1]) + (red[2] + red[3]);
+  __syncthreads();  // red is free again
+  return v;
+}
+// M sums at once; red holds 4 M numbers.
+template <int WPR, int M>
+__device__ __forceinline__ void row_sums(float (&v)[M], float* red, int wave) {
+#pragma unroll
+  for (int i = 0; i < M; ++i) v[i] = group_sum<WAVE>(v[i]);
+  if constexpr (WPR > 1) {
+    if ((threadIdx.x & 63) == 0) {
+#pragma unroll
+      for (int i = 0; i < M; ++i) red[wave * M + i] = v[i];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < M; ++i) v[i] = (red[i] + red[M + i]) + (red[2 * M + i] + red[3 * M + i]);
+    __syncthreads();
+  }
+}
+
+// Chunks per lane and waves per row for rows of C chunks: one wave up to 512
+// chunks (8 KiB), a workgroup of four above.
+#define PK_NORM_DISPATCH(C, F)                                            \
+  do {                                                                    \
+    if ((C) <= 64) { F(1, 1); }                                           \
+    else if ((C) <= 128) { F(2, 1); }                                     \
+    else if ((C) <= 256) { F(4, 1); }                                     \
+    else if ((C) <= 512) { F(8, 1); }                                     \
+    else if ((C) <= 1024) { F(4, 4); }                                    \
+    else { F(8, 4); }                                                     \
+  } while (0)
+
+// One launch holds fewer than 2^32 threads: more rows go in several.
+constexpr int64_t LAUNCH_WORKGROUPS = 1 << 23;
+
+// Workgroups of the backward, fixed by the number of rows: the parts that
+// grad_weight is added up from do not depend on the machine.
+inline int norm_parts(int64_t rows) {
+  const int64_t b = (rows + 3) / 4;
+  return (int)(b < 512 ? b : 512);
+}
+
+}  // namespace pk
