@@ -553,6 +553,44 @@ int mem_glu_backward(const void* dy, const void* z, pkmem_dtype dt, int act, int
                      void* dz_out, pkmem_stream_t stream);
 
 /* ------------------------------------------------------------------------ *
+ * A matrix in 8 bits with a scale for each block of 128 elements: the operands of
+ * mem_linear_blocks, as rows, as columns (transposed codes), or both from one reading.
+ *   x       [R, C] dtype dt (PKMEM_F32 or PKMEM_BF16), C % 16 == 0, C <= 2^20.
+ *   tile    0: a block is 128 consecutive elements of a row (of a column for qt_out),
+ *           otherwise 128 x 128 elements (weights: the same codes both ways).
+ *   q_out   [R, C] PKMEM_E4M3 with scale_out fp32 [ceil(C / 128), R] (tile: [ceil(C / 128),
+ *           ceil(R / 128)]): x[r,c] ~ q_out[r,c] * scale_out[c / 128, r (r / 128)].
+ *   qt_out  [C, R16] PKMEM_E4M3, R16 = R rounded up to 16, codes past R zero, with
+ *           scale_t_out fp32 [ceil(R / 128), C] (tile: [ceil(R / 128), ceil(C / 128)]).
+ *   scale = max(max|x| / 448, 2^-126) of the block, codes the numbers nearest to
+ *   448 x / max|x|, ties to even, exactly.
+ * Either pair may be NULL.  Buffers 16-byte aligned, scales 4; no two may share bytes
+ * (refused).  R = 0 is a valid no-op.
+ * ------------------------------------------------------------------------ */
+int mem_quantize_blocks(const void* x, pkmem_dtype dt, int64_t R, int C, int tile, void* q_out,
+                        float* scale_out, void* qt_out, float* scale_t_out, pkmem_stream_t stream);
+
+/* ------------------------------------------------------------------------ *
+ * mem_linear for operands in blocks: with b = k / 128,
+ *   z[t,n] = sum_k x[t,k] x_scale[b,t] w[n,k] w_scale[b,n] + bias[n],
+ *   y[t,:] = act(z[t,:]) + res[t,:].
+ *   x  [T, K], w [N, K] PKMEM_E4M3; x_scale [ceil(K / 128), T]; w_scale [ceil(K / 128), N], or
+ *      with w_tile [ceil(K / 128), ceil(N / 128)], one for each 128 rows of w.
+ *   bias, res, act, z_out, y_out, y_dt, limits (K % 16 == 0) and refusals as mem_linear's.
+ *   Sums: for y_dt PKMEM_F32, and for up to 8 tokens, products are exact and added in
+ *   fp32.  For PKMEM_BF16 the products of 8 k are aligned to the largest of them and cut 13
+ *   bits below it, and then added in fp32: each is within 2^-13 of that largest one, far
+ *   below half a step of the result unless the sum cancels.
+ * The products of a training step: y from x and w; dx [T, K] from the gradient's rows and
+ * w's columns (qt_out as w, N and K changed round); grad_w from both columns, with
+ * res = y_out = grad_w in PKMEM_F32 to accumulate.
+ * w_scale 16-byte aligned without w_tile, x_scale (and w_scale with it) 4, others 16.
+ * ------------------------------------------------------------------------ */
+int mem_linear_blocks(const void* x, const void* w, const float* x_scale, const float* w_scale,
+                      int w_tile, const void* bias, const void* res, int64_t T, int N, int K, int act,
+                      void* z_out, void* y_out, pkmem_dtype y_dt, pkmem_stream_t stream);
+
+/* ------------------------------------------------------------------------ *
  * AdamW (decoupled weight decay) over many tensors in few launches.  With
  * g = grad * *grad_scale (1 where grad_scale is NULL), t = step:
  *   m = beta1 m + (1 - beta1) g;   v = beta2 v + (1 - beta2) g^2

@@ -34,12 +34,14 @@ __all__ = [
     "E4M3", "mem_rmsnorm", "mem_rmsnorm_backward", "mem_quantize_rows",
     "mem_linear", "mem_act_backward", "mem_linear_backward", "ACTIVATIONS",
     "mem_layernorm", "mem_layernorm_backward", "mem_glu", "mem_glu_backward",
+    "mem_quantize_blocks", "mem_linear_blocks", "SCALE_BLOCK",
     "mem_adamw", "mem_adamw_rows", "mem_adamw_state", "ADAMW_STATE_BLOCK",
 ]
 
 F32, BF16, E4M3 = 0, 1, 2
 ACTIVATIONS = {"none": 0, "relu": 1, "silu": 2, "gelu": 3}
 ADAMW_STATE_BLOCK = 128  # elements that share the scales of 8-bit optimizer states
+SCALE_BLOCK = 128  # elements along k (rows and columns of a tile) that share a scale
 NOALLOC_SCRATCH_BYTES = 128 << 20  # PKMEM_NOALLOC_SCRATCH_BYTES
 BWD_MODES = {"auto": 0, "atomic": 1, "sorted": 2}
 _HERE = os.path.dirname(os.path.abspath(__file__))
@@ -133,6 +135,10 @@ def load() -> ctypes.CDLL:
     L.mem_glu.restype = I32
     L.mem_glu_backward.argtypes = [P, P, I32, I32, I64, I32, P, P]
     L.mem_glu_backward.restype = I32
+    L.mem_quantize_blocks.argtypes = [P, I32, I64, I32, I32, P, P, P, P, P]
+    L.mem_quantize_blocks.restype = I32
+    L.mem_linear_blocks.argtypes = [P, P, P, P, I32, P, P, I64, I32, I32, I32, P, P, I32, P]
+    L.mem_linear_blocks.restype = I32
     L.mem_adamw.argtypes = [P, I32, P, P]
     L.mem_adamw.restype = I32
     L.mem_adamw_rows.argtypes = [P, I64, I32, P, I64, P, P]
@@ -948,6 +954,95 @@ def mem_glu_backward(dy: torch.Tensor, z: torch.Tensor, act="silu", *, dz_out=No
     _like(dz_out, (T, 2 * N), dy.dtype, "dz_out")
     _check(L.mem_glu_backward(_ptr(dy), _ptr(z), dt, _act(act), T, N, _ptr(dz_out), _stream(stream)))
     return dz_out
+
+
+@_launches_on_stream
+def mem_quantize_blocks(x: torch.Tensor, *, tile: bool = False, want_rows: bool = True,
+                        want_cols: bool = False, q_out=None, scale_out=None, qt_out=None,
+                        scale_t_out=None, stream=None):
+    """x [R, C] in 8 bits with a scale for each 128 elements of a row (tile: each 128 x 128).
+
+    Returns (q, scale, qt, scale_t), what is not wanted None: q float8_e4m3fn [R, C] with scale
+    fp32 [ceil(C/128), R] (tile: [ceil(C/128), ceil(R/128)]), and the same of x's columns:
+    qt [C, R rounded up to 16] (zeros past R) with scale_t [ceil(R/128), C] (tile:
+    [ceil(R/128), ceil(C/128)]).  They are operands of mem_linear_blocks."""
+    _here(x, q_out, scale_out, qt_out, scale_t_out)
+    R, C = x.shape
+    dt = _dt(x)
+    rb, cb = -(-R // SCALE_BLOCK), -(-C // SCALE_BLOCK)
+    qp = sp = qtp = stp = None
+    if want_rows or q_out is not None or scale_out is not None:
+        shape, sshape = (R, C), (cb, rb if tile else R)
+        if q_out is None:
+            q_out = x.new_empty(shape, dtype=torch.float8_e4m3fn)
+        else:
+            _like(q_out, shape, torch.float8_e4m3fn, "q_out")
+        if scale_out is None:
+            scale_out = x.new_empty(sshape, dtype=torch.float32)
+        else:
+            _like(scale_out, sshape, torch.float32, "scale_out")
+        qp, sp = q_out.data_ptr(), scale_out.data_ptr()
+    if want_cols or qt_out is not None or scale_t_out is not None:
+        shape, sshape = (C, -(-R // 16) * 16), (rb, cb if tile else C)
+        if qt_out is None:
+            qt_out = x.new_empty(shape, dtype=torch.float8_e4m3fn)
+        else:
+            _like(qt_out, shape, torch.float8_e4m3fn, "qt_out")
+        if scale_t_out is None:
+            scale_t_out = x.new_empty(sshape, dtype=torch.float32)
+        else:
+            _like(scale_t_out, sshape, torch.float32, "scale_t_out")
+        qtp, stp = qt_out.data_ptr(), scale_t_out.data_ptr()
+    if R:  # empty tensors have no address
+        _check((_LIB or load()).mem_quantize_blocks(x.data_ptr(), dt, R, C, bool(tile), qp, sp, qtp, stp,
+                                                    _stream(stream)))
+    return q_out, scale_out, qt_out, scale_t_out
+
+
+@_launches_on_stream
+def mem_linear_blocks(x: torch.Tensor, w: torch.Tensor, x_scale: torch.Tensor, w_scale: torch.Tensor,
+                      bias=None, *, residual=None, act="none", out_dtype=None, y_out=None, z_out=None,
+                      want_z: bool = False, stream=None):
+    """act(x w^T + bias) + residual for float8_e4m3fn operands x [T, K] and w [N, K] with a scale
+    for each 128 along K: x_scale [ceil(K/128), T], w_scale [ceil(K/128), N] or, for
+    128 x 128 tiles, [ceil(K/128), ceil(N/128)] (mem_quantize_blocks).
+
+    out_dtype: float32 or bfloat16 (the default), the dtype of bias and residual too; in
+    float32 products are exact.  y_out may be residual.  Returns (y, z) with z = x w^T + bias
+    before the activation, None unless want_z."""
+    _here(x, w, x_scale, w_scale, bias, residual, y_out, z_out)
+    T, K = x.shape
+    N = w.shape[0]
+    if x.dtype is not torch.float8_e4m3fn:
+        raise TypeError(f"unsupported dtype {x.dtype} (float8_e4m3fn)")
+    _like(w, (N, K), torch.float8_e4m3fn, "w")
+    kb, nb = -(-K // SCALE_BLOCK), -(-N // SCALE_BLOCK)
+    _like(x_scale, (kb, T), torch.float32, "x_scale")
+    tiled = tuple(w_scale.shape) == (kb, nb)
+    _like(w_scale, (kb, nb if tiled else N), torch.float32, "w_scale")
+    if out_dtype is None:
+        out_dtype = torch.bfloat16
+    shape = (T, N)
+    zp = bp = rp = None
+    if y_out is None:
+        y_out = x.new_empty(shape, dtype=out_dtype)
+    else:
+        _like(y_out, shape, out_dtype, "y_out")
+    if z_out is None and want_z:
+        z_out = x.new_empty(shape, dtype=out_dtype)
+    if z_out is not None:
+        _like(z_out, shape, out_dtype, "z_out")
+        zp = z_out.data_ptr()
+    if bias is not None:
+        _like(bias, (N,), out_dtype, "bias")
+        bp = bias.data_ptr()
+    if residual is not None:
+        _like(residual, shape, out_dtype, "residual")
+        rp = residual.data_ptr()
+    _check((_LIB or load()).mem_linear_blocks(x.data_ptr(), w.data_ptr(), x_scale.data_ptr(), w_scale.data_ptr(),
+                                              tiled, bp, rp, T, N, K, _act(act), zp, y_out.data_ptr(),
+                                              _dt(y_out), _stream(stream)))
+    return y_out, z_out
 
 
 class _AdamwTensor(ctypes.Structure):  # pkmem_adamw_tensor

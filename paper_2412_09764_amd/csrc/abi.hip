@@ -1157,4 +1157,51 @@ int mem_glu_backward(const void* dy, const void* z, pkmem_dtype dt, int act, int
                                             reinterpret_cast<hipStream_t>(stream)), fn);
 }
 
+int mem_quantize_blocks(const void* x, pkmem_dtype dt, int64_t R, int C, int tile, void* q_out, float* scale_out,
+                        void* qt_out, float* scale_t_out, pkmem_stream_t stream) {
+  const char* fn = "mem_quantize_blocks";
+  if (!dtype_ok(dt)) return fail(PKMEM_ERR_INVALID, "%s: unknown dtype %d", fn, (int)dt);
+  if (R < 0) return fail(PKMEM_ERR_INVALID, "%s: R must be >= 0", fn);
+  if (R > 0x7FFFFFFF) return fail(PKMEM_ERR_UNSUPPORTED, "%s: R must be < 2^31", fn);
+  if (C < 16 || C % 16 != 0 || C > (1 << 20))
+    return fail(PKMEM_ERR_UNSUPPORTED, "%s: C must be a positive multiple of 16, at most 2^20 (got %d)", fn, C);
+  if ((!q_out != !scale_out) || (!qt_out != !scale_t_out))
+    return fail(PKMEM_ERR_INVALID, "%s: codes and their scales come together", fn);
+  if (R > 0 && (!x || (!q_out && !qt_out))) return fail(PKMEM_ERR_INVALID, "%s: null pointer", fn);
+  if (!aligned(x, 16) || !aligned(q_out, 16) || !aligned(qt_out, 16) || !aligned(scale_out, 4) || !aligned(scale_t_out, 4))
+    return fail(PKMEM_ERR_INVALID, "%s: buffers must be 16-byte aligned (scales 4)", fn);
+  if (R == 0) return PKMEM_OK;
+  const size_t rb = ((size_t)R + 127) / 128, cb = ((size_t)C + 127) / 128;
+  const Bytes bx{x, (size_t)R * C * esize(dt)}, bq{q_out, (size_t)R * C}, bs{scale_out, cb * (tile ? rb : (size_t)R) * 4},
+      bqt{qt_out, (size_t)C * (((size_t)R + 15) / 16 * 16)}, bst{scale_t_out, rb * (tile ? cb : (size_t)C) * 4};
+  if (over(bq, {bx, bs, bqt, bst}) || over(bs, {bx, bqt, bst}) || over(bqt, {bx, bst}) || over(bst, {bx}))
+    return fail(PKMEM_ERR_INVALID, "%s: no two buffers may share bytes", fn);
+  const pk::QuantizeCall c{x, dt == PKMEM_BF16, tile != 0, R, C, q_out, scale_out, qt_out, scale_t_out};
+  return hip_status(pk::launch_quantize_blocks(c, reinterpret_cast<hipStream_t>(stream)), fn);
+}
+
+int mem_linear_blocks(const void* x, const void* w, const float* x_scale, const float* w_scale, int w_tile,
+                      const void* bias, const void* res, int64_t T, int N, int K, int act, void* z_out, void* y_out,
+                      pkmem_dtype y_dt, pkmem_stream_t stream) {
+  const char* fn = "mem_linear_blocks";
+  int rc = check_linear_shapes(fn, PKMEM_E4M3, true, T, N, K);
+  if (rc) return rc;
+  if (!tiles_fit(T, N)) return fail(PKMEM_ERR_UNSUPPORTED, "%s: 2^23 tiles of 256 x 256 or more", fn);
+  if (!dtype_ok(y_dt)) return fail(PKMEM_ERR_INVALID, "%s: y_dt must be PKMEM_F32 or PKMEM_BF16", fn);
+  if (act < PKMEM_ACT_NONE || act > PKMEM_ACT_GELU) return fail(PKMEM_ERR_INVALID, "%s: unknown activation %d", fn, act);
+  if (T > 0 && (!x || !w || !y_out || !x_scale || !w_scale)) return fail(PKMEM_ERR_INVALID, "%s: null pointer", fn);
+  if (!aligned(x, 16) || !aligned(w, 16) || !aligned(x_scale, 4) || !aligned(w_scale, w_tile ? 4 : 16) || !aligned(bias, 16) ||
+      !aligned(res, 16) || !aligned(z_out, 16) || !aligned(y_out, 16))
+    return fail(PKMEM_ERR_INVALID, "%s: buffers must be 16-byte aligned (x_scale, and w_scale of tiles, 4)", fn);
+  if (T == 0) return PKMEM_OK;
+  const size_t kb = ((size_t)K + 127) / 128, nb = w_tile ? ((size_t)N + 127) / 128 : (size_t)N, ye = esize(y_dt),
+               out = (size_t)T * N * ye;
+  const Bytes bx{x, (size_t)T * K}, bw{w, (size_t)N * K}, bsx{x_scale, kb * T * 4}, bsw{w_scale, kb * nb * 4},
+      bb{bias, N * ye}, br{res, out}, bz{z_out, out}, by{y_out, out};
+  if (over(by, {bx, bw, bsx, bsw, bb, bz}, {br}) || over(bz, {bx, bw, bsx, bsw, bb, br}))
+    return fail(PKMEM_ERR_INVALID, "%s: an output may share no bytes with an operand or the other output (y_out may be res itself)", fn);
+  const pk::LinearCall c{x, w, PKMEM_E4M3, x_scale, w_scale, bias, res, T, N, K, act, z_out, y_out, y_dt == PKMEM_BF16};
+  return hip_status(pk::launch_linear_blocks(c, w_tile != 0, reinterpret_cast<hipStream_t>(stream)), fn);
+}
+
 }  // extern "C"

@@ -94,6 +94,12 @@ __device__ __forceinline__ void lds_dma16_buf(__amdgpu_buffer_rsrc_t r, uint32_t
                                            (int)voff, (int)soff, 0, 0);
 }
 
+// One dword a lane, from any addresses, to 256 consecutive bytes of LDS.
+__device__ __forceinline__ void lds_dma4(const void* from, void* lds_base) {
+  __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)from,
+                                   (__attribute__((address_space(3))) void*)lds_base, 4, 0, 0);
+}
+
 // ---------------------------------------------------------------- bf16 ----
 // silu(x) = x * sigmoid(x) = x / (1 + exp(-x)) (Memory+ gate, Sec. 3.1.4);
 // for very negative x the denominator overflows to inf and the result is -0.

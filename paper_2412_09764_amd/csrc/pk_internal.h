@@ -188,6 +188,21 @@ hipError_t launch_glu(const LinearCall& c, hipStream_t st);
 hipError_t launch_glu_backward(bool bf16, const void* dy, const void* z, int act, int64_t T, int N, void* dz,
                                hipStream_t st);
 
+// ---- 8 bits in blocks (quantize.hip, blocks.hip) ------------------------------
+struct QuantizeCall {
+  const void* x;
+  bool bf16, tile;
+  int64_t R;
+  int C;
+  void* q;  // with scale, or null
+  float* scale;
+  void* qt;  // with scale_t, or null
+  float* scale_t;
+};
+hipError_t launch_quantize_blocks(const QuantizeCall& c, hipStream_t st);
+// x_scale, w_scale: of blocks of 128 k; tiled: of 128 rows of w too.
+hipError_t launch_linear_blocks(const LinearCall& c, bool tiled, hipStream_t st);
+
 // ---- optimizer (adamw.hip) -------------------------------------------------
 constexpr int ADAMW_STATE_BLOCK = 128;  // elements that share the scales of 8-bit states
 // Elements of one tensor of mem_adamw: as many as one launch takes, about 2^36.
