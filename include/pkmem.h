@@ -535,7 +535,8 @@ int mem_layernorm_backward(const void* dy, const void* h, const void* weight, pk
  *   act     pkmem_act, with mem_linear's precision.
  *   z_out   [T, 2 N] dtype y_dt: z (what mem_glu_backward needs); NULL to skip it.
  *   y_out   [T, N] dtype y_dt.
- * Types, exactness of products and limits as mem_linear's with 2 N in place of N;
+ * Types, exactness of products and limits as mem_linear's with 2 N in place of N (for
+ * PKMEM_E4M3 with y_dt PKMEM_BF16 products as in mem_linear_blocks);
  * N % 8 == 0 and N <= 2^19.  No output may share bytes with another buffer (refused).
  * All buffers 16-byte aligned.  T = 0 is a valid no-op.
  * ------------------------------------------------------------------------ */

@@ -4,7 +4,7 @@
 //
 // The projections' kernel; a stage brings the scales of its rows into LDS beside the codes.  The
 // sums of a stage (64 k) start from 0 and are added, times their scales, in fp32.
-#include "pk_gemm.h"
+#include "pk_gemm8.h"
 
 namespace pk {
 
@@ -19,9 +19,16 @@ void blocks_tile(GemmArgs g, hipStream_t st) {
 }
 template <int MODE>
 void blocks_launch(const GemmArgs& g, hipStream_t st) {
+  constexpr bool EIGHT = MODE >= G_BLOCKS8;
   switch (pick_tile(false, g.M, g.N)) {
-    case TILE_256: blocks_tile<MODE, 256, 256, 2, 4, 1>(g, st); break;
-    case TILE_128: blocks_tile<MODE, 128, 128, 2, 2, 1>(g, st); break;
+    case TILE_256:
+      if constexpr (EIGHT) gemm8_launch<256, 256, 2, 4, MODE>(g, st);
+      else blocks_tile<MODE, 256, 256, 2, 4, 1>(g, st);
+      break;
+    case TILE_128:
+      if constexpr (EIGHT) gemm8_launch<128, 128, 2, 2, MODE>(g, st);
+      else blocks_tile<MODE, 128, 128, 2, 2, 1>(g, st);
+      break;
     case TILE_128_K2: blocks_tile<MODE, 128, 128, 2, 2, 2>(g, st); break;
     case TILE_64: blocks_tile<MODE, 64, 64, 1, 1, 4>(g, st); break;
     default: blocks_tile<MODE, 32, 32, 1, 1, 8>(g, st);

@@ -7,7 +7,7 @@
 // The product's tiles hold 32 columns of the gate and the same 32 of the up projection in
 // turn, so that one wave has both numbers of a result in its registers: z is written only
 // for a backward that asks for it.
-#include "pk_gemm.h"
+#include "pk_gemm8.h"
 
 namespace pk {
 
@@ -26,7 +26,12 @@ void glu_launch(const GemmArgs& g, hipStream_t st) {
     hipLaunchKernelGGL((k_gemm_few<DT, G_GLU>), dim3((unsigned)ceil_div(g.N, 16)), dim3(FEW_WAVES * 64), 0, st, g);
     return;
   }
-  switch (pick_tile(DT == D_F32, g.M, 2 * (int64_t)g.N)) {
+  const int tile = pick_tile(DT == D_F32, g.M, 2 * (int64_t)g.N);
+  if constexpr (DT == D_E4M3) {
+    if (g.out_bf16 && tile == TILE_256) return gemm8_launch<256, 256, 2, 4, G_GLU>(g, st);
+    if (g.out_bf16 && tile == TILE_128) return gemm8_launch<128, 128, 2, 2, G_GLU>(g, st);
+  }
+  switch (tile) {
     case TILE_256: glu_tile<DT, 256, 256, 2, 4, 1>(g, st); break;
     case TILE_128: glu_tile<DT, 128, 128, 2, 2, 1>(g, st); break;
     case TILE_128_K2: glu_tile<DT, 128, 128, 2, 2, 2>(g, st); break;

@@ -648,7 +648,9 @@ __global__ __launch_bounds__(WM* WN* KG * 64) void k_gemm(const GemmArgs g) {
           mma_bf16(b[nj][q], q & 1 ? widen8(f.z, f.w) : widen8(f.x, f.y), p[t & 1]);
         }
       }
+      __builtin_amdgcn_sched_barrier(0);  // or one set of registers would do, and wait
       if (t > 0) add(p[(t - 1) & 1], t - 1);
+      __builtin_amdgcn_sched_barrier(0);
     }
     add(p[(MI * NJ - 1) & 1], MI * NJ - 1);
   };
