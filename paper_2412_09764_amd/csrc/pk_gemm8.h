@@ -36,12 +36,12 @@ struct Codes {
   __device__ static __forceinline__ int source_chunk(int wave, int lane) {
     return (lane & 7) ^ ((wave * 4 + (lane >> 4)) & 7);
   }
-  __device__ __forceinline__ void init(const void* p, int64_t row0, int64_t rows, int64_t K, int wave, int lane) {
-    left = (int)K;
+  __device__ __forceinline__ void init(const void* p, int64_t row0, int64_t rows, int64_t K, bool in, int wave, int lane) {
+    left = in ? (int)K : 0;
     base = (const char*)p + row0 * K;
     up = rows * K;
     row = (uint32_t)K;
-    bytes = (int)((rows - row0 < R ? rows - row0 : R) * K);
+    bytes = in ? (int)((rows - row0 < R ? rows - row0 : R) * K) : 0;
     off = (uint32_t)((GLU ? (wave & 3) : wave) * 8 + (lane >> 3)) * row + source_chunk(wave, lane) * 16;
     if (GLU && (wave & 4)) base += up;
   }
@@ -60,11 +60,10 @@ struct Codes {
     bytes -= STEP_K;
     left -= STEP_K;
   }
-  // This lane's 32 codes of row r: chunks q and q + 4, q = lane / 16.
-  __device__ static __forceinline__ void read(const unsigned char* lds, int r, int lane, uint4 (&f)[2]) {
-    const int c = (lane >> 4) ^ ((r >> 1) & 7);
-    f[0] = ld16(lds + r * STEP_K + c * 16);
-    f[1] = ld16(lds + r * STEP_K + (c ^ 4) * 16);
+  // Where this lane's codes of row r (its number in a block of 16 rows: lane % 16) lie: chunks
+  // q and q + 4, q = lane / 16, the second one 64 bytes up or down.
+  __device__ static __forceinline__ uint32_t place(int r, int lane) {
+    return r * STEP_K + (((lane >> 4) ^ ((r >> 1) & 7)) << 4);
   }
 };
 
@@ -72,9 +71,11 @@ struct Codes {
 // meet when its codes have landed and the step before has been read, the loads of the next one
 // are issued, and each wave walks down its blocks of 16 rows, the fragments of a block read
 // while the one before is multiplied.  The last block's operands stay in registers over the
-// meeting, so that the matrix cores have work while the first reads return.  MODE: G_GLU (sums
-// in place), G_BLOCKS8 and G_BLOCKS8_TILED (a step's sums are added with their scales two
-// products later).
+// meeting, so that the matrix cores have work while the first reads return.  A workgroup
+// takes tile after tile: in the last step of one the loads of the next one's first step are
+// issued, and its results leave (through LDS that step has used) while they arrive.  MODE: G_GLU
+// (sums in place), G_BLOCKS8 and G_BLOCKS8_TILED (a step's sums are added with their scales
+// two products later).
 template <int BM, int BN, int WM, int WN, int MODE>
 __global__ __launch_bounds__(WM* WN * 64) void k_gemm8(const GemmArgs g) {
   constexpr int NW = WM * WN, MI = BM / WM / 16, NJ = BN / WN / 16;
@@ -83,38 +84,56 @@ __global__ __launch_bounds__(WM* WN * 64) void k_gemm8(const GemmArgs g) {
   using CA = Codes<BM, NW, false>;
   using CB = Codes<BN, NW, GLU>;
   constexpr int SCALE_LOADS = GLU ? 0 : (BM + BN) / 64 / NW, SCALES_AT = CA::BYTES + CB::BYTES;
-  constexpr int L = CA::LOADS + CB::LOADS + SCALE_LOADS, BYTES = SCALES_AT + (GLU ? 0 : (BM + BN) * 4);
+  constexpr int BYTES = SCALES_AT + (GLU ? 0 : (BM + BN) * 4);
   __shared__ __align__(1024) unsigned char st0[BYTES], st1[BYTES];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int wi = (wave / WN) * (BM / WM), wj = (wave % WN) * 64;
 
-  // tiles in the order of k_gemm's
-  const int nwg = gridDim.x, x = blockIdx.x & 7, q = nwg >> 3, rem = nwg & 7;
-  int pid = x * q + (x < rem ? x : rem) + (blockIdx.x >> 3);
-  const int group = pid / (4 * g.tiles_n), m_first = group * 4;
-  const int m_count = g.tiles_m - m_first < 4 ? g.tiles_m - m_first : 4;
-  pid -= group * 4 * g.tiles_n;
-  const int64_t i0 = (int64_t)(m_first + pid % m_count) * BM;
-  const int j0 = pid / m_count * (GLU ? BN / 2 : BN);
+  // Tiles in the order of k_gemm's: XCD x has a contiguous run of them, of which its
+  // workgroups take one after another.
+  const int tiles = g.tiles_m * g.tiles_n, x = blockIdx.x & 7, rem = tiles & 7;
+  const int mine = (int)((gridDim.x - x + 7) >> 3);  // workgroups of this XCD
+  const int run_end = (x + 1) * (tiles >> 3) + (x + 1 < rem ? x + 1 : rem);
+  int tile = x * (tiles >> 3) + (x < rem ? x : rem) + (int)(blockIdx.x >> 3);
 
   CA ca;
   CB cb;
-  ca.init(g.a, i0, g.M, g.K, wave, lane);
-  cb.init(g.b, j0, g.N, g.K, wave, lane);
-  const int wi = (wave / WN) * (BM / WM), wj = (wave % WN) * 64;
   const float* scale_at[SCALE_LOADS ? SCALE_LOADS : 1];
   int scale_step[SCALE_LOADS ? SCALE_LOADS : 1];
+  int64_t i0 = 0;
+  int j0 = 0;
+  // What follows depends on the lane alone and would be kept over the steps, which need every
+  // register: it is computed again for each tile.
+  auto again = [&]() PK_INLINE {
+    int l = lane;
+    asm volatile("" : "+v"(l));
+    return l;
+  };
+  // The operands of tile t; past the run's end: none.
+  auto set_tile = [&](int t, int64_t& ti, int& tj) PK_INLINE {
+    const int lane = again();
+    const bool in = t < run_end;
+    if (!in) t = 0;
+    const int group = t / (4 * g.tiles_n), m_first = group * 4;
+    const int m_count = g.tiles_m - m_first < 4 ? g.tiles_m - m_first : 4;
+    t -= group * 4 * g.tiles_n;
+    ti = (int64_t)(m_first + t % m_count) * BM;
+    tj = t / m_count * (GLU ? BN / 2 : BN);
+    ca.init(g.a, ti, g.M, g.K, in, wave, lane);
+    cb.init(g.b, tj, g.N, g.K, in, wave, lane);
 #pragma unroll
-  for (int i = 0; i < SCALE_LOADS; ++i) {  // rows past the end take the last one's: their codes are 0
-    const int r = (i * NW + wave) * 64 + lane;
-    if (r < BM) {
-      scale_at[i] = g.a_block + (i0 + r < g.M ? i0 + r : g.M - 1);
-      scale_step[i] = (int)g.M;
-    } else {
-      const int j = j0 + r - BM < g.N ? j0 + r - BM : g.N - 1;
-      scale_at[i] = g.b_block + (TILED ? j / SCALE_K : j);
-      scale_step[i] = TILED ? (g.N + SCALE_K - 1) / SCALE_K : g.N;
+    for (int i = 0; i < SCALE_LOADS; ++i) {  // rows past the end take the last one's: their codes are 0
+      const int r = (i * NW + wave) * 64 + lane;
+      if (r < BM) {
+        scale_at[i] = g.a_block + (ti + r < g.M ? ti + r : g.M - 1);
+        scale_step[i] = (int)g.M;
+      } else {
+        const int j = tj + r - BM < g.N ? tj + r - BM : g.N - 1;
+        scale_at[i] = g.b_block + (TILED ? j / SCALE_K : j);
+        scale_step[i] = TILED ? (g.N + SCALE_K - 1) / SCALE_K : g.N;
+      }
     }
-  }
+  };
   auto fill = [&](unsigned char* st) PK_INLINE {
 #pragma unroll
     for (int i = 0; i < SCALE_LOADS; ++i) {
@@ -129,33 +148,42 @@ __global__ __launch_bounds__(WM* WN * 64) void k_gemm8(const GemmArgs g) {
   uint4 fa[2][2], fb[NJ][2];
   float sa[4] = {0.f, 0.f, 0.f, 0.f}, sb[NJ][TILED ? 1 : 4];
   const uint4 none{0, 0, 0, 0};
+  // Before a tile's first step: no sums, and a last block of zeros.
+  auto clear = [&]() PK_INLINE {
 #pragma unroll
-  for (int mi = 0; mi < MI; ++mi)
+    for (int mi = 0; mi < MI; ++mi)
 #pragma unroll
-    for (int nj = 0; nj < NJ; ++nj) acc[mi][nj] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-  // before the first step: a last block of zeros
+      for (int nj = 0; nj < NJ; ++nj) acc[mi][nj] = f32x4_t{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-  for (int nj = 0; nj < NJ; ++nj) {
-    fb[nj][0] = fb[nj][1] = none;
+    for (int nj = 0; nj < NJ; ++nj) {
+      fb[nj][0] = fb[nj][1] = none;
 #pragma unroll
-    for (int e = 0; e < (TILED ? 1 : 4); ++e) sb[nj][e] = 0.f;
-  }
-  fa[(MI - 1) & 1][0] = fa[(MI - 1) & 1][1] = none;
+      for (int e = 0; e < (TILED ? 1 : 4); ++e) sb[nj][e] = 0.f;
+    }
+    fa[(MI - 1) & 1][0] = fa[(MI - 1) & 1][1] = none;
+    sa[(MI - 1) & 3] = 0.f;
+  };
 
+  // 16 rows are 2048 bytes and swizzled alike: one place serves all blocks of rows
+  const uint32_t at_a = CA::place(wi + (lane & 15), lane), at_b = CB::place(wj + (lane & 15), lane);
+  const uint32_t at_sa = SCALES_AT + (wi + (lane & 15)) * 4, at_sb = SCALES_AT + (BM + wj + (TILED ? 0 : 4 * (lane >> 4))) * 4;
   auto read_a = [&](const unsigned char* st, int mi) PK_INLINE {
-    const int r = wi + mi * 16 + (lane & 15);
-    CA::read(st, r, lane, fa[mi & 1]);
-    if constexpr (!GLU) sa[mi & 3] = reinterpret_cast<const float*>(st + SCALES_AT)[r];
+    fa[mi & 1][0] = ld16(st + at_a + mi * 16 * STEP_K);
+    fa[mi & 1][1] = ld16(st + (at_a ^ 64) + mi * 16 * STEP_K);
+    if constexpr (!GLU) sa[mi & 3] = *reinterpret_cast<const float*>(st + at_sa + mi * 64);
+  };
+  auto read_b = [&](const unsigned char* st, int nj) PK_INLINE {
+    fb[nj][0] = ld16(st + CA::BYTES + at_b + nj * 16 * STEP_K);
+    fb[nj][1] = ld16(st + CA::BYTES + (at_b ^ 64) + nj * 16 * STEP_K);
   };
   auto read_sb = [&](const unsigned char* st) PK_INLINE {
     if constexpr (!GLU) {
-      const float* sc = reinterpret_cast<const float*>(st + SCALES_AT) + BM + wj;
 #pragma unroll
       for (int nj = 0; nj < NJ; ++nj) {
         if constexpr (TILED) {
-          if (nj == 0) sb[0][0] = sc[0];  // 64 columns of one tile
+          if (nj == 0) sb[0][0] = *reinterpret_cast<const float*>(st + at_sb);  // 64 columns of one tile
         } else {
-          const float4 f = *reinterpret_cast<const float4*>(sc + nj * 16 + 4 * (lane >> 4));
+          const float4 f = *reinterpret_cast<const float4*>(st + at_sb + nj * 64);
           sb[nj][0] = f.x; sb[nj][1] = f.y; sb[nj][2] = f.z; sb[nj][3] = f.w;
         }
       }
@@ -182,14 +210,13 @@ __global__ __launch_bounds__(WM* WN * 64) void k_gemm8(const GemmArgs g) {
     }
   };
   auto step = [&](const unsigned char* st, unsigned char* next) PK_INLINE {
-    wait_and_meet<0>();
     read_a(st, 0);
     __builtin_amdgcn_sched_barrier(0);
     constexpr int LAST = MI - 1;
 #pragma unroll
     for (int nj = 0; nj < NJ; ++nj) {
       multiply(LAST, nj);
-      CB::read(st + CA::BYTES, wj + nj * 16 + (lane & 15), lane, fb[nj]);
+      read_b(st, nj);
       __builtin_amdgcn_sched_barrier(0);
       if (nj >= 2) add(LAST, nj - 2);
     }
@@ -213,76 +240,137 @@ __global__ __launch_bounds__(WM* WN * 64) void k_gemm8(const GemmArgs g) {
     add(LAST - 1, NJ - 2);
     add(LAST - 1, NJ - 1);
   };
-  const int steps = (int)((g.K + STEP_K - 1) / STEP_K);
-  fill(st0);
-  int s = 0;
-  for (; s + 2 <= steps; s += 2) {
-    step(st0, st1);
-    step(st1, st0);
-  }
-  if (s < steps) step(st0, st1);
-  wait_loads<0>();  // no load may reach LDS after the workgroup has left it
+  // The sums leave through LDS, 32 rows of a wave's 64 columns at a time, so that every store
+  // covers whole cache lines; chunk c of row r lies at slot c ^ (r mod 16).
+  constexpr int PIECE = 32 * 256;
+  static_assert(BYTES >= NW * PIECE, "a piece for each wave");
+  constexpr int ROW_LANES = GLU ? 4 : 8, STEP = 64 / ROW_LANES, ROWS = 32 / STEP;
+  constexpr int STORES = MI * 16 / STEP;  // of a wave whose tile is whole, at least
+  auto leave_as = [&](auto act) PK_INLINE {
+    constexpr int ACT = decltype(act)::value;
+    const int lane = again(), rr = lane / ROW_LANES, cc = lane % ROW_LANES;
+    unsigned char* buf = st1 + wave * PIECE;
+    const int j = j0 + (GLU ? wj / 2 : wj) + 8 * cc;
+    const bool in = j < g.N;
+    constexpr int U = GLU ? 2 : 1;
+    float scale[U][8], bias[U][8];  // of this lane's columns
 #pragma unroll
-  for (int nj = 0; nj < NJ; ++nj) multiply(MI - 1, nj), add(MI - 1, nj);
-
-  // The sums leave through LDS, 64 rows of a wave's 64 columns at a time, as k_gemm's.
-  __syncthreads();
-  constexpr int PIECE = 64 * 256, PER = BYTES / PIECE;
-  static_assert(PER * 2 >= NW, "a piece for each wave");
-  unsigned char* buf = (wave < PER ? st0 : st1) + wave % PER * PIECE;
-  constexpr int ROW_LANES = GLU ? 4 : 8, STEP = 64 / ROW_LANES, ROWS = 64 / STEP;
-  const int rr = lane / ROW_LANES, cc = lane % ROW_LANES;
-  const int j = j0 + (GLU ? wj / 2 : wj) + 8 * cc;
-  typename std::conditional<GLU, GluEpilogue, Epilogue>::type epi;
-  epi.init(g, j);
+    for (int u = 0; u < U; ++u) {
 #pragma unroll
-  for (int mp = 0; mp < MI; mp += 4) {
-    const int64_t ip = i0 + wi + mp * 16 + rr;
-    Raw8 res[ROWS];
-    if constexpr (!GLU) {
-      if (g.res && j < g.N) {
-#pragma unroll
-        for (int t = 0; t < ROWS; ++t)
-          if (ip + STEP * t < g.M) res[t].load(g.res, (size_t)(ip + STEP * t) * g.N + j, true);
+      for (int e = 0; e < 8; ++e) scale[u][e] = 1.f, bias[u][e] = 0.f;
+      if (GLU && in) {
+        Raw8 r;
+        r.load(g.b_scale, (size_t)u * g.N + j, false);
+        r.unpack(false, scale[u]);
+      }
+      if (g.bias && in) {
+        Raw8 r;
+        r.load(g.bias, (size_t)u * g.N + j, true);
+        r.unpack(true, bias[u]);
       }
     }
+    const int row_z = U * g.N;
+    uint16_t *z = (uint16_t*)g.z, *out = (uint16_t*)g.out;
 #pragma unroll
-    for (int m = 0; m < 4; ++m)
+    for (int mp = 0; mp < MI; mp += 2) {
+      const int64_t ip = i0 + wi + mp * 16 + rr;
+      uint4 res[ROWS];
+      float sx[ROWS];
 #pragma unroll
-      for (int nj = 0; nj < NJ; ++nj) {
-        const f32x4_t& c = acc[mp + m][nj];
-        const int row = m * 16 + (lane & 15), ch = nj * 4 + (lane >> 4);
-        *reinterpret_cast<float4*>(buf + row * 256 + ((ch ^ (row & 15)) << 4)) = float4{c[0], c[1], c[2], c[3]};
+      for (int t = 0; t < ROWS; ++t) {
+        const int64_t i = ip + STEP * t;
+        res[t] = none;
+        sx[t] = 1.f;
+        if (GLU && i < g.M) sx[t] = g.a_scale[i];
+        if (!GLU && g.res && in && i < g.M) res[t] = ld16((const uint16_t*)g.res + (size_t)i * g.N + j);
       }
-    if (j < g.N) {
+#pragma unroll
+      for (int m = 0; m < 2; ++m)
+#pragma unroll
+        for (int nj = 0; nj < NJ; ++nj) {
+          const f32x4_t& c = acc[mp + m][nj];
+          const int row = m * 16 + (lane & 15), ch = nj * 4 + (lane >> 4);
+          *reinterpret_cast<float4*>(buf + row * 256 + ((ch ^ (row & 15)) << 4)) = float4{c[0], c[1], c[2], c[3]};
+        }
 #pragma unroll
       for (int t = 0; t < ROWS; ++t) {
         const int row = rr + STEP * t;
         const int64_t i = ip + STEP * t;
-        if (i >= g.M) continue;
-        auto gather = [&](int c, float (&v)[8]) PK_INLINE {
-          Chunk<float>::unpack(ld16(buf + row * 256 + ((c ^ (row & 15)) << 4)), v);
-          Chunk<float>::unpack(ld16(buf + row * 256 + (((c + 1) ^ (row & 15)) << 4)), v + 4);
-        };
-        float v[8];
-        gather(2 * cc, v);
-        if constexpr (GLU) {
-          float u[8];
-          gather(8 + 2 * cc, u);
-          epi.store(g, i, j, g.a_scale ? g.a_scale[i] : 1.f, v, u);
-        } else {
-          epi.store(g, (size_t)i * g.N + j, 1.f, res[t], v);
+        if (!in || i >= g.M) continue;
+        float v[U][8];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+          const int c = 8 * u + 2 * cc;
+          Chunk<float>::unpack(ld16(buf + row * 256 + ((c ^ (row & 15)) << 4)), v[u]);
+          Chunk<float>::unpack(ld16(buf + row * 256 + (((c + 1) ^ (row & 15)) << 4)), v[u] + 4);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) v[u][e] = GLU ? fmaf(v[u][e], sx[t] * scale[u][e], bias[u][e]) : v[u][e] + bias[u][e];
+          if (z) store8(z, (size_t)i * row_z + u * g.N + j, true, v[u]);
         }
+        float r[8];
+        Chunk<uint16_t>::unpack(res[t], r);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          v[0][e] = act_of<true, ACT>(v[0][e]);
+          v[0][e] = GLU ? v[0][e] * v[U - 1][e] : v[0][e] + r[e];
+        }
+        store8(out, (size_t)i * g.N + j, true, v[0]);
       }
     }
+  };
+  auto leave = [&]() PK_INLINE {
+    if (g.act == PKMEM_ACT_NONE) leave_as(std::integral_constant<int, PKMEM_ACT_NONE>());
+    else if (g.act == PKMEM_ACT_SILU) leave_as(std::integral_constant<int, PKMEM_ACT_SILU>());
+    else if (g.act == PKMEM_ACT_GELU) leave_as(std::integral_constant<int, PKMEM_ACT_GELU>());
+    else leave_as(std::integral_constant<int, PKMEM_ACT_RELU>());
+  };
+
+  // Steps in pairs, so that every tile starts in st0 (an odd last one gets an empty one).
+  const int pairs = (int)((g.K + 2 * STEP_K - 1) / (2 * STEP_K));
+  set_tile(tile, i0, j0);
+  fill(st0);
+  bool drain = true;  // the loads are the newest operations
+  while (true) {
+    clear();
+    // the first step's loads are older than the stores of the tile before, which need not be waited for
+    if (drain) wait_and_meet<0>();
+    else wait_and_meet<STORES>();
+    step(st0, st1);
+    for (int s = 1; s < pairs; ++s) {
+      wait_and_meet<0>();
+      step(st1, st0);
+      wait_and_meet<0>();
+      step(st0, st1);
+    }
+    int64_t next_i;
+    int next_j;
+    set_tile(tile + mine, next_i, next_j);
+    wait_and_meet<0>();
+    step(st1, st0);
+#pragma unroll
+    for (int nj = 0; nj < NJ; ++nj) multiply(MI - 1, nj), add(MI - 1, nj);
+    // the additions stay here: the compiler would move them to where the sums are used, and spill
+#pragma unroll
+    for (int mi = 0; mi < MI; ++mi)
+#pragma unroll
+      for (int nj = 0; nj < NJ; ++nj) asm volatile("" : "+v"(acc[mi][nj]));
+    wait_and_meet<63>();  // st1 has been read
+    leave();
+    drain = i0 + BM > g.M || j0 + (GLU ? BN / 2 : BN) > g.N;
+    tile += mine;
+    if (tile >= run_end) break;
+    i0 = next_i;
+    j0 = next_j;
   }
+  wait_loads<0>();  // no load may reach LDS after the workgroup has left it
 }
 
 template <int BM, int BN, int WM, int WN, int MODE>
 void gemm8_launch(GemmArgs g, hipStream_t st) {
   g.tiles_m = ceil_div(g.M, BM);
   g.tiles_n = ceil_div(g.N, MODE == G_GLU ? BN / 2 : BN);
-  hipLaunchKernelGGL((k_gemm8<BM, BN, WM, WN, MODE>), dim3((unsigned)(g.tiles_m * g.tiles_n)), dim3(WM * WN * 64), 0,
+  const int tiles = g.tiles_m * g.tiles_n, most = BM == 256 ? 256 : 512;  // of the chip's 256 CUs, by LDS
+  hipLaunchKernelGGL((k_gemm8<BM, BN, WM, WN, MODE>), dim3((unsigned)(tiles < most ? tiles : most)), dim3(WM * WN * 64), 0,
                      st, g);
 }
 
