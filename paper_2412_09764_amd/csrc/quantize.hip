@@ -16,11 +16,32 @@ namespace {
 
 constexpr int SIDE = 128;
 
-// Codes of the elements of one block.  They are divided as v / d, v = x f and d = max|x| f / 448
-// with f a power of two that brings max|x| to [2, 4): no product below loses digits there.
-// d = div + rest to 46 bits.
+// Codes of the elements of one block, from the size of its largest.
 template <typename T>
-struct Coder {
+struct Coder;
+
+// bf16: quotients of numbers of 8 bits come no nearer to a border between two codes than 2^-14
+// of themselves, or lie on it.  x times an inverse that is within 2^-22 is therefore right
+// once it is rounded to 17 bits, which puts those on a border back onto it.
+template <>
+struct Coder<uint16_t> {
+  float inv, scale;
+  __device__ __forceinline__ explicit Coder(float top) {
+    constexpr float R = 1.f / E4M3_MAX;
+    const float s = top * R;  // top / 448, to nearest after the correction
+    scale = fmaxf(fmaf(fmaf(-s, E4M3_MAX, top), R, s), 0x1p-126f);
+    if (!(top < __builtin_inff())) scale = top;
+    inv = __builtin_amdgcn_rcpf(scale);
+  }
+  __device__ __forceinline__ float operator()(float x) const {
+    return __uint_as_float((__float_as_uint(x * inv) + 0x40u) & ~0x7Fu);
+  }
+};
+
+// fp32: the elements are divided as v / d, v = x f and d = max|x| f / 448 with f a power of two
+// that brings max|x| to [2, 4): no product below loses digits there.  d = div + rest to 46 bits.
+template <>
+struct Coder<float> {
   float f, div, rest, inv, scale;
   __device__ __forceinline__ explicit Coder(float top) {
     scale = top / E4M3_MAX;
@@ -37,16 +58,13 @@ struct Coder {
     const float v = x * f;
     float q = v * inv;
     q = fmaf(fmaf(-q, rest, fmaf(-q, div, v)), inv, q);
-    if constexpr (sizeof(T) == 4) {
-      // The quotient is rounded to 24 bits here and to a code later.  Where the 24 bits
-      // lie on a border between two codes (their last 12 are 0 then) and the remainder, of
-      // 2^-34 of v at least or 0 there, is not 0, one unit puts it on its own side.
-      // Quotients of bf16 numbers come no nearer to a border than 2^-14.
-      const float r = fmaf(-q, rest, fmaf(-q, div, v));
-      const uint32_t b = __float_as_uint(q);
-      if ((b & 0xFFFu) == 0 && fabsf(r) > fabsf(v) * 0x1p-40f)
-        q = __uint_as_float((r > 0.f) == (q > 0.f) ? b + 1 : b - 1);
-    }
+    // The quotient is rounded to 24 bits here and to a code later.  Where the 24 bits lie on a
+    // border between two codes (their last 12 are 0 then) and the remainder, of 2^-34 of v at
+    // least or 0 there, is not 0, one unit puts it on its own side.
+    const float r = fmaf(-q, rest, fmaf(-q, div, v));
+    const uint32_t b = __float_as_uint(q);
+    if ((b & 0xFFFu) == 0 && fabsf(r) > fabsf(v) * 0x1p-40f)
+      q = __uint_as_float((r > 0.f) == (q > 0.f) ? b + 1 : b - 1);
     return q;
   }
 };
@@ -66,11 +84,22 @@ __device__ __forceinline__ float largest(const float (&v)[8]) {
   for (int e = 0; e < 8; ++e) m = fmaxf(m, fabsf(v[e]));
   return m;
 }
-template <int FROM, int TO>
-__device__ __forceinline__ float lanes_max(float m) {
-#pragma unroll
-  for (int s = FROM; s <= TO; s *= 2) m = fmaxf(m, __shfl_xor(m, s, WAVE));
+// The largest over groups of 16 lanes, in all of them.
+__device__ __forceinline__ float max16(float m) {
+#define PK_ROR(N) m = fmaxf(m, __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(m), 0x120 + N, 15, 15, true)))
+  PK_ROR(8);
+  PK_ROR(4);
+  PK_ROR(2);
+  PK_ROR(1);
+#undef PK_ROR
   return m;
+}
+// The largest over the wave's four lanes of equal number mod 16.
+__device__ __forceinline__ float max_across(float m) {
+  auto a = __builtin_amdgcn_permlane32_swap(__float_as_uint(m), __float_as_uint(m), false, false);
+  m = fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
+  a = __builtin_amdgcn_permlane16_swap(__float_as_uint(m), __float_as_uint(m), false, false);
+  return fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
 }
 template <typename T>
 __device__ __forceinline__ uint2 codes8(const Coder<T>& c, const float (&v)[8]) {
@@ -100,7 +129,7 @@ __global__ __launch_bounds__(256) void k_quantize_rows128(const T* __restrict__ 
 #pragma unroll
     for (int i = 0; i < BLOCKS_AT_ONCE; ++i) {
       const int c = (b0 + i) * SIDE + lane * 8;
-      const Coder<T> code(lanes_max<1, 8>(largest(v[i])));
+      const Coder<T> code(max16(largest(v[i])));
       if (c < C) *reinterpret_cast<uint2*>(q + (size_t)row * C + c) = codes8(code, v[i]);
       if (lane == 0 && b0 + i < blocks) scale[(size_t)(b0 + i) * R + row] = code.scale;
     }
@@ -136,7 +165,7 @@ __global__ __launch_bounds__(256) void k_quantize_square(const T* __restrict__ x
     if constexpr (TILE) {
 #pragma unroll
       for (int i = 0; i < 8; ++i) top = fmaxf(top, largest(v[i]));
-      top = lanes_max<1, 32>(top);
+      top = max_across(max16(top));
       if ((threadIdx.x & 63) == 0) tops[wave][0] = top;
       __syncthreads();
       top = fmaxf(fmaxf(tops[0][0], tops[1][0]), fmaxf(tops[2][0], tops[3][0]));
@@ -170,7 +199,7 @@ __global__ __launch_bounds__(256) void k_quantize_square(const T* __restrict__ x
           float m = 0.f;
 #pragma unroll
           for (int i = 0; i < 8; ++i) m = fmaxf(m, fabsf(v[i][e]));
-          m = lanes_max<16, 32>(m);
+          m = max_across(m);
           if ((threadIdx.x & 48) == 0) tops[wave][cl * 8 + e] = m;
         }
         __syncthreads();
@@ -178,7 +207,7 @@ __global__ __launch_bounds__(256) void k_quantize_square(const T* __restrict__ x
       if (q) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-          const Coder<T> code(lanes_max<1, 8>(largest(v[i])));
+          const Coder<T> code(max16(largest(v[i])));
           if (r0 + i >= R) continue;
           if (c0 < C) *reinterpret_cast<uint2*>(q + (size_t)(r0 + i) * C + c0) = codes8(code, v[i]);
           if (cl == 0) scale[(size_t)bc * R + r0 + i] = code.scale;
