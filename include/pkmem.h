@@ -586,10 +586,15 @@ int mem_quantize_blocks(const void* x, pkmem_dtype dt, int64_t R, int C, int til
  * w's columns (qt_out as w, N and K changed round); grad_w from both columns, with
  * res = y_out = grad_w in PKMEM_F32 to accumulate.
  * w_scale 16-byte aligned without w_tile, x_scale (and w_scale with it) 4, others 16.
+ * Workspace: mem_linear_blocks_workspace_size(T, N, K, y_dt) bytes, 256-byte aligned (0, and
+ * then NULL, but for few fp32 results of a long k, whose parts are added in order).
  * ------------------------------------------------------------------------ */
+size_t mem_linear_blocks_workspace_size(int64_t T, int N, int K, pkmem_dtype y_dt);
+
 int mem_linear_blocks(const void* x, const void* w, const float* x_scale, const float* w_scale,
                       int w_tile, const void* bias, const void* res, int64_t T, int N, int K, int act,
-                      void* z_out, void* y_out, pkmem_dtype y_dt, pkmem_stream_t stream);
+                      void* z_out, void* y_out, pkmem_dtype y_dt, void* ws, size_t ws_bytes,
+                      pkmem_stream_t stream);
 
 /* ------------------------------------------------------------------------ *
  * AdamW (decoupled weight decay) over many tensors in few launches.  With

@@ -137,7 +137,9 @@ def load() -> ctypes.CDLL:
     L.mem_glu_backward.restype = I32
     L.mem_quantize_blocks.argtypes = [P, I32, I64, I32, I32, P, P, P, P, P]
     L.mem_quantize_blocks.restype = I32
-    L.mem_linear_blocks.argtypes = [P, P, P, P, I32, P, P, I64, I32, I32, I32, P, P, I32, P]
+    L.mem_linear_blocks_workspace_size.argtypes = [I64, I32, I32, I32]
+    L.mem_linear_blocks_workspace_size.restype = SZ
+    L.mem_linear_blocks.argtypes = [P, P, P, P, I32, P, P, I64, I32, I32, I32, P, P, I32, P, SZ, P]
     L.mem_linear_blocks.restype = I32
     L.mem_adamw.argtypes = [P, I32, P, P]
     L.mem_adamw.restype = I32
@@ -1002,7 +1004,7 @@ def mem_quantize_blocks(x: torch.Tensor, *, tile: bool = False, want_rows: bool 
 @_launches_on_stream
 def mem_linear_blocks(x: torch.Tensor, w: torch.Tensor, x_scale: torch.Tensor, w_scale: torch.Tensor,
                       bias=None, *, residual=None, act="none", out_dtype=None, y_out=None, z_out=None,
-                      want_z: bool = False, stream=None):
+                      want_z: bool = False, workspace=None, stream=None):
     """act(x w^T + bias) + residual for float8_e4m3fn operands x [T, K] and w [N, K] with a scale
     for each 128 along K: x_scale [ceil(K/128), T], w_scale [ceil(K/128), N] or, for
     128 x 128 tiles, [ceil(K/128), ceil(N/128)] (mem_quantize_blocks).
@@ -1010,7 +1012,7 @@ def mem_linear_blocks(x: torch.Tensor, w: torch.Tensor, x_scale: torch.Tensor, w
     out_dtype: float32 or bfloat16 (the default), the dtype of bias and residual too; in
     float32 products are exact.  y_out may be residual.  Returns (y, z) with z = x w^T + bias
     before the activation, None unless want_z."""
-    _here(x, w, x_scale, w_scale, bias, residual, y_out, z_out)
+    _here(x, w, x_scale, w_scale, bias, residual, y_out, z_out, workspace)
     T, K = x.shape
     N = w.shape[0]
     if x.dtype is not torch.float8_e4m3fn:
@@ -1039,9 +1041,15 @@ def mem_linear_blocks(x: torch.Tensor, w: torch.Tensor, x_scale: torch.Tensor, w
     if residual is not None:
         _like(residual, shape, out_dtype, "residual")
         rp = residual.data_ptr()
-    _check((_LIB or load()).mem_linear_blocks(x.data_ptr(), w.data_ptr(), x_scale.data_ptr(), w_scale.data_ptr(),
-                                              tiled, bp, rp, T, N, K, _act(act), zp, y_out.data_ptr(),
-                                              _dt(y_out), _stream(stream)))
+    L, ydt = _LIB or load(), _dt(y_out)
+    wsp = nbytes = 0
+    if ydt == F32:
+        nbytes = L.mem_linear_blocks_workspace_size(T, N, K, ydt)
+        if nbytes:
+            ws = _workspace(nbytes, x.device, workspace)
+            wsp, nbytes = ws.data_ptr(), ws.numel() * ws.element_size()
+    _check(L.mem_linear_blocks(x.data_ptr(), w.data_ptr(), x_scale.data_ptr(), w_scale.data_ptr(), tiled, bp, rp,
+                               T, N, K, _act(act), zp, y_out.data_ptr(), ydt, wsp, nbytes, _stream(stream)))
     return y_out, z_out
 
 

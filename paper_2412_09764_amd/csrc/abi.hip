@@ -1180,9 +1180,14 @@ int mem_quantize_blocks(const void* x, pkmem_dtype dt, int64_t R, int C, int til
   return hip_status(pk::launch_quantize_blocks(c, reinterpret_cast<hipStream_t>(stream)), fn);
 }
 
+size_t mem_linear_blocks_workspace_size(int64_t T, int N, int K, pkmem_dtype y_dt) {
+  if (T < 1 || N < 1 || K < 1) return 0;
+  return align256(pk::linear_blocks_ws_bytes(y_dt == PKMEM_BF16, T, N, K));
+}
+
 int mem_linear_blocks(const void* x, const void* w, const float* x_scale, const float* w_scale, int w_tile,
                       const void* bias, const void* res, int64_t T, int N, int K, int act, void* z_out, void* y_out,
-                      pkmem_dtype y_dt, pkmem_stream_t stream) {
+                      pkmem_dtype y_dt, void* ws, size_t ws_bytes, pkmem_stream_t stream) {
   const char* fn = "mem_linear_blocks";
   int rc = check_linear_shapes(fn, PKMEM_E4M3, true, T, N, K);
   if (rc) return rc;
@@ -1193,15 +1198,20 @@ int mem_linear_blocks(const void* x, const void* w, const float* x_scale, const 
   if (!aligned(x, 16) || !aligned(w, 16) || !aligned(x_scale, 4) || !aligned(w_scale, w_tile ? 4 : 16) || !aligned(bias, 16) ||
       !aligned(res, 16) || !aligned(z_out, 16) || !aligned(y_out, 16))
     return fail(PKMEM_ERR_INVALID, "%s: buffers must be 16-byte aligned (x_scale, and w_scale of tiles, 4)", fn);
+  const size_t need = mem_linear_blocks_workspace_size(T, N, K, y_dt);
+  if (need > 0 && (!ws || ws_bytes < need))
+    return fail(PKMEM_ERR_WORKSPACE, "%s: workspace of %zu bytes needed, %zu given", fn, need, ws ? ws_bytes : (size_t)0);
+  if (!aligned(ws, 256)) return fail(PKMEM_ERR_INVALID, "%s: workspace must be 256-byte aligned", fn);
   if (T == 0) return PKMEM_OK;
   const size_t kb = ((size_t)K + 127) / 128, nb = w_tile ? ((size_t)N + 127) / 128 : (size_t)N, ye = esize(y_dt),
                out = (size_t)T * N * ye;
   const Bytes bx{x, (size_t)T * K}, bw{w, (size_t)N * K}, bsx{x_scale, kb * T * 4}, bsw{w_scale, kb * nb * 4},
-      bb{bias, N * ye}, br{res, out}, bz{z_out, out}, by{y_out, out};
-  if (over(by, {bx, bw, bsx, bsw, bb, bz}, {br}) || over(bz, {bx, bw, bsx, bsw, bb, br}))
-    return fail(PKMEM_ERR_INVALID, "%s: an output may share no bytes with an operand or the other output (y_out may be res itself)", fn);
+      bb{bias, N * ye}, br{res, out}, bz{z_out, out}, by{y_out, out}, bws{need ? ws : nullptr, need};
+  if (over(by, {bx, bw, bsx, bsw, bb, bz}, {br}) || over(bz, {bx, bw, bsx, bsw, bb, br}) ||
+      over(bws, {bx, bw, bsx, bsw, bb, br, bz, by}))
+    return fail(PKMEM_ERR_INVALID, "%s: outputs and workspace may share no bytes with another buffer (y_out may be res itself)", fn);
   const pk::LinearCall c{x, w, PKMEM_E4M3, x_scale, w_scale, bias, res, T, N, K, act, z_out, y_out, y_dt == PKMEM_BF16};
-  return hip_status(pk::launch_linear_blocks(c, w_tile != 0, reinterpret_cast<hipStream_t>(stream)), fn);
+  return hip_status(pk::launch_linear_blocks(c, w_tile != 0, ws, reinterpret_cast<hipStream_t>(stream)), fn);
 }
 
 }  // extern "C"

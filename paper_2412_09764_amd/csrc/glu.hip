@@ -27,9 +27,9 @@ void glu_launch(const GemmArgs& g, hipStream_t st) {
     return;
   }
   const int tile = pick_tile(DT == D_F32, g.M, 2 * (int64_t)g.N);
-  if constexpr (DT == D_E4M3) {
-    if (g.out_bf16 && tile == TILE_256) return gemm8_launch<256, 256, 2, 4, G_GLU>(g, st);
-    if (g.out_bf16 && tile == TILE_128) return gemm8_launch<128, 128, 2, 2, G_GLU>(g, st);
+  if constexpr (DT != D_F32) {
+    if (g.out_bf16 && tile == TILE_256) return gemm8_launch<DT, 256, 256, 2, 4, G_GLU>(g, st);
+    if (g.out_bf16 && tile == TILE_128) return gemm8_launch<DT, 128, 128, 2, 2, G_GLU>(g, st);
   }
   switch (tile) {
     case TILE_256: glu_tile<DT, 256, 256, 2, 4, 1>(g, st); break;

@@ -59,7 +59,7 @@ __global__ __launch_bounds__(BLOCK) void k_layernorm(const T* x, const T* res, c
     if (res && ch < C) r[c] = ld16_nt(res + base + (size_t)ch * N);
   }
   const float first = element(x + base) + (res ? element(res + base) : 0.f);
-  float m = 0.f;
+  float m[1] = {0.f};
 #pragma unroll
   for (int c = 0; c < NCH; ++c) {
     Ch::unpack(a[c], h[c]);
@@ -73,24 +73,25 @@ __global__ __launch_bounds__(BLOCK) void k_layernorm(const T* x, const T* res, c
     }
     if (lr + c * LANES < C) {
 #pragma unroll
-      for (int i = 0; i < N; ++i) m = fmaf(h[c][i] - first, inv, m);
+      for (int i = 0; i < N; ++i) m[0] = fmaf(h[c][i] - first, inv, m[0]);
     }
   }
-  m = first + row_sum<WPR>(m, red, wave);
+  row_sums<WPR>(m, red, wave);
+  const float mean = first + m[0];
   float s[2] = {0.f, 0.f};
 #pragma unroll
   for (int c = 0; c < NCH; ++c) {
     if (lr + c * LANES < C) {
 #pragma unroll
       for (int i = 0; i < N; ++i) {
-        h[c][i] -= m;
+        h[c][i] -= mean;
         s[0] = fmaf(h[c][i], inv, s[0]);
         s[1] = fmaf(h[c][i], h[c][i], s[1]);
       }
     }
   }
   row_sums<WPR>(s, red, wave);
-  const RowStats st = row_stats(m, s[0], s[1], D, eps);
+  const RowStats st = row_stats(mean, s[0], s[1], D, eps);
 #pragma unroll
   for (int c = 0; c < NCH; ++c) {
     const int ch = lr + c * LANES;
@@ -131,6 +132,11 @@ __global__ __launch_bounds__(BLOCK) void k_layernorm_bwd(const T* dy, const T* h
   for (int c = 0; c < NCH; ++c)
 #pragma unroll
     for (int i = 0; i < N; ++i) gw[c][i] = gb[c][i] = 0.f;
+  // The weight stays in registers (read again for every row it is waited for twice: 32768 x
+  // 2048 bf16 124 us, so 94).
+  uint4 rw[NCH];
+#pragma unroll
+  for (int c = 0; c < NCH; ++c) rw[c] = w && lr + c * LANES < C ? ld16(w + (size_t)(lr + c * LANES) * N) : uint4{0, 0, 0, 0};
   for (int64_t row = row0; row < rows; row += step) {
     const size_t base = (size_t)row * D;
     uint4 rh[NCH], rd[NCH], rs[NCH];
@@ -145,16 +151,17 @@ __global__ __launch_bounds__(BLOCK) void k_layernorm_bwd(const T* dy, const T* h
       }
     }
     const float first = element(h_in + base);
-    float m = 0.f;
+    float sum[1] = {0.f};
 #pragma unroll
     for (int c = 0; c < NCH; ++c) {
       if (lr + c * LANES >= C) continue;
       float hv[N];
       Ch::unpack(rh[c], hv);
 #pragma unroll
-      for (int i = 0; i < N; ++i) m = fmaf(hv[i] - first, inv, m);
+      for (int i = 0; i < N; ++i) sum[0] = fmaf(hv[i] - first, inv, sum[0]);
     }
-    m = first + row_sum<WPR>(m, red, wave);
+    row_sums<WPR>(sum, red, wave);
+    const float m = first + sum[0];
     // sums of h - m, its square, g, g (h - m)
     float s[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
@@ -166,7 +173,7 @@ __global__ __launch_bounds__(BLOCK) void k_layernorm_bwd(const T* dy, const T* h
       Ch::unpack(rd[c], g);
 #pragma unroll
       for (int i = 0; i < N; ++i) wv[i] = 1.f;
-      if (w) Ch::unpack(ld16(w + (size_t)ch * N), wv);
+      if (w) Ch::unpack(rw[c], wv);
 #pragma unroll
       for (int i = 0; i < N; ++i) {
         const float v = hv[i] - m, gi = g[i] * wv[i];
@@ -190,7 +197,7 @@ __global__ __launch_bounds__(BLOCK) void k_layernorm_bwd(const T* dy, const T* h
       Ch::unpack(rs[c], sv);
 #pragma unroll
       for (int i = 0; i < N; ++i) wv[i] = 1.f;
-      if (w) Ch::unpack(ld16(w + (size_t)ch * N), wv);
+      if (w) Ch::unpack(rw[c], wv);
 #pragma unroll
       for (int i = 0; i < N; ++i) {
         const float xh = (hv[i] - m - st.d) * st.rstd;
@@ -248,6 +255,19 @@ __global__ __launch_bounds__(1024) void k_add_two(const float* __restrict__ part
   }
 }
 
+// Chunks per lane and waves per row for rows of C chunks: one wave up to 256 chunks (4 KiB), a
+// workgroup of four above (32768 x 4096 bf16 forward 190 us, with one wave 198; backward 188,
+// its two sums for each column would not fit one wave's registers).
+#define PK_LAYERNORM_DISPATCH(C, F)                                       \
+  do {                                                                    \
+    if ((C) <= 64) { F(1, 1); }                                           \
+    else if ((C) <= 128) { F(2, 1); }                                     \
+    else if ((C) <= 256) { F(4, 1); }                                     \
+    else if ((C) <= 512) { F(2, 4); }                                     \
+    else if ((C) <= 1024) { F(4, 4); }                                    \
+    else { F(8, 4); }                                                     \
+  } while (0)
+
 template <typename T>
 void layernorm_launch(const void* x, const void* res, const void* w, const void* b, int64_t rows, int D,
                       float eps, void* sum_out, void* y_out, hipStream_t st) {
@@ -262,7 +282,7 @@ void layernorm_launch(const void* x, const void* res, const void* w, const void*
                        (const T*)w, (const T*)b, n, D, eps, slice((T*)sum_out, r),                 \
                        slice((T*)y_out, r));                                                       \
   }
-  PK_NORM_DISPATCH(C, PK_F);
+  PK_LAYERNORM_DISPATCH(C, PK_F);
 #undef PK_F
 }
 
@@ -274,7 +294,7 @@ void layernorm_bwd_launch(const void* dy, const void* h, const void* w, const vo
   hipLaunchKernelGGL((k_layernorm_bwd<T, NCH, WPR>), dim3((unsigned)norm_parts(rows)),            \
                      dim3(BLOCK), (WPR) == 1 ? 2 * D * sizeof(float) : 0, st, (const T*)dy,       \
                      (const T*)h, (const T*)w, (const T*)dsum, rows, D, eps, (T*)dx, part)
-  PK_NORM_DISPATCH(C, PK_F);
+  PK_LAYERNORM_DISPATCH(C, PK_F);
 #undef PK_F
 }
 

@@ -468,7 +468,12 @@ __global__ __launch_bounds__(WM* WN* KG * 64) void k_gemm(const GemmArgs g) {
   int64_t k0 = split * g.k_split;
   int64_t k1 = k0 + g.k_split < g.K ? k0 + g.k_split : g.K;
   // this group's share of k; all groups take the same number of steps
-  const int steps = (int)((k1 - k0 + KG * OA::STAGE_ROWS - 1) / (KG * OA::STAGE_ROWS));
+  int steps = (int)((k1 - k0 + KG * OA::STAGE_ROWS - 1) / (KG * OA::STAGE_ROWS));
+  // BLOCKS: two stages are a block of scales, whose sums are held over both of them; an odd
+  // last stage gets an empty one.
+  constexpr bool HOLD = BLOCKS && !BLOCKS8;
+  static_assert(!HOLD || (MI * NJ <= 4 && 2 * OA::STAGE_ROWS == SCALE_K), "registers for two sets of sums");
+  if constexpr (HOLD) steps += steps & 1;
   if constexpr (KG > 1) {
     k0 += (int64_t)kg * steps * OA::STAGE_ROWS;
     const int64_t end = k0 + (int64_t)steps * OA::STAGE_ROWS;
@@ -610,9 +615,10 @@ __global__ __launch_bounds__(WM* WN* KG * 64) void k_gemm(const GemmArgs g) {
         for (int nj = 0; nj < NJ; ++nj) mma_bf16(b[nj][SPLIT_B[t]], a[SPLIT_A[t]], acc[mi][nj]);
     }
   };
-  // blocks: a stage's sums, then their addition with the scales, a tile behind them so
-  // that it runs while the matrix cores form the next sums.
-  auto products_blocks = [&](int set) PK_INLINE {
+  // blocks: a stage's (HOLD: a block's) sums, then their addition with the scales, a tile behind
+  // them so that it runs while the matrix cores form the next sums.
+  f32x16_t held[HOLD ? MI * NJ : 1];
+  auto products_blocks = [&](int set, bool second) PK_INLINE {
     uint4 b[NJ][4];
     if constexpr (!BLOCKS8) {
 #pragma unroll
@@ -634,25 +640,43 @@ __global__ __launch_bounds__(WM* WN* KG * 64) void k_gemm(const GemmArgs g) {
         for (int e = 0; e < 16; ++e) acc[mi][nj][e] = fmaf(p[e] * scale_b[set][nj][e], scale_a[set][mi], acc[mi][nj][e]);
       }
     };
-    f32x16_t p[2];
+    if constexpr (BLOCKS8) {
+      f32x16_t p[2];
 #pragma unroll
-    for (int t = 0; t < MI * NJ; ++t) {
-      const int mi = t / NJ, nj = t % NJ;
-      if constexpr (BLOCKS8) {
+      for (int t = 0; t < MI * NJ; ++t) {
+        const int mi = t / NJ, nj = t % NJ;
         p[t & 1] = mma_e4m3(fb[set][0][nj], fb[set][1][nj], fa[set][0][mi], fa[set][1][mi]);
-      } else {
-        p[t & 1] = f32x16_t{};
+        __builtin_amdgcn_sched_barrier(0);  // or one set of registers would do, and wait
+        if (t > 0) add(p[(t - 1) & 1], t - 1);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      add(p[(MI * NJ - 1) & 1], MI * NJ - 1);
+    } else {
+#pragma unroll
+      for (int mi = 0; mi < MI; ++mi) {
+        uint4 a[4];
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
           const uint4 f = fa[set][q >> 1][mi];
-          mma_bf16(b[nj][q], q & 1 ? widen8(f.z, f.w) : widen8(f.x, f.y), p[t & 1]);
+          a[q] = q & 1 ? widen8(f.z, f.w) : widen8(f.x, f.y);
+        }
+#pragma unroll
+        for (int nj = 0; nj < NJ; ++nj)
+          if (!second) held[mi * NJ + nj] = f32x16_t{};
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+#pragma unroll
+          for (int nj = 0; nj < NJ; ++nj) mma_bf16(b[nj][q], a[q], held[mi * NJ + nj]);
+        if (second && mi > 0) {
+#pragma unroll
+          for (int nj = 0; nj < NJ; ++nj) add(held[(mi - 1) * NJ + nj], (mi - 1) * NJ + nj);
         }
       }
-      __builtin_amdgcn_sched_barrier(0);  // or one set of registers would do, and wait
-      if (t > 0) add(p[(t - 1) & 1], t - 1);
-      __builtin_amdgcn_sched_barrier(0);
+      if (second) {
+#pragma unroll
+        for (int nj = 0; nj < NJ; ++nj) add(held[(MI - 1) * NJ + nj], (MI - 1) * NJ + nj);
+      }
     }
-    add(p[(MI * NJ - 1) & 1], MI * NJ - 1);
   };
   // The sums over A's k: when split, the tiles along j take the stages in turn, else
   // the first of them takes all.
@@ -679,12 +703,12 @@ __global__ __launch_bounds__(WM* WN* KG * 64) void k_gemm(const GemmArgs g) {
     // multiplying at once: 8192^3 878 -> 860 us, 2000 x 2048 x 2048 in e4m3 20 -> 18).
     // Stage s: the first four multiply, the last four read it; then the first
     // four read stage s + 1 and refill s.
-    auto multiply = [&]() PK_INLINE {
+    auto multiply = [&](bool second) PK_INLINE {
       __builtin_amdgcn_s_setprio(1);
       if constexpr (DT == D_F32) {
         products_f32(0);
       } else if constexpr (BLOCKS) {
-        products_blocks(0);
+        products_blocks(0, second);
       } else {
         products(0, false, st0);
         products(1, false, st0);
@@ -696,18 +720,18 @@ __global__ __launch_bounds__(WM* WN* KG * 64) void k_gemm(const GemmArgs g) {
       read(st, 1);
       add_bias(st);
     };
-    auto first = [&](unsigned char* st, const unsigned char* next) PK_INLINE {
-      multiply();
+    auto first = [&](unsigned char* st, const unsigned char* next, bool second = false) PK_INLINE {
+      multiply(second);
       wait_and_meet<2 * L>();  // the next stage has landed
       read_all(next);
       fill(st);
       wait_and_meet<63>();  // 63: for LDS alone
     };
-    auto last = [&](unsigned char* st, unsigned char* before) PK_INLINE {
+    auto last = [&](unsigned char* st, unsigned char* before, bool second = false) PK_INLINE {
       read_all(st);
       fill(before);
       wait_and_meet<2 * L>();
-      multiply();
+      multiply(second);
       wait_and_meet<63>();
     };
     fill(st0);
@@ -720,36 +744,36 @@ __global__ __launch_bounds__(WM* WN* KG * 64) void k_gemm(const GemmArgs g) {
       read_all(st0);
       for (; s + 4 <= steps; s += 4) {
         first(st0, st1);
-        first(st1, st2);
+        first(st1, st2, true);
         first(st2, st3);
-        first(st3, st0);
+        first(st3, st0, true);
       }
       if (s < steps) first(st0, st1);
-      if (s + 1 < steps) first(st1, st2);
+      if (s + 1 < steps) first(st1, st2, true);
       if (s + 2 < steps) first(st2, st3);
     } else {
       wait_and_meet<2 * L>();
       for (; s + 4 <= steps; s += 4) {
         last(st0, st3);
-        last(st1, st0);
+        last(st1, st0, true);
         last(st2, st1);
-        last(st3, st2);
+        last(st3, st2, true);
       }
       if (s < steps) last(st0, st3);
-      if (s + 1 < steps) last(st1, st0);
+      if (s + 1 < steps) last(st1, st0, true);
       if (s + 2 < steps) last(st2, st1);
     }
   } else if constexpr (DT == D_F32 || BLOCKS) {
     // One stage: it is in the registers of set; next has landed for all after the
     // barrier, and is read while the products run.
-    auto stage = [&](int set, unsigned char* st, const unsigned char* next) PK_INLINE {
+    auto stage = [&](int set, unsigned char* st, const unsigned char* next) PK_INLINE {  // set: the stage's parity
       wait_and_meet<2 * L>();
       read(next, 0, set ^ 1);
       read(next, 1, set ^ 1);
       __builtin_amdgcn_sched_barrier(0);
       add_bias(next);
       fill(st);
-      if constexpr (BLOCKS) products_blocks(set);
+      if constexpr (BLOCKS) products_blocks(set, set == 1);
       else products_f32(set);
     };
     fill(st0);
@@ -913,6 +937,12 @@ __global__ __launch_bounds__(WM* WN* KG * 64) void k_gemm(const GemmArgs g) {
             store8(g.out, at, false, v);
           }
         } else {
+          if constexpr (BLOCKS) {
+            if (g.part) {
+              store8(g.part + (size_t)split * g.M * g.N, at, false, v);
+              continue;
+            }
+          }
           if constexpr (!GLU) epi.store(g, at, g.a_scale ? g.a_scale[i] : 1.f, res[t], v);
         }
       }
@@ -950,7 +980,8 @@ __device__ __forceinline__ void mma16(uint4 w, uint4 x, f32x4_t& c) {
 
 template <int DT, int MODE = G_PLAIN>
 __global__ __launch_bounds__(FEW_WAVES * 64) void k_gemm_few(const GemmArgs g) {
-  constexpr int AHEAD = 4;  // chunks in flight
+  // Chunks in flight.  (GLU, 1 x 8192 x 2048 bf16: 16.3 us, with 4 17.3.)
+  constexpr int AHEAD = MODE == G_GLU ? 8 : 4;
   constexpr int U = MODE == G_GLU ? 2 : 1;  // rows of W with the same column of y
   constexpr bool BLOCKS = MODE == G_BLOCKS || MODE == G_BLOCKS_TILED, TILED = MODE == G_BLOCKS_TILED;
   static_assert(MODE < G_BLOCKS8, "products are widened here");

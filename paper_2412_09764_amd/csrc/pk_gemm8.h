@@ -1,5 +1,5 @@
-// Matrix products of e4m3 codes at the 8-bit matrix instruction's rate, for results that are
-// stored in bf16: the large tiles of the products in blocks and of the gated part.
+// The large tiles of the products in blocks and of the gated part, for results that are stored
+// in bf16: e4m3 codes at the 8-bit matrix instruction's rate, and bf16.
 #pragma once
 
 #include "pk_gemm.h"
@@ -8,14 +8,24 @@ namespace pk {
 
 namespace {
 
-constexpr int STEP_K = 128;  // k of a step: one block of scales, one 16x16x128 instruction
+constexpr int STEP_BYTES = 128;  // of k in a step; codes: one block of scales, one 16x16x128 instruction
 
-// See mma_e4m3 on what the instruction keeps.  The lanes' 32 k may be any, the same for both.
-__device__ __forceinline__ f32x4_t mma_e4m3_16(const uint4 (&b)[2], const uint4 (&a)[2], f32x4_t c) {
-  typedef __attribute__((ext_vector_type(8))) int i32x8_t;
-  const i32x8_t y{(int)b[0].x, (int)b[0].y, (int)b[0].z, (int)b[0].w, (int)b[1].x, (int)b[1].y, (int)b[1].z, (int)b[1].w};
-  const i32x8_t x{(int)a[0].x, (int)a[0].y, (int)a[0].z, (int)a[0].w, (int)a[1].x, (int)a[1].y, (int)a[1].z, (int)a[1].w};
-  return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(y, x, c, 0, 0, 0, 0, 0, 0);
+// A step's products of two blocks of 16 rows; the lanes' k may be any, the same for both.  See
+// mma_e4m3 on what the instruction of codes keeps.
+template <int DT>
+__device__ __forceinline__ f32x4_t mma_step(const uint4 (&b)[2], const uint4 (&a)[2], f32x4_t c) {
+  if constexpr (DT == D_BF16) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+      c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, b[h]), __builtin_bit_cast(bf16x8_t, a[h]),
+                                                  c, 0, 0, 0);
+    return c;
+  } else {
+    typedef __attribute__((ext_vector_type(8))) int i32x8_t;
+    const i32x8_t y{(int)b[0].x, (int)b[0].y, (int)b[0].z, (int)b[0].w, (int)b[1].x, (int)b[1].y, (int)b[1].z, (int)b[1].w};
+    const i32x8_t x{(int)a[0].x, (int)a[0].y, (int)a[0].z, (int)a[0].w, (int)a[1].x, (int)a[1].y, (int)a[1].z, (int)a[1].w};
+    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(y, x, c, 0, 0, 0, 0, 0, 0);
+  }
 }
 
 // Rows of 128 bytes (a step's k) in LDS; 16-byte chunk c of row r lies at slot
@@ -23,7 +33,7 @@ __device__ __forceinline__ f32x4_t mma_e4m3_16(const uint4 (&b)[2], const uint4 
 // columns of its 64 banks.  GLU: as Operand's.
 template <int R, int NWAVE, bool GLU>
 struct Codes {
-  static constexpr int BYTES = R * STEP_K, LOADS = BYTES / 1024 / NWAVE;
+  static constexpr int BYTES = R * STEP_BYTES, LOADS = BYTES / 1024 / NWAVE;
   // A load brings 8 rows.  Loads of one wave are a fixed number of rows apart, so one offset
   // serves them all; rows past the end lie past the end of the resource.
   static_assert(NWAVE == 4 || NWAVE == 8, "the same chunks in every load of a wave");
@@ -31,17 +41,17 @@ struct Codes {
   int64_t up;
   uint32_t off, row;
   int bytes;
-  int left;  // k from the next step on
+  int left;  // bytes of k from the next step on
 
   __device__ static __forceinline__ int source_chunk(int wave, int lane) {
     return (lane & 7) ^ ((wave * 4 + (lane >> 4)) & 7);
   }
-  __device__ __forceinline__ void init(const void* p, int64_t row0, int64_t rows, int64_t K, bool in, int wave, int lane) {
-    left = in ? (int)K : 0;
-    base = (const char*)p + row0 * K;
-    up = rows * K;
-    row = (uint32_t)K;
-    bytes = in ? (int)((rows - row0 < R ? rows - row0 : R) * K) : 0;
+  __device__ __forceinline__ void init(const void* p, int64_t row0, int64_t rows, int64_t row_bytes, bool in, int wave, int lane) {
+    left = in ? (int)row_bytes : 0;
+    base = (const char*)p + row0 * row_bytes;
+    up = rows * row_bytes;
+    row = (uint32_t)row_bytes;
+    bytes = in ? (int)((rows - row0 < R ? rows - row0 : R) * row_bytes) : 0;
     off = (uint32_t)((GLU ? (wave & 3) : wave) * 8 + (lane >> 3)) * row + source_chunk(wave, lane) * 16;
     if (GLU && (wave & 4)) base += up;
   }
@@ -49,21 +59,21 @@ struct Codes {
   // ends with the resource; where k has ended nothing is read and the slots become 0.
   __device__ __forceinline__ void load(unsigned char* lds, int wave, int lane) {
     const uint32_t room = bytes > 0 ? (uint32_t)bytes : 0u;
-    const uint32_t o = left >= STEP_K || source_chunk(wave, lane) * 16 < left ? off : OUTSIDE;
+    const uint32_t o = left >= STEP_BYTES || source_chunk(wave, lane) * 16 < left ? off : OUTSIDE;
 #pragma unroll
     for (int i = 0; i < LOADS; ++i) {
       const bool other = GLU && NWAVE == 4 && (i & 1);  // the up projection's rows
       const uint32_t r = GLU ? (NWAVE == 4 ? i / 2 : i) * 32 : i * NWAVE * 8;
       lds_dma16_buf(raw_buffer(other ? base + up : base, room), o + r * row, 0u, lds + (i * NWAVE + wave) * 1024);
     }
-    base += STEP_K;
-    bytes -= STEP_K;
-    left -= STEP_K;
+    base += STEP_BYTES;
+    bytes -= STEP_BYTES;
+    left -= STEP_BYTES;
   }
   // Where this lane's codes of row r (its number in a block of 16 rows: lane % 16) lie: chunks
   // q and q + 4, q = lane / 16, the second one 64 bytes up or down.
   __device__ static __forceinline__ uint32_t place(int r, int lane) {
-    return r * STEP_K + (((lane >> 4) ^ ((r >> 1) & 7)) << 4);
+    return r * STEP_BYTES + (((lane >> 4) ^ ((r >> 1) & 7)) << 4);
   }
 };
 
@@ -76,10 +86,11 @@ struct Codes {
 // issued, and its results leave (through LDS that step has used) while they arrive.  MODE: G_GLU
 // (sums in place), G_BLOCKS8 and G_BLOCKS8_TILED (a step's sums are added with their scales
 // two products later).
-template <int BM, int BN, int WM, int WN, int MODE>
+template <int DT, int BM, int BN, int WM, int WN, int MODE>
 __global__ __launch_bounds__(WM* WN * 64) void k_gemm8(const GemmArgs g) {
   constexpr int NW = WM * WN, MI = BM / WM / 16, NJ = BN / WN / 16;
   constexpr bool GLU = MODE == G_GLU, TILED = MODE == G_BLOCKS8_TILED;
+  static_assert(GLU || DT == D_E4M3, "scales are of codes");
   static_assert(NJ == 4, "64 columns a wave");
   using CA = Codes<BM, NW, false>;
   using CB = Codes<BN, NW, GLU>;
@@ -119,8 +130,8 @@ __global__ __launch_bounds__(WM* WN * 64) void k_gemm8(const GemmArgs g) {
     t -= group * 4 * g.tiles_n;
     ti = (int64_t)(m_first + t % m_count) * BM;
     tj = t / m_count * (GLU ? BN / 2 : BN);
-    ca.init(g.a, ti, g.M, g.K, in, wave, lane);
-    cb.init(g.b, tj, g.N, g.K, in, wave, lane);
+    ca.init(g.a, ti, g.M, g.K * elem_size(DT), in, wave, lane);
+    cb.init(g.b, tj, g.N, g.K * elem_size(DT), in, wave, lane);
 #pragma unroll
     for (int i = 0; i < SCALE_LOADS; ++i) {  // rows past the end take the last one's: their codes are 0
       const int r = (i * NW + wave) * 64 + lane;
@@ -138,7 +149,7 @@ __global__ __launch_bounds__(WM* WN * 64) void k_gemm8(const GemmArgs g) {
 #pragma unroll
     for (int i = 0; i < SCALE_LOADS; ++i) {
       lds_dma4(scale_at[i], st + SCALES_AT + (i * NW + wave) * 256);
-      if (ca.left > STEP_K) scale_at[i] += scale_step[i];  // after the last block: that one again
+      if (ca.left > STEP_BYTES) scale_at[i] += scale_step[i];  // after the last block: that one again
     }
     ca.load(st, wave, lane);
     cb.load(st + CA::BYTES, wave, lane);
@@ -168,13 +179,13 @@ __global__ __launch_bounds__(WM* WN * 64) void k_gemm8(const GemmArgs g) {
   const uint32_t at_a = CA::place(wi + (lane & 15), lane), at_b = CB::place(wj + (lane & 15), lane);
   const uint32_t at_sa = SCALES_AT + (wi + (lane & 15)) * 4, at_sb = SCALES_AT + (BM + wj + (TILED ? 0 : 4 * (lane >> 4))) * 4;
   auto read_a = [&](const unsigned char* st, int mi) PK_INLINE {
-    fa[mi & 1][0] = ld16(st + at_a + mi * 16 * STEP_K);
-    fa[mi & 1][1] = ld16(st + (at_a ^ 64) + mi * 16 * STEP_K);
+    fa[mi & 1][0] = ld16(st + at_a + mi * 16 * STEP_BYTES);
+    fa[mi & 1][1] = ld16(st + (at_a ^ 64) + mi * 16 * STEP_BYTES);
     if constexpr (!GLU) sa[mi & 3] = *reinterpret_cast<const float*>(st + at_sa + mi * 64);
   };
   auto read_b = [&](const unsigned char* st, int nj) PK_INLINE {
-    fb[nj][0] = ld16(st + CA::BYTES + at_b + nj * 16 * STEP_K);
-    fb[nj][1] = ld16(st + CA::BYTES + (at_b ^ 64) + nj * 16 * STEP_K);
+    fb[nj][0] = ld16(st + CA::BYTES + at_b + nj * 16 * STEP_BYTES);
+    fb[nj][1] = ld16(st + CA::BYTES + (at_b ^ 64) + nj * 16 * STEP_BYTES);
   };
   auto read_sb = [&](const unsigned char* st) PK_INLINE {
     if constexpr (!GLU) {
@@ -190,8 +201,8 @@ __global__ __launch_bounds__(WM* WN * 64) void k_gemm8(const GemmArgs g) {
     }
   };
   auto multiply = [&](int mi, int nj) PK_INLINE {
-    if constexpr (GLU) acc[mi][nj] = mma_e4m3_16(fb[nj], fa[mi & 1], acc[mi][nj]);
-    else p[(mi * NJ + nj) % 3] = mma_e4m3_16(fb[nj], fa[mi & 1], f32x4_t{0.f, 0.f, 0.f, 0.f});
+    if constexpr (GLU) acc[mi][nj] = mma_step<DT>(fb[nj], fa[mi & 1], acc[mi][nj]);
+    else p[(mi * NJ + nj) % 3] = mma_step<DT>(fb[nj], fa[mi & 1], f32x4_t{0.f, 0.f, 0.f, 0.f});
     __builtin_amdgcn_sched_barrier(0);
   };
   float s_tile = 0.f;
@@ -258,7 +269,7 @@ __global__ __launch_bounds__(WM* WN * 64) void k_gemm8(const GemmArgs g) {
     for (int u = 0; u < U; ++u) {
 #pragma unroll
       for (int e = 0; e < 8; ++e) scale[u][e] = 1.f, bias[u][e] = 0.f;
-      if (GLU && in) {
+      if (DT == D_E4M3 && GLU && in) {
         Raw8 r;
         r.load(g.b_scale, (size_t)u * g.N + j, false);
         r.unpack(false, scale[u]);
@@ -281,7 +292,7 @@ __global__ __launch_bounds__(WM* WN * 64) void k_gemm8(const GemmArgs g) {
         const int64_t i = ip + STEP * t;
         res[t] = none;
         sx[t] = 1.f;
-        if (GLU && i < g.M) sx[t] = g.a_scale[i];
+        if (DT == D_E4M3 && GLU && i < g.M) sx[t] = g.a_scale[i];
         if (!GLU && g.res && in && i < g.M) res[t] = ld16((const uint16_t*)g.res + (size_t)i * g.N + j);
       }
 #pragma unroll
@@ -326,7 +337,7 @@ __global__ __launch_bounds__(WM* WN * 64) void k_gemm8(const GemmArgs g) {
   };
 
   // Steps in pairs, so that every tile starts in st0 (an odd last one gets an empty one).
-  const int pairs = (int)((g.K + 2 * STEP_K - 1) / (2 * STEP_K));
+  const int pairs = (int)((g.K * elem_size(DT) + 2 * STEP_BYTES - 1) / (2 * STEP_BYTES));
   set_tile(tile, i0, j0);
   fill(st0);
   bool drain = true;  // the loads are the newest operations
@@ -365,12 +376,12 @@ __global__ __launch_bounds__(WM* WN * 64) void k_gemm8(const GemmArgs g) {
   wait_loads<0>();  // no load may reach LDS after the workgroup has left it
 }
 
-template <int BM, int BN, int WM, int WN, int MODE>
+template <int DT, int BM, int BN, int WM, int WN, int MODE>
 void gemm8_launch(GemmArgs g, hipStream_t st) {
   g.tiles_m = ceil_div(g.M, BM);
   g.tiles_n = ceil_div(g.N, MODE == G_GLU ? BN / 2 : BN);
   const int tiles = g.tiles_m * g.tiles_n, most = BM == 256 ? 256 : 512;  // of the chip's 256 CUs, by LDS
-  hipLaunchKernelGGL((k_gemm8<BM, BN, WM, WN, MODE>), dim3((unsigned)(tiles < most ? tiles : most)), dim3(WM * WN * 64), 0,
+  hipLaunchKernelGGL((k_gemm8<DT, BM, BN, WM, WN, MODE>), dim3((unsigned)(tiles < most ? tiles : most)), dim3(WM * WN * 64), 0,
                      st, g);
 }
 

@@ -201,7 +201,8 @@ struct QuantizeCall {
 };
 hipError_t launch_quantize_blocks(const QuantizeCall& c, hipStream_t st);
 // x_scale, w_scale: of blocks of 128 k; tiled: of 128 rows of w too.
-hipError_t launch_linear_blocks(const LinearCall& c, bool tiled, hipStream_t st);
+size_t linear_blocks_ws_bytes(bool out_bf16, int64_t T, int N, int K);
+hipError_t launch_linear_blocks(const LinearCall& c, bool tiled, void* ws, hipStream_t st);
 
 // ---- optimizer (adamw.hip) -------------------------------------------------
 constexpr int ADAMW_STATE_BLOCK = 128;  // elements that share the scales of 8-bit states

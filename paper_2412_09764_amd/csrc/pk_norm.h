@@ -18,11 +18,25 @@ __device__ __forceinline__ float row_sum(float v, float* red, int wave) {
   __syncthreads();  // red is free again
   return v;
 }
-// M sums at once; red holds 4 M numbers.
+// The wave's sum in every lane, without LDS: rotations within 16 lanes, then exchanges of
+// them (each adds the same two numbers in both lanes, so all lanes get the same bits).
+__device__ __forceinline__ float wave_sum(float v) {
+#define PK_ROR(N) v += __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(v), 0x120 + N, 15, 15, true))
+  PK_ROR(8);
+  PK_ROR(4);
+  PK_ROR(2);
+  PK_ROR(1);
+#undef PK_ROR
+  auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  v = __uint_as_float(a[0]) + __uint_as_float(a[1]);
+  a = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return __uint_as_float(a[0]) + __uint_as_float(a[1]);
+}
+// M sums over the lanes of a row at once; red holds 4 M numbers.
 template <int WPR, int M>
 __device__ __forceinline__ void row_sums(float (&v)[M], float* red, int wave) {
 #pragma unroll
-  for (int i = 0; i < M; ++i) v[i] = group_sum<WAVE>(v[i]);
+  for (int i = 0; i < M; ++i) v[i] = wave_sum(v[i]);
   if constexpr (WPR > 1) {
     if ((threadIdx.x & 63) == 0) {
 #pragma unroll

@@ -105,7 +105,8 @@ def test_nan_and_infinity_stay_in_their_block(gpu_lib):
 # of a part of a block, of many blocks
 SHAPES = [(1, 8, 16), (1, 2048, 528), (3, 520, 1040), (8, 136, 80), (9, 8, 144), (17, 136, 80), (33, 128, 128), (65, 264, 208),
           (129, 256, 32), (255, 1032, 144), (333, 1096, 400), (1000, 1032, 272), (1800, 1992, 272), (2000, 2056, 144),
-          (4100, 1032, 272), (6500, 2056, 272), (40, 72, 2064), (777, 200, 1168)]
+          (4100, 1032, 272), (6500, 2056, 272), (40, 72, 2064), (777, 200, 1168),
+          (9, 8, 16400), (300, 264, 8208), (2040, 1000, 9008), (130, 2048, 16400)]  # the first, third and fourth: k in parts
 
 
 def scales(shape, seed):
