@@ -489,7 +489,7 @@ int mem_linear_backward(const void* dz, const void* x, const void* w, pkmem_dtyp
  *   y[t,:] = (h[t,:] - mean[t]) * rstd[t] * weight + bias, mean and biased variance
  *            over the row in fp32 (deviations from a first mean correct both),
  *            rstd = 1 / sqrt(variance + eps) (0 where that sum is 0 or past the largest
- *            number: rows with deviations beyond 1e18 may give bias), rounded once to dt.
+ *            number; rows with deviations beyond 1e18 may give bias or NaN), rounded once to dt.
  *
  *   x       [T, D] dtype dt (PKMEM_F32 or PKMEM_BF16).
  *   res     [T, D] dtype dt; NULL: h = x.
