@@ -94,6 +94,11 @@ __device__ __forceinline__ void lds_dma16_buf(__amdgpu_buffer_rsrc_t r, uint32_t
                                            (int)voff, (int)soff, 0, 0);
 }
 
+// 16 bytes a lane; past the resource's end nothing is written.
+__device__ __forceinline__ void store16(__amdgpu_buffer_rsrc_t r, uint4 v, uint32_t off) {
+  typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
+  __builtin_amdgcn_raw_buffer_store_b128(u32x4{v.x, v.y, v.z, v.w}, r, off, 0, 0);
+}
 // One dword a lane, from any addresses, to 256 consecutive bytes of LDS.
 __device__ __forceinline__ void lds_dma4(const void* from, void* lds_base) {
   __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)from,

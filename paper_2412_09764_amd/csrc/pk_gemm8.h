@@ -251,101 +251,152 @@ __global__ __launch_bounds__(WM* WN * 64) void k_gemm8(const GemmArgs g) {
     add(LAST - 1, NJ - 2);
     add(LAST - 1, NJ - 1);
   };
-  // The sums leave through LDS, 32 rows of a wave's 64 columns at a time, so that every store
-  // covers whole cache lines; chunk c of row r lies at slot c ^ (r mod 16).
-  constexpr int PIECE = 32 * 256;
-  static_assert(BYTES >= NW * PIECE, "a piece for each wave");
-  constexpr int ROW_LANES = GLU ? 4 : 8, STEP = 64 / ROW_LANES, ROWS = 32 / STEP;
-  constexpr int STORES = MI * 16 / STEP;  // of a wave whose tile is whole, at least
-  auto leave_as = [&](auto act) PK_INLINE {
+  // The results are formed where the sums lie (a lane has 4 consecutive columns of a row, the
+  // gate's and the up projection's alike), rounded, and leave through LDS, 32 rows of a wave at a time,
+  // so that every store covers whole cache lines.  Rows of 128 bytes (64 for GLU's y); 16-byte
+  // chunk c of row r lies at slot c ^ (r / 2) (c ^ (r / 4)) modulo the chunks of a row.
+  constexpr int Z_PIECE = 32 * 128, Y_ROW = GLU ? 64 : 128, Y_PIECE = 32 * Y_ROW;
+  static_assert(BYTES >= NW * (Z_PIECE + Y_PIECE), "pieces for each wave");
+  constexpr int ROW_LANES = Y_ROW / 16, STEP = 64 / ROW_LANES;
+  constexpr int STORES = MI * 16 / STEP;  // of y, by a wave and tile
+  // Loads and stores go through resources that end with the tile's rows (or are empty), so that no
+  // branch hides from the compiler how many of them are under way.
+  auto leave_as = [&](auto act, auto with_z, auto with_res) PK_INLINE {
     constexpr int ACT = decltype(act)::value;
-    const int lane = again(), rr = lane / ROW_LANES, cc = lane % ROW_LANES;
-    unsigned char* buf = st1 + wave * PIECE;
-    const int j = j0 + (GLU ? wj / 2 : wj) + 8 * cc;
-    const bool in = j < g.N;
-    constexpr int U = GLU ? 2 : 1;
-    float scale[U][8], bias[U][8];  // of this lane's columns
+    constexpr bool Z = decltype(with_z)::value, RES = decltype(with_res)::value;
+    constexpr bool SCALED = GLU && DT == D_E4M3;
+    const int lane = again(), il = lane & 15, q4 = 4 * (lane >> 4);
+    unsigned char *zb = st1 + wave * (Z_PIECE + Y_PIECE), *yb = zb + Z_PIECE;
+    const int64_t tile_rows = g.M - i0 < BM ? g.M - i0 : BM;
+    const uint32_t row_y = 2u * g.N, row_z = (GLU ? 2 : 1) * row_y;
+    auto rows_of = [&](const void* p, uint32_t row_bytes) PK_INLINE {
+      return raw_buffer((const char*)p + (size_t)i0 * row_bytes, (uint32_t)tile_rows * row_bytes);
+    };
+    const auto out = rows_of(g.out, row_y), zs = rows_of(g.z, Z ? row_z : 0), rs = rows_of(g.res, RES ? row_y : 0);
+    const auto sx_rows = raw_buffer(g.a_scale + (SCALED ? i0 : 0), SCALED ? (uint32_t)tile_rows * 4 : 0);
+    // column block nj of this lane: GLU: 0 and 1 are the gate's, 2 and 3 the up projection's
+    auto column = [&](int nj) PK_INLINE { return j0 + (GLU ? wj / 2 + (nj & 1) * 16 : wj + nj * 16) + q4; };
+    float bias[NJ][4], scale[SCALED ? NJ : 1][4];
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
+    for (int nj = 0; nj < NJ; ++nj) {
+      const size_t at = (size_t)column(nj) + (GLU && nj >= 2 ? g.N : 0);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) scale[u][e] = 1.f, bias[u][e] = 0.f;
-      if (DT == D_E4M3 && GLU && in) {
-        Raw8 r;
-        r.load(g.b_scale, (size_t)u * g.N + j, false);
-        r.unpack(false, scale[u]);
-      }
-      if (g.bias && in) {
-        Raw8 r;
-        r.load(g.bias, (size_t)u * g.N + j, true);
-        r.unpack(true, bias[u]);
+      for (int e = 0; e < 4; ++e) bias[nj][e] = 0.f;
+      if (column(nj) < g.N) {
+        if (g.bias) {
+          const uint2 r = *reinterpret_cast<const uint2*>((const uint16_t*)g.bias + at);
+          bias[nj][0] = bf16_lo(r.x); bias[nj][1] = bf16_hi(r.x); bias[nj][2] = bf16_lo(r.y); bias[nj][3] = bf16_hi(r.y);
+        }
+        if constexpr (SCALED) load4(g.b_scale, at, scale[nj]);
       }
     }
-    const int row_z = U * g.N;
-    uint16_t *z = (uint16_t*)g.z, *out = (uint16_t*)g.out;
-#pragma unroll
-    for (int mp = 0; mp < MI; mp += 2) {
-      const int64_t ip = i0 + wi + mp * 16 + rr;
-      uint4 res[ROWS];
-      float sx[ROWS];
-#pragma unroll
-      for (int t = 0; t < ROWS; ++t) {
-        const int64_t i = ip + STEP * t;
-        res[t] = none;
-        sx[t] = 1.f;
-        if (DT == D_E4M3 && GLU && i < g.M) sx[t] = g.a_scale[i];
-        if (!GLU && g.res && in && i < g.M) res[t] = ld16((const uint16_t*)g.res + (size_t)i * g.N + j);
-      }
+    // where 8 bytes of block nj (or a half of GLU's y) of row r go
+    auto slot = [&](unsigned char* p, int row_bytes, int r, int block) PK_INLINE {
+      const int c = block * 2 + (lane >> 5), x = row_bytes == 128 ? (r >> 1) & 7 : (r >> 2) & 3;
+      return reinterpret_cast<uint2*>(p + r * row_bytes + ((c ^ x) << 4) + ((lane >> 4) & 1) * 8);
+    };
+    // whole rows of 128 bytes: 8 rows an access, this lane's 16 bytes of them
+    const int row8 = lane >> 3, chunk = lane & 7;
+    const int jz = j0 + (GLU ? wj / 2 + 8 * (chunk & 3) : wj + 8 * chunk);
+    const uint32_t oz = jz < g.N ? (wi + row8) * row_z + 2u * (jz + (GLU && chunk >= 4 ? g.N : 0)) : OUTSIDE;
+    const uint32_t orow = !GLU ? oz : 0;
+    // rows of y: this lane's 16 bytes
+    const int rr = lane / ROW_LANES, cc = lane % ROW_LANES, jy = j0 + (GLU ? wj / 2 : wj) + 8 * cc;
+    const uint32_t oy = jy < g.N ? (wi + rr) * row_y + 2u * jy : OUTSIDE;
+    // What the rows of a piece bring along, loaded a piece ahead: the residual in whole cache
+    // lines, turned round in y's place.
+    uint4 res[4];
+    float sx[2] = {1.f, 1.f};
+    auto ahead = [&](int mp) PK_INLINE {
 #pragma unroll
       for (int m = 0; m < 2; ++m)
+        if constexpr (SCALED)
+          sx[m] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(sx_rows, (wi + (mp + m) * 16 + il) * 4, 0, 0));
+#pragma unroll
+      for (int t = 0; t < 4; ++t)
+        if constexpr (RES)
+          res[t] = __builtin_bit_cast(uint4, __builtin_amdgcn_raw_buffer_load_b128(rs, orow + (mp * 16 + 8 * t) * row_y, 0, 0));
+    };
+    ahead(0);
+#pragma unroll
+    for (int mp = 0; mp < MI; mp += 2) {
+      const float sx0 = sx[0], sx1 = sx[1];
+      if constexpr (RES) {
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+          const int r = 8 * t + row8;
+          *reinterpret_cast<uint4*>(yb + r * Y_ROW + ((chunk ^ ((r >> 1) & 7)) << 4)) = res[t];
+        }
+      }
+      if (mp + 2 < MI) ahead(mp + 2);
+#pragma unroll
+      for (int m = 0; m < 2; ++m) {
+        const int r = m * 16 + il;
+        float v[NJ][4];
 #pragma unroll
         for (int nj = 0; nj < NJ; ++nj) {
-          const f32x4_t& c = acc[mp + m][nj];
-          const int row = m * 16 + (lane & 15), ch = nj * 4 + (lane >> 4);
-          *reinterpret_cast<float4*>(buf + row * 256 + ((ch ^ (row & 15)) << 4)) = float4{c[0], c[1], c[2], c[3]};
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            v[nj][e] = SCALED ? fmaf(acc[mp + m][nj][e], (m ? sx1 : sx0) * scale[SCALED ? nj : 0][e], bias[nj][e]) : acc[mp + m][nj][e] + bias[nj][e];
+          if constexpr (Z) *slot(zb, 128, r, nj) = uint2{to_bf16x2(v[nj][0], v[nj][1]), to_bf16x2(v[nj][2], v[nj][3])};
         }
 #pragma unroll
-      for (int t = 0; t < ROWS; ++t) {
-        const int row = rr + STEP * t;
-        const int64_t i = ip + STEP * t;
-        if (!in || i >= g.M) continue;
-        float v[U][8];
+        for (int nj = 0; nj < (GLU ? 2 : NJ); ++nj) {
+          float u[4] = {0.f, 0.f, 0.f, 0.f};
+          if constexpr (RES) {
+            const uint2 w = *slot(yb, Y_ROW, r, nj);
+            u[0] = bf16_lo(w.x), u[1] = bf16_hi(w.x), u[2] = bf16_lo(w.y), u[3] = bf16_hi(w.y);
+          }
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-          const int c = 8 * u + 2 * cc;
-          Chunk<float>::unpack(ld16(buf + row * 256 + ((c ^ (row & 15)) << 4)), v[u]);
-          Chunk<float>::unpack(ld16(buf + row * 256 + (((c + 1) ^ (row & 15)) << 4)), v[u] + 4);
-#pragma unroll
-          for (int e = 0; e < 8; ++e) v[u][e] = GLU ? fmaf(v[u][e], sx[t] * scale[u][e], bias[u][e]) : v[u][e] + bias[u][e];
-          if (z) store8(z, (size_t)i * row_z + u * g.N + j, true, v[u]);
+          for (int e = 0; e < 4; ++e) {
+            const float a = act_of<true, ACT>(v[nj][e]);
+            u[e] = GLU ? a * v[(nj + 2) % NJ][e] : RES ? a + u[e] : a;
+          }
+          *slot(yb, Y_ROW, r, nj) = uint2{to_bf16x2(u[0], u[1]), to_bf16x2(u[2], u[3])};
         }
-        float r[8];
-        Chunk<uint16_t>::unpack(res[t], r);
+      }
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          v[0][e] = act_of<true, ACT>(v[0][e]);
-          v[0][e] = GLU ? v[0][e] * v[U - 1][e] : v[0][e] + r[e];
+      for (int t = 0; t < 32 / STEP; ++t) {
+        const int r = rr + STEP * t, x = GLU ? (r >> 2) & 3 : (r >> 1) & 7;
+        store16(out, ld16(yb + r * Y_ROW + ((cc ^ x) << 4)), oy + (mp * 16 + STEP * t) * row_y);
+      }
+      if constexpr (Z) {
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+          const int r = row8 + 8 * t;
+          store16(zs, ld16(zb + r * 128 + ((chunk ^ ((r >> 1) & 7)) << 4)), oz + (mp * 16 + 8 * t) * row_z);
         }
-        store8(out, (size_t)i * g.N + j, true, v[0]);
       }
     }
   };
+  auto leave_z = [&](auto z, auto res) PK_INLINE {
+    if (g.act == PKMEM_ACT_NONE) leave_as(std::integral_constant<int, PKMEM_ACT_NONE>(), z, res);
+    else if (g.act == PKMEM_ACT_SILU) leave_as(std::integral_constant<int, PKMEM_ACT_SILU>(), z, res);
+    else if (g.act == PKMEM_ACT_GELU) leave_as(std::integral_constant<int, PKMEM_ACT_GELU>(), z, res);
+    else leave_as(std::integral_constant<int, PKMEM_ACT_RELU>(), z, res);
+  };
   auto leave = [&]() PK_INLINE {
-    if (g.act == PKMEM_ACT_NONE) leave_as(std::integral_constant<int, PKMEM_ACT_NONE>());
-    else if (g.act == PKMEM_ACT_SILU) leave_as(std::integral_constant<int, PKMEM_ACT_SILU>());
-    else if (g.act == PKMEM_ACT_GELU) leave_as(std::integral_constant<int, PKMEM_ACT_GELU>());
-    else leave_as(std::integral_constant<int, PKMEM_ACT_RELU>());
+    if (g.z) {
+      if (!GLU && g.res) leave_z(std::true_type(), std::bool_constant<!GLU>());
+      else leave_z(std::true_type(), std::false_type());
+    } else {
+      if (!GLU && g.res) leave_z(std::false_type(), std::bool_constant<!GLU>());
+      else leave_z(std::false_type(), std::false_type());
+    }
   };
 
   // Steps in pairs, so that every tile starts in st0 (an odd last one gets an empty one).
   const int pairs = (int)((g.K * elem_size(DT) + 2 * STEP_BYTES - 1) / (2 * STEP_BYTES));
   set_tile(tile, i0, j0);
   fill(st0);
-  bool drain = true;  // the loads are the newest operations
+  bool first = true;
   while (true) {
     clear();
-    // the first step's loads are older than the stores of the tile before, which need not be waited for
-    if (drain) wait_and_meet<0>();
+    // the first step's loads are older than the stores of the tile before, STORES at least, which
+    // need not be waited for
+    if (first) wait_and_meet<0>();
     else wait_and_meet<STORES>();
+    first = false;
     step(st0, st1);
     for (int s = 1; s < pairs; ++s) {
       wait_and_meet<0>();
@@ -367,7 +418,6 @@ __global__ __launch_bounds__(WM* WN * 64) void k_gemm8(const GemmArgs g) {
       for (int nj = 0; nj < NJ; ++nj) asm volatile("" : "+v"(acc[mi][nj]));
     wait_and_meet<63>();  // st1 has been read
     leave();
-    drain = i0 + BM > g.M || j0 + (GLU ? BN / 2 : BN) > g.N;
     tile += mine;
     if (tile >= run_end) break;
     i0 = next_i;
