@@ -2,8 +2,12 @@
 //   y = act(z + bias) + res,  z[t, n] = sum over blocks b of sx[b, t] sw[b, n] times the sum
 //   over the block of the products of codes.
 //
-// The projections' kernel; a stage brings the scales of its rows into LDS beside the codes.  The
-// sums of a stage (64 k) start from 0 and are added, times their scales, in fp32.
+// A step brings the scales of its rows into LDS beside the codes; its sums start from 0 and are
+// added, times their scales, in fp32.  Results in bf16 take the tiles of two steps (256 and 128
+// wide) or the projections' kernel with the 8-bit instruction, results in fp32 the latter with
+// exact products.  Calls in a graph: 32768 x 2048 x 2048 124 us (2.2 PFLOP/s), with residual 158;
+// 8192^3 430 (2.55), a scale for each row of the weight 520; 2000 x 4096 x 2048 23; in fp32
+// 2048 x 1024 x 16384 101 with its residual, 8192^3 1135 (0.97).
 #include "pk_gemm8.h"
 
 namespace pk {

