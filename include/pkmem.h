@@ -577,7 +577,8 @@ int mem_quantize_blocks(const void* x, pkmem_dtype dt, int64_t R, int C, int til
  *   y[t,:] = act(z[t,:]) + res[t,:].
  *   x  [T, K], w [N, K] PKMEM_E4M3; x_scale [ceil(K / 128), T]; w_scale [ceil(K / 128), N], or
  *      with w_tile [ceil(K / 128), ceil(N / 128)], one for each 128 rows of w.
- *   bias, res, act, z_out, y_out, y_dt, limits (K % 16 == 0) and refusals as mem_linear's.
+ *   bias, res, act, z_out, y_out, y_dt, limits (K % 16 == 0) and refusals as mem_linear's;
+ *      for y_dt PKMEM_F32 ceil(T / 128) * ceil(N / 128) < 2^23.
  *   Sums: for y_dt PKMEM_F32, and for up to 8 tokens, products are exact and added in
  *   fp32.  For PKMEM_BF16 the products of 8 k are aligned to the largest of them and cut 13
  *   bits below it, and then added in fp32: each is within 2^-13 of that largest one, far

@@ -1193,6 +1193,9 @@ int mem_linear_blocks(const void* x, const void* w, const float* x_scale, const 
   if (rc) return rc;
   if (!tiles_fit(T, N)) return fail(PKMEM_ERR_UNSUPPORTED, "%s: 2^23 tiles of 256 x 256 or more", fn);
   if (!dtype_ok(y_dt)) return fail(PKMEM_ERR_INVALID, "%s: y_dt must be PKMEM_F32 or PKMEM_BF16", fn);
+  // exact products take 128-wide tiles of 512 threads: fewer than 2^32 a launch
+  if (y_dt == PKMEM_F32 && (T + 127) / 128 * ((N + 127) / 128) >= (int64_t(1) << 23))
+    return fail(PKMEM_ERR_UNSUPPORTED, "%s: 2^23 tiles of 128 x 128 or more in fp32", fn);
   if (act < PKMEM_ACT_NONE || act > PKMEM_ACT_GELU) return fail(PKMEM_ERR_INVALID, "%s: unknown activation %d", fn, act);
   if (T > 0 && (!x || !w || !y_out || !x_scale || !w_scale)) return fail(PKMEM_ERR_INVALID, "%s: null pointer", fn);
   if (!aligned(x, 16) || !aligned(w, 16) || !aligned(x_scale, 4) || !aligned(w_scale, w_tile ? 4 : 16) || !aligned(bias, 16) ||

@@ -124,6 +124,7 @@ def test_quantize_blocks_rejects(lib, kw, code, text):
     (dict(ydt=E4M3), INVALID, "y_dt"), (dict(act=9), INVALID, "activation"), (dict(T=-1), INVALID, "T must"),
     (dict(T=1 << 31), UNSUPPORTED, "2^31"), (dict(N=4), UNSUPPORTED, "multiple of 8"), (dict(K=24), UNSUPPORTED, "multiple of 16"),
     (dict(N=(1 << 20) + 8), UNSUPPORTED, "2^20"), (dict(T=(1 << 31) - 1, N=1 << 20), UNSUPPORTED, "tiles"),
+    (dict(T=(1 << 30) - 127, N=8, K=16, ydt=F32), UNSUPPORTED, "128 x 128"), (dict(T=(1 << 30) - 128, N=8, K=16, ydt=F32), HIP, ""),
     (dict(x=None), INVALID, "null"), (dict(w=None), INVALID, "null"), (dict(sx=None), INVALID, "null"),
     (dict(sw=None), INVALID, "null"), (dict(y=None), INVALID, "null"), (dict(w=B + 4), INVALID, "aligned"),
     (dict(sx=C + 2), INVALID, "aligned"), (dict(sw=D + 4), INVALID, "aligned"), (dict(sw=D + 4, tile=1), HIP, ""),
