@@ -564,7 +564,8 @@ int mem_glu_backward(const void* dy, const void* z, pkmem_dtype dt, int act, int
  *   qt_out  [C, R16] PKMEM_E4M3, R16 = R rounded up to 16, codes past R zero, with
  *           scale_t_out fp32 [ceil(R / 128), C] (tile: [ceil(R / 128), ceil(C / 128)]).
  *   scale = max(max|x| / 448, 2^-126) of the block, codes the numbers nearest to
- *   448 x / max|x|, ties to even, exactly.
+ *   448 x / max|x|, ties to even, exactly.  A NaN is stored as NaN and leaves its block's
+ *   scale alone; an infinity makes the scale infinite, its own code NaN and the others' 0.
  * Either pair may be NULL.  Buffers 16-byte aligned, scales 4; no two may share bytes
  * (refused).  R = 0 is a valid no-op.
  * ------------------------------------------------------------------------ */
@@ -582,7 +583,8 @@ int mem_quantize_blocks(const void* x, pkmem_dtype dt, int64_t R, int C, int til
  *   Sums: for y_dt PKMEM_F32, and for up to 8 tokens, products are exact and added in
  *   fp32.  For PKMEM_BF16 the products of 8 k are aligned to the largest of them and cut 13
  *   bits below it, and then added in fp32: each is within 2^-13 of that largest one, far
- *   below half a step of the result unless the sum cancels.
+ *   below half a step of the result unless the sum cancels.  With w_tile the two scales are
+ *   multiplied first: a product of theirs below 2^-126 loses digits, one past 2^128 overflows.
  * The products of a training step: y from x and w; dx [T, K] from the gradient's rows and
  * w's columns (qt_out as w, N and K changed round); grad_w from both columns, with
  * res = y_out = grad_w in PKMEM_F32 to accumulate.

@@ -52,7 +52,9 @@ struct Coder<float> {
     if (low) scale = 0x1p-126f;
     const uint32_t e = __float_as_uint(top) & 0x7F800000u;
     f = low ? 0x1p126f : __uint_as_float(0x7F800000u - e);
-    const float num = low ? 1.f : top * f, den = low ? 1.f : E4M3_MAX;
+    // max|x| infinite: f is 0, all codes but the infinite numbers' become 0
+    const bool one = low || !(top < __builtin_inff());
+    const float num = one ? 1.f : top * f, den = one ? 1.f : E4M3_MAX;
     div = num / den;
     inv = 1.f / div;
     rest = fmaf(-div, den, num) * __builtin_amdgcn_rcpf(den);

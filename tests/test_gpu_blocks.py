@@ -101,6 +101,20 @@ def test_nan_and_infinity_stay_in_their_block(gpu_lib):
     assert torch.equal(v, w)
 
 
+@pytest.mark.parametrize("tile", [False, True], ids=["rows", "tiles"])
+@pytest.mark.parametrize("dt", [F32, BF16])
+@pytest.mark.parametrize("sign", [1.0, -1.0])
+def test_codes_beside_an_infinity(gpu_lib, dt, tile, sign):
+    x = randn((128, 128), dt, 1)
+    x[7, 9], x[70, 9], x[90, 3] = sign * float("inf"), float("nan"), -3.0e38
+    q, s, qt, st = pk.mem_quantize_blocks(x, tile=tile, want_cols=True)
+    for code, scale, line in ((q, s, 7), (qt.t(), st, 9)):
+        v = code.float() if tile else code.float()[7] if line == 7 else code.float()[:, 9]
+        hit = ~torch.isfinite(x if tile else x[7] if line == 7 else x[:, 9])
+        assert torch.isnan(v[hit]).all() and (v[~hit] == 0).all()
+        assert torch.isinf(scale).all() if tile else torch.isinf(scale[0, line]) and torch.isfinite(scale).sum() == 127
+
+
 # T, N, K: one row to few, edges of the 32-, 64-, 128- and 256-wide tiles, k of a part of a stage,
 # of a part of a block, of many blocks
 SHAPES = [(1, 8, 16), (1, 2048, 528), (3, 520, 1040), (8, 136, 80), (9, 8, 144), (17, 136, 80), (33, 128, 128), (65, 264, 208),
