@@ -433,7 +433,7 @@ template <int DT, int BM, int BN, int WM, int WN, int MODE>
 void gemm8_launch(GemmArgs g, hipStream_t st) {
   g.tiles_m = ceil_div(g.M, BM);
   g.tiles_n = ceil_div(g.N, MODE == G_GLU ? BN / 2 : BN);
-  const int tiles = g.tiles_m * g.tiles_n, most = BM == 256 ? 256 : 512;  // of the chip's 256 CUs, by LDS
+  const int tiles = g.tiles_m * g.tiles_n, most = step_tile_places(BM == 256 ? TILE_256 : TILE_128);
   hipLaunchKernelGGL((k_gemm8<DT, BM, BN, WM, WN, MODE>), dim3((unsigned)(tiles < most ? tiles : most)), dim3(WM * WN * 64), 0,
                      st, g);
 }

@@ -32,6 +32,10 @@ inline int pick_tile(bool f32, int64_t M, int64_t N) {
   return mid <= 256 ? TILE_128_K2 : TILE_128;
 }
 
+// Workgroups of the tiles of two steps (pk_gemm8.h) that 256 CUs hold at once, by LDS; of more tiles
+// each takes one after another.
+inline int step_tile_places(int tile) { return tile == TILE_256 ? 256 : 512; }
+
 // grad_W [N, K] from T tokens: the tile and the number of splits of the tokens
 // with the least time by these measured parts: a stage of 64 bytes of k takes a
 // workgroup 0.85 us (256 wide), 0.35 (128, two groups), 0.1 (64, four groups) or
