@@ -535,8 +535,9 @@ int mem_layernorm_backward(const void* dy, const void* h, const void* weight, pk
  *   act     pkmem_act, with mem_linear's precision.
  *   z_out   [T, 2 N] dtype y_dt: z (what mem_glu_backward needs); NULL to skip it.
  *   y_out   [T, N] dtype y_dt.
- * Types, exactness of products and limits as mem_linear's with 2 N in place of N (for
- * PKMEM_E4M3 with y_dt PKMEM_BF16 products as in mem_linear_blocks);
+ * Types, exactness of products and limits as mem_linear's with 2 N in place of N, but that
+ * PKMEM_E4M3 with y_dt PKMEM_BF16 cuts products as mem_linear_blocks does where T > 8 and z has
+ * more than 256 tiles of 128 x 128 (PKMEM_F32 is for sums that cancel);
  * N % 8 == 0 and N <= 2^19.  No output may share bytes with another buffer (refused).
  * All buffers 16-byte aligned.  T = 0 is a valid no-op.
  * ------------------------------------------------------------------------ */
@@ -581,10 +582,13 @@ int mem_quantize_blocks(const void* x, pkmem_dtype dt, int64_t R, int C, int til
  *   bias, res, act, z_out, y_out, y_dt, limits (K % 16 == 0) and refusals as mem_linear's;
  *      for y_dt PKMEM_F32 ceil(T / 128) * ceil(N / 128) < 2^23.
  *   Sums: for y_dt PKMEM_F32, and for up to 8 tokens, products are exact and added in
- *   fp32.  For PKMEM_BF16 the products of 8 k are aligned to the largest of them and cut 13
- *   bits below it, and then added in fp32: each is within 2^-13 of that largest one, far
- *   below half a step of the result unless the sum cancels.  With w_tile the two scales are
- *   multiplied first: a product of theirs below 2^-126 loses digits, one past 2^128 overflows.
+ *   fp32.  For PKMEM_BF16 and more tokens the products of 8 k are aligned to the largest of
+ *   them and cut 13 bits below it, and then added in fp32: a sum is within 2^-10 of the sum of
+ *   its sizes (a quarter of bf16's half step where nothing cancels; what cancels leaves no more
+ *   digits than that).  PKMEM_F32 is for sums that cancel.
+ *   With w_tile and more than 8 tokens the two scales are multiplied first: a product of theirs
+ *   below 2^-126 loses digits, one past 2^128 overflows.  Else a block's sum (at most 2^25) takes
+ *   w's scale first, which overflows past 2^103.
  * The products of a training step: y from x and w; dx [T, K] from the gradient's rows and
  * w's columns (qt_out as w, N and K changed round); grad_w from both columns, with
  * res = y_out = grad_w in PKMEM_F32 to accumulate.

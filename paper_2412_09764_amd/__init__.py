@@ -905,7 +905,9 @@ def mem_glu(x: torch.Tensor, w: torch.Tensor, bias=None, *, act="silu", x_scale=
     """The gated feed-forward part: with z = x w^T + bias, act(z[:, :N]) * z[:, N:].
 
     x [T, K]; w [2 N, K] (the gate's N rows, then the up projection's), bias [2 N]; act, 8-bit
-    operands with x_scale [T] and w_scale [2 N], and out_dtype as for mem_linear.
+    operands with x_scale [T] and w_scale [2 N], and out_dtype as for mem_linear.  bfloat16
+    results of many 8-bit rows (more than 256 tiles of 128 x 128 of z) cut products 13 bits
+    below the largest of 8 along K: ask for float32 where sums cancel.
     Returns (y [T, N], z [T, 2 N], None unless want_z)."""
     _here(x, w, bias, x_scale, w_scale, y_out, z_out)
     T, K = x.shape
@@ -1010,7 +1012,8 @@ def mem_linear_blocks(x: torch.Tensor, w: torch.Tensor, x_scale: torch.Tensor, w
     128 x 128 tiles, [ceil(K/128), ceil(N/128)] (mem_quantize_blocks).
 
     out_dtype: float32 or bfloat16 (the default), the dtype of bias and residual too; in
-    float32 products are exact.  y_out may be residual.  Returns (y, z) with z = x w^T + bias
+    float32, and for up to 8 rows, products are exact, else they are cut 13 bits below the
+    largest of 8 along K: ask for float32 where sums cancel.  y_out may be residual.  Returns (y, z) with z = x w^T + bias
     before the activation, None unless want_z."""
     _here(x, w, x_scale, w_scale, bias, residual, y_out, z_out, workspace)
     T, K = x.shape
