@@ -8,10 +8,12 @@
 // turn, so that one lane has both numbers of a result in its registers: z is written only
 // for a backward that asks for it.
 //
-// Calls in a graph: 16384 x 4096 x 1024 bf16 230 us, with z 271 (403 MB written); 8192 x 4096 x
-// 8192 bf16 745 (1.48 PFLOP/s), e4m3 382 (2.88); 2000 x 8192 x 2048 e4m3 61-65; 1 x 8192 x 2048
-// bf16 16 (the weight at 4.1 TB/s).  The element-wise backward of 16384 x 4096 bf16 107 us
-// (6.3 TB/s); its exponentials are the exact ones, so that dz is rounded as the definition's.
+// Calls in a graph, on three boxes: 16384 x 4096 x 1024 bf16 230-234 us, with z 243-271 (403 MB
+// written); 8192 x 4096 x 8192 bf16 745-769 (1.43-1.48 PFLOP/s), e4m3 369-387 (2.8-3.0); 2000 x
+// 8192 x 2048 e4m3 55-58, to fp32 (exact products) 111-118, fp32 628-661 (0.20-0.21); 1 x 8192 x
+// 2048 bf16 16 (weights apart, each read at 4.2 TB/s), e4m3 10.7 (3.1), fp32 33 (4.0).  The
+// element-wise backward of 16384 x 4096 bf16 107-117 us (5.7-6.3 TB/s); its exponentials are
+// the exact ones, so that dz is rounded as the definition's.
 #include "pk_gemm8.h"
 
 namespace pk {
@@ -31,7 +33,8 @@ void glu_launch(const GemmArgs& g, hipStream_t st) {
     hipLaunchKernelGGL((k_gemm_few<DT, G_GLU>), dim3((unsigned)ceil_div(g.N, 16)), dim3(FEW_WAVES * 64), 0, st, g);
     return;
   }
-  // The tiles of a product with 2 N columns.  Tiles 64 high against 32 high at sizes where
+  // The tiles of a product with 2 N columns (pick_tile, where both widths of the tiles of two
+  // steps are measured).  Tiles 64 high against 32 high at sizes where
   // the rule takes either: 200 x 1024 x 4096 bf16 14.8 against 16.9 us, 777 x 328 x 200 fp32
   // 8.6 against 12.0; the other way round 300 x 512 x 1024 bf16 6.9 against 6.2 and
   // 64 x 4096 x 2048 bf16 13.5 against 11.6, which no rule on the number of tiles alone parts.

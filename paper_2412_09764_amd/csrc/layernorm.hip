@@ -12,7 +12,8 @@
 // mean and variance for the roundings of the first one.
 //
 // Memory bound: 32768 x 2048 bf16 with residual 84-86 us (6.3 TB/s), called in turn with its
-// backward 100; backward 88-94 (5.7-6.1); 16384 x 2048 fp32 81 and 91.  Below some 4000 rows a
+// backward 96-100; backward 88-94 (dy, h, dsum read and dx written at 5.7-6.1); 16384 x 2048 fp32
+// 79-81 and 88-91.  Below some 4000 rows a
 // call is bound by its launch (777 x 200 fp32: 2.8 and 3.9 us of kernel, joining the parts 4.1).
 #include "pk_internal.h"
 #include "pk_norm.h"
@@ -260,7 +261,7 @@ __global__ __launch_bounds__(1024) void k_add_two(const float* __restrict__ part
 }
 
 // Chunks per lane and waves per row for rows of C chunks: one wave up to 256 chunks (4 KiB), a
-// workgroup of four above (32768 x 4096 bf16 forward 190 us, with one wave 198; backward 188,
+// workgroup of four above (32768 x 4096 bf16 forward 190-192 us, with one wave 198; backward 188,
 // its two sums for each column would not fit one wave's registers).
 #define PK_LAYERNORM_DISPATCH(C, F)                                       \
   do {                                                                    \

@@ -32,6 +32,18 @@ inline int pick_tile(bool f32, int64_t M, int64_t N) {
   return mid <= 256 ? TILE_128_K2 : TILE_128;
 }
 
+// The products in blocks and the gated part (with 2 N columns) take their tiles by the same rule,
+// which was measured on them too: codes with tiled scales of 2048 k, gated part in bf16 of 2048 k,
+// gated part in codes of 2048 k, us in tiles of two steps 256 wide and 128 wide:
+//   2000 x 8192 (256 taken) 34 / 38, 51 / 59, 29 / 34;   4096 x 4096 (256) 34 / 38, 50 / 59, 30 / 33;
+//   6000 x 4096 (256) 56 / 55, 88 / 87, 50 / 48;         3000 x 4096 (128) 31 / 31, 48 / 51, 28 / 29;
+//   2000 x 4096 (128) 29 / 21, 45 / 31, 26 / 18;         3000 x 2048 (128) 27 / 19, 44 / 27, 25 / 16.
+// Where it takes TILE_128_K2, at 128 to 256 tiles, which is k_gemm's alone, the 128-wide tiles of
+// two steps would be faster but for the gated part in bf16 of a long k: 2000 x 2048 of 2048 k in
+// blocks 17.9 / 14.1 (a scale for each row 20.8 / 16.3), 1000 x 4096 16.9 / 14.0; gated 2000 x 4096
+// of 1024 k in bf16 13.6 / 11.6, of 2048 k 24.5 / 25.3, in codes 17.3 / 11.8.  In codes the
+// gated part's products are exact there and would not be in those tiles.
+
 // Workgroups of the tiles of two steps (pk_gemm8.h) that 256 CUs hold at once, by LDS; of more tiles
 // each takes one after another.
 inline int step_tile_places(int tile) { return tile == TILE_256 ? 256 : 512; }

@@ -9,7 +9,9 @@
 // and turns the codes round in LDS.
 //
 // 32768 x 2048 bf16 rows 38 us (5.2 TB/s of reads and writes); 16384 x 2048 bf16 both ways 37
-// (3.6 TB/s; the vector unit is busy 36% of it); 8192 x 2048 fp32 in tiles both ways 22.6 (4.4).
+// (3.6 TB/s; the vector unit is busy 36% of it: a workgroup loads, meets, rounds, turns, meets and
+// stores its square with no load of another under way); 8192 x 2048 fp32 in tiles both ways
+// 22.6-23.6 (4.3-4.4).
 #include "pk_internal.h"
 #include "pk_row.h"
 
