@@ -5,7 +5,7 @@
 // A step brings the scales of its rows into LDS beside the codes; its sums start from 0 and are
 // added, times their scales, in fp32.  Results in bf16 take the tiles of two steps (256 and 128
 // wide) or the projections' kernel with the 8-bit instruction, results in fp32 the latter with
-// exact products.  Calls in a graph, on three boxes: 32768 x 2048 x 2048 124-133 us (2.1-2.2
+// exact products.  Calls in a graph, on three cards: 32768 x 2048 x 2048 124-133 us (2.1-2.2
 // PFLOP/s), with residual 153-158, a scale for each row of the weight 143-151 (two vector
 // instructions for each sum of a block instead of one); 8192^3 422-442 (2.5-2.6), for each row
 // 504-528; 2000 x 4096 x 2048 22, for each row 24; in fp32 for each row 2048 x 1024 x 16384 88-101

@@ -8,7 +8,7 @@
 // turn, so that one lane has both numbers of a result in its registers: z is written only
 // for a backward that asks for it.
 //
-// Calls in a graph, on three boxes: 16384 x 4096 x 1024 bf16 230-234 us, with z 243-271 (403 MB
+// Calls in a graph, on three cards: 16384 x 4096 x 1024 bf16 230-234 us, with z 243-271 (403 MB
 // written); 8192 x 4096 x 8192 bf16 745-769 (1.43-1.48 PFLOP/s), e4m3 369-387 (2.8-3.0); 2000 x
 // 8192 x 2048 e4m3 55-58, to fp32 (exact products) 111-118, fp32 628-661 (0.20-0.21); 1 x 8192 x
 // 2048 bf16 16 (weights apart, each read at 4.2 TB/s), e4m3 10.7 (3.1), fp32 33 (4.0).  The
